@@ -14,6 +14,9 @@
  * queries together with the row statistics that let sablock_score read K once; behind them,
  * sablock_decode_attention is one decode step over the cache they leave (or over the full cache, for comparison).
  * sablock_score_all_heads / sablock_compact_shared are the variant with one retained set per layer.
+ * sablock_compact_paged puts the retained rows into the pages of a cache instead, sablock_append_paged adds new tokens to
+ * those (rotating queries and keys on the way), sablock_decode_paged is the decode step over them, and
+ * sablock_select_pages picks the pages that such a step should read.
  *
  * Conventions shared by all calls
  * -------------------------------
@@ -361,6 +364,114 @@ SABLOCK_API sablock_status sablock_decode_workspace_bytes(const sablock_shape *s
 SABLOCK_API sablock_status sablock_decode_attention(const sablock_shape *shape, const void *q, const void *k_cache,
                                         const void *v_cache, const int32_t *n_sel, int32_t budget, float *out,
                                         void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The paged cache: what a serving program keeps between tokens, with room for as many as it likes.  The rows of a sequence lie in
+ * pages of page_size rows of a pool; page_table [n_seq][max_pages] (device int32) names them: row r of sequence s is row
+ * r % page_size of page page_table[s][r / page_size], in every layer and KV head alike.  lengths [n_seq] (device int32) are
+ * the rows that a sequence has.  Rows count from 0 without a gap and are NOT positions: behind a compressed prompt the
+ * next row is budget + W, the next position L.
+ * Page bounds (optional): [n_layers][n_pages][n_kv_heads][2][D], dense, dtype of the cache: per page, layer and KV head the least
+ *   and the largest value of every element of K over the page's rows.  sablock_compact_paged and sablock_append_paged write
+ *   them where they are given, sablock_select_pages reads them.  A page's bounds mean something once its row 0 was written
+ *   with them.
+ * Device data: table entries outside [0, n_pages) name no page: what would be written there is dropped, their rows are
+ *   skipped by attention and their scores are -infinity.  Lengths count as 0 .. max_pages * page_size.  Different entries within
+ *   the sequences' lengths may name one page (a shared prefix); then no call may write to it.
+ * Limits: n_seq <= 4096, n_seq * n_layers * n_kv_heads <= 65535, page_size a power of two in [16, 256],
+ *   max_pages * page_size <= 2^30; UNSUPPORTED beyond.  The pools are 16-byte aligned, strides (in elements) multiples of 8, [3] at least head_dim;
+ *   the stride of an axis with one entry is not looked at. */
+typedef struct {
+    int32_t n_seq;
+    int32_t n_layers;
+    int32_t n_q_heads;        /* multiple of n_kv_heads */
+    int32_t n_kv_heads;
+    int32_t head_dim;         /* D: multiple of 8, 8 <= D <= 256 */
+    int32_t dtype;            /* sablock_dtype of the pools, the bounds and the new rows */
+    int32_t page_size;        /* rows per page */
+    int32_t n_pages;          /* pages of the pool */
+    int32_t max_pages;        /* entries of a sequence in the page table */
+    int32_t compute_units;    /* as in sablock_tuning */
+    int32_t reserved[2];      /* must be 0 */
+    int64_t k_stride[4];      /* K pool: layer, page, KV head, row */
+    int64_t v_stride[4];      /* V pool, same axes */
+} sablock_pages;
+
+/* Cache construction (end of Sec. 3.3) into pages: per problem, rows idx[0 .. n) of K and V, n = min(budget, T), bit for
+ * bit to rows 0 .. n-1 of the sequence, then, if append_window, the W most recent rows behind them without a gap (the
+ * gap of sablock_compact's dense layout has no counterpart).
+ *   shape       as in sablock_compact; its n_seq, n_layers, n_kv_heads, head_dim and dtype are those of `pages`
+ *   idx         [P][budget] int32 as written by sablock_select, which fills n entries for every problem; an entry outside
+ *               [0, L) gives a row of zeros
+ *   bounds      nullable; written for every page that gets a row
+ *   lengths_out nullable, [n_seq] int32: n + (append_window ? W : 0)
+ * INVALID_ARG if the rows do not fit max_pages pages. */
+SABLOCK_API sablock_status sablock_compact_paged(const sablock_shape *shape, const void *k, const void *v, const int32_t *idx,
+                                     int32_t budget, int32_t append_window, const sablock_pages *pages,
+                                     const int32_t *page_table, void *k_pool, void *v_pool, void *bounds /* nullable */,
+                                     int32_t *lengths_out /* nullable */, void *stream);
+
+/* New tokens of a sequence: one while decoding, a prompt's worth otherwise.  Strides in elements (sequence, layer, head,
+ * token), so that q, k and v may be views of one projection's output; multiples of 8, the token's at least head_dim where
+ * n_new > 1.  The stride of an axis with one entry is not looked at. */
+typedef struct {
+    int32_t n_new;            /* tokens per sequence in the tensors; a sequence may have fewer, see counts */
+    int32_t rotary_dim;       /* R: the first R elements of a head are rotated; a multiple of 16, 0 <= R <= head_dim */
+    int32_t interleaved;      /* pairs: 0 = (i, i + R/2), 1 = (2i, 2i + 1), i < R/2 */
+    int32_t reserved;         /* must be 0 */
+    int64_t q_stride[4];      /* [n_seq][n_layers][n_q_heads][n_new][D] */
+    int64_t k_stride[4];      /* [n_seq][n_layers][n_kv_heads][n_new][D] */
+    int64_t v_stride[4];
+} sablock_new_tokens;
+
+/* New rows of the paged cache.  Token j of sequence s, j < c = counts[s], has position positions[s] + j and becomes row
+ * lengths[s] - c + j: `lengths` are those WITH the new tokens, so that one array serves all layers' calls of a step, and the
+ * attention behind them.  K's and q's pairs (a, b) turn by the angle t = position * inv_freq[i]:
+ *   (a cos t - b sin t, b cos t + a sin t)
+ * (t in fp64, the products in fp32, one rounding to the dtype); V and the elements behind R are copied.
+ *   q, q_out    both or neither; q_out [n_seq][n_layers][n_q_heads][n_new][D] dense, of the dtype; it may not overlap q
+ *   counts      nullable (every sequence has n_new), or [n_seq] int32, taken as 0 .. n_new and at most lengths[s]; rows of
+ *               q_out and of the pools that belong to no token stay as they are
+ *   positions   [n_seq] int32, of each sequence's first new token; may be NULL where R = 0, as may inv_freq
+ *   inv_freq    [R/2] fp32, radians per position
+ *   bounds      nullable; those of the touched pages are extended by the new rows (begun, where row 0 is among them)
+ * Two sequences may not add rows to one page. */
+SABLOCK_API sablock_status sablock_append_paged(const sablock_pages *pages, const sablock_new_tokens *tokens,
+                                    const void *q /* nullable */, const void *k, const void *v,
+                                    const int32_t *counts /* nullable */, const int32_t *positions, const float *inv_freq,
+                                    const int32_t *page_table, const int32_t *lengths, void *q_out /* nullable */,
+                                    void *k_pool, void *v_pool, void *bounds /* nullable */, void *stream);
+
+/* Decode-time attention of ONE new token per sequence over its pages (Sec. 2.1, Eq. 1 with a single query position):
+ *   out[h] = softmax_r(<q[h], K[r]> / sqrt(D)) . V[r]  over the rows r < lengths[s], or those of the listed pages.
+ *   q           [n_seq][n_layers][n_q_heads][D], dense, dtype of the cache
+ *   page_list   nullable, or [P][n_listed] int32 as written by sablock_select_pages: the pages (places in the sequence's row of the
+ *               table) whose rows count, in the first min(n_listed, pages of the sequence) entries; entries outside the sequence's pages
+ *               are skipped, one that comes twice counts twice
+ *   out         [n_seq][n_layers][n_q_heads][D] fp32, dense.  A sequence without any row gives zeros.
+ *   ws          at least sablock_decode_paged_workspace_bytes(pages) bytes, 16-byte aligned
+ * What pages hold behind a sequence's last row, NaN and infinity too, does not matter.
+ * Supported: G <= 16; head_dim a multiple of 32 (bf16) or 16 (fp32).  Errors as for the other calls. */
+SABLOCK_API sablock_status sablock_decode_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out);
+SABLOCK_API sablock_status sablock_decode_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool,
+                                    const int32_t *page_table, const int32_t *lengths,
+                                    const int32_t *page_list /* nullable */, int32_t n_listed, float *out,
+                                    void *ws, size_t ws_bytes, void *stream);
+
+/* The pages that a decode step reads when it may not read all: per problem, the first n_first and the last n_last pages of the
+ * sequence and, of the others, those with the best scores, n_pick in all.  A page's score is a bound of its rows' logits,
+ *   max over the G query heads of  sum_d max(q_d lo_d, q_d hi_d) >= sqrt(D) * (any logit of the page),
+ * with lo, hi the page bounds; summed in fp64 and rounded to fp32 once.  Equal scores: the lower page first; a score that
+ * is not a number counts as the largest.
+ *   q           [n_seq][n_layers][n_q_heads][D], dense, dtype of the cache
+ *   list_out    [P][n_pick] int32: pages in ascending order, all of them where the sequence has no more than n_pick; -1 behind
+ *               the last
+ *   ws          at least sablock_select_pages_workspace_bytes(pages) bytes, 16-byte aligned
+ * n_pick >= 1, n_first, n_last >= 0, n_first + n_last <= n_pick (INVALID_ARG otherwise); G <= 16. */
+SABLOCK_API sablock_status sablock_select_pages_workspace_bytes(const sablock_pages *pages, size_t *bytes_out);
+SABLOCK_API sablock_status sablock_select_pages(const sablock_pages *pages, const void *q, const void *bounds,
+                                    const int32_t *page_table, const int32_t *lengths, int32_t n_pick, int32_t n_first,
+                                    int32_t n_last, int32_t *list_out, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

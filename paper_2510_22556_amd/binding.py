@@ -27,7 +27,9 @@ EXPORTS = ("sablock_version", "sablock_last_error", "sablock_workspace_bytes", "
            "sablock_decode_attention", "sablock_score_all_heads_workspace_bytes", "sablock_score_all_heads",
            "sablock_compact_shared", "sablock_search_select", "sablock_window_attention_workspace_bytes",
            "sablock_window_attention", "sablock_score_static", "sablock_stream_probe", "sablock_validate_segments",
-           "sablock_segment_slices", "sablock_segment_slice_count", "sablock_segment_slice_offsets")
+           "sablock_segment_slices", "sablock_segment_slice_count", "sablock_segment_slice_offsets",
+           "sablock_compact_paged", "sablock_append_paged", "sablock_decode_paged_workspace_bytes", "sablock_decode_paged",
+           "sablock_select_pages_workspace_bytes", "sablock_select_pages")
 
 
 class SablockError(RuntimeError):
@@ -53,6 +55,22 @@ class CShape(ctypes.Structure):
 
 class CHparams(ctypes.Structure):
     _fields_ = [("eps", ctypes.c_float), ("alpha", ctypes.c_float), ("eta", ctypes.c_float), ("tau", ctypes.c_float)]
+
+
+class CPages(ctypes.Structure):
+    """A paged cache (``sablock_pages``)."""
+
+    _fields_ = [("n_seq", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("compute_units", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2),
+                ("k_stride", ctypes.c_int64 * 4), ("v_stride", ctypes.c_int64 * 4)]
+
+
+class CNewTokens(ctypes.Structure):
+    """The new tokens of an append (``sablock_new_tokens``)."""
+
+    _fields_ = [("n_new", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64 * 4), ("k_stride", ctypes.c_int64 * 4), ("v_stride", ctypes.c_int64 * 4)]
 
 
 def load():
@@ -99,6 +117,13 @@ def load():
         lib.sablock_compact_shared.argtypes = [sp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
         lib.sablock_window_attention_workspace_bytes.argtypes = [sp, ctypes.POINTER(ctypes.c_size_t)]
         lib.sablock_window_attention.argtypes = [sp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        pp = ctypes.POINTER(CPages)
+        lib.sablock_compact_paged.argtypes = [sp, vp, vp, vp, i32, i32, pp, vp, vp, vp, vp, vp, vp]
+        lib.sablock_append_paged.argtypes = [pp, ctypes.POINTER(CNewTokens)] + [vp] * 13
+        lib.sablock_decode_paged_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
+        lib.sablock_decode_paged.argtypes = [pp, vp, vp, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
+        lib.sablock_select_pages_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
+        lib.sablock_select_pages.argtypes = [pp, vp, vp, vp, vp, i32, i32, i32, vp, vp, ctypes.c_size_t, vp]
         for n in EXPORTS[2:]:
             getattr(lib, n).restype = ctypes.c_int
         _lib = lib
@@ -352,6 +377,93 @@ def sablock_decode_attention(shape: CShape, q, k_cache, v_cache, out, ws, n_sel=
                                            _stream(stream)))
 
 
+def make_pages(k_pool, v_pool, page_table, n_q_heads: int, compute_units: int = 0) -> CPages:
+    """Descriptor of a paged cache from its pools ``[n_layers, n_pages, Hkv, page_size, D]`` (any strides on the four outer axes) and
+    ``page_table [n_seq, max_pages]`` int32."""
+    import torch
+
+    assert k_pool.dim() == 5 and v_pool.shape == k_pool.shape and k_pool.stride(-1) == 1 and v_pool.stride(-1) == 1
+    assert k_pool.dtype == v_pool.dtype and k_pool.dtype in (torch.float32, torch.bfloat16)
+    assert page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.is_contiguous()
+    c = CPages()
+    c.n_layers, c.n_pages, c.n_kv_heads, c.page_size, c.head_dim = k_pool.shape
+    c.n_seq, c.max_pages = page_table.shape
+    c.n_q_heads, c.compute_units = int(n_q_heads), int(compute_units)
+    c.dtype = SABLOCK_F32 if k_pool.dtype == torch.float32 else SABLOCK_BF16
+    for a in range(4):
+        c.k_stride[a], c.v_stride[a] = k_pool.stride(a), v_pool.stride(a)
+    return c
+
+
+def make_new_tokens(k, v, q=None, rotary_dim: Optional[int] = None, interleaved: bool = False) -> CNewTokens:
+    """Descriptor of the new tokens of an append: ``k, v [n_seq, n_layers, Hkv, n_new, D]``, ``q [n_seq, n_layers, Hq, n_new, D]``, any
+    strides on the four outer axes; ``rotary_dim`` None = the whole head."""
+    assert k.dim() == 5 and v.shape == k.shape and k.stride(-1) == 1 and v.stride(-1) == 1 and k.dtype == v.dtype
+    assert q is None or (q.dim() == 5 and q.dtype == k.dtype and q.stride(-1) == 1 and (q.shape[:2] + q.shape[3:]) == (k.shape[:2] + k.shape[3:]))
+    t = CNewTokens()
+    t.n_new, t.rotary_dim, t.interleaved = k.shape[3], k.shape[4] if rotary_dim is None else int(rotary_dim), 1 if interleaved else 0
+    for a in range(4):
+        t.k_stride[a], t.v_stride[a] = k.stride(a), v.stride(a)
+        t.q_stride[a] = 0 if q is None else q.stride(a)
+    return t
+
+
+def sablock_compact_paged(shape: CShape, k, v, idx, budget: int, append_window: bool, pages: CPages, page_table, k_pool, v_pool, bounds=None,
+                          lengths_out=None, stream=None):
+    _check(load().sablock_compact_paged(ctypes.byref(shape), _ptr(k), _ptr(v), _ptr(idx), budget, 1 if append_window else 0, ctypes.byref(pages),
+                                        _ptr(page_table), _ptr(k_pool), _ptr(v_pool), _ptr(bounds), _ptr(lengths_out), _stream(stream)))
+
+
+def sablock_append_paged(pages: CPages, tokens: CNewTokens, k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q=None, q_out=None,
+                         counts=None, bounds=None, stream=None):
+    """``lengths`` are the rows of every sequence WITH the new tokens."""
+    _check(load().sablock_append_paged(ctypes.byref(pages), ctypes.byref(tokens), _ptr(q), _ptr(k), _ptr(v), _ptr(counts), _ptr(positions),
+                                       _ptr(inv_freq), _ptr(page_table), _ptr(lengths), _ptr(q_out), _ptr(k_pool), _ptr(v_pool), _ptr(bounds),
+                                       _stream(stream)))
+
+
+def sablock_decode_paged_workspace_bytes(pages: CPages) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().sablock_decode_paged_workspace_bytes(ctypes.byref(pages), ctypes.byref(out)))
+    return int(out.value)
+
+
+def sablock_decode_paged(pages: CPages, q, k_pool, v_pool, page_table, lengths, out, ws, page_list=None, stream=None):
+    """``page_list [P, n]`` int32, dense: the pages to read (``sablock_select_pages``); None = all."""
+    _check(load().sablock_decode_paged(ctypes.byref(pages), _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(lengths),
+                                       _ptr(page_list), 0 if page_list is None else page_list.shape[-1], _ptr(out), _ptr(ws),
+                                       ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def sablock_select_pages_workspace_bytes(pages: CPages) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().sablock_select_pages_workspace_bytes(ctypes.byref(pages), ctypes.byref(out)))
+    return int(out.value)
+
+
+def sablock_select_pages(pages: CPages, q, bounds, page_table, lengths, n_pick: int, list_out, ws, n_first: int = 1, n_last: int = 1, stream=None):
+    _check(load().sablock_select_pages(ctypes.byref(pages), _ptr(q), _ptr(bounds), _ptr(page_table), _ptr(lengths), n_pick, n_first, n_last,
+                                       _ptr(list_out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+class PagedCache:
+    """Pools, page table and lengths of a paged cache, page bounds where asked for, and the workspaces of the calls that read it.
+
+    Which pages a sequence has is the caller's to say: ``page_table`` starts as -1 (no page)."""
+
+    def __init__(self, n_seq: int, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, max_pages: int,
+                 dtype, device, bounds: bool = True):
+        import torch
+
+        self.k_pool, self.v_pool = (torch.zeros((n_layers, n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device) for _ in range(2))
+        self.bounds = torch.zeros((n_layers, n_pages, n_kv_heads, 2, head_dim), dtype=dtype, device=device) if bounds else None
+        self.page_table = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros((n_seq,), dtype=torch.int32, device=device)
+        self.pages = make_pages(self.k_pool, self.v_pool, self.page_table, n_q_heads)
+        self.ws = torch.empty((sablock_decode_paged_workspace_bytes(self.pages),), dtype=torch.uint8, device=device)
+        self.select_ws = torch.empty((sablock_select_pages_workspace_bytes(self.pages),), dtype=torch.uint8, device=device) if bounds else None
+
+
 class Buffers:
     """Device buffers for one call geometry: outputs of every step plus the workspace.
 
@@ -384,9 +496,10 @@ class Buffers:
 
 
 def compress(shape: CShape, q, k, v, seg: Segments, cand: Sequence[int], budget: int, buf: Buffers,
-             eps=1e-6, alpha=0.9, eta=1.0, tau=0.85, row_lse=None, stream=None, fused=True) -> Buffers:
+             eps=1e-6, alpha=0.9, eta=1.0, tau=0.85, row_lse=None, stream=None, fused=True, cache: Optional[PagedCache] = None) -> Buffers:
     """The whole hot path: score, refine, search_blocks + select (one call for both, or the two separate calls with
-    ``fused=False``: same results), compact."""
+    ``fused=False``: same results), compact: into ``buf.k_out`` / ``buf.v_out``, or into the pages of ``cache`` where one is given (its
+    ``lengths`` are written, and its bounds)."""
     # the calls above with their arguments marshalled once: small calls are bound by what the host does between launches
     lib, st, sp = load(), _stream(stream), ctypes.byref(shape)
     s, ent, s_tilde, topb, idx, n_sel = (_ptr(t) for t in (buf.s, buf.ent, buf.s_tilde, buf.topb, buf.idx, buf.n_sel))
@@ -401,6 +514,10 @@ def compress(shape: CShape, q, k, v, seg: Segments, cand: Sequence[int], budget:
     else:
         _check(lib.sablock_search_blocks(sp, s_tilde, *segs, *cl, budget, tau, bk, g, topb, *ws))
         _check(lib.sablock_select(sp, s_tilde, *segs, bk, g, topb, budget, idx, n_sel, *ws))
+    if cache is not None:
+        sablock_compact_paged(shape, k, v, buf.idx, budget, buf.append_window, cache.pages, cache.page_table, cache.k_pool, cache.v_pool,
+                              cache.bounds, cache.lengths, stream)
+        return buf
     _check(lib.sablock_compact(sp, kp, _ptr(v), idx, n_sel, budget, 1 if buf.append_window else 0, _ptr(buf.k_out),
                                _ptr(buf.v_out), st))
     return buf

@@ -625,4 +625,210 @@ sablock_status sablock_decode_attention(const sablock_shape *shape, const void *
                "sablock_decode_attention");
 }
 
+static bool axes_ok(const int64_t (&stride)[4], const int32_t (&n)[4], int64_t least, const char *who, const char *what, sablock_status *st)
+{
+    for (int a = 0; a < 4; ++a) {
+        if (n[a] <= 1) continue;
+        if (stride[a] < 0) { *st = fail(SABLOCK_ERR_INVALID_ARG, "%s: negative %s stride", who, what); return false; }
+        if (stride[a] % 8) {
+            *st = fail(SABLOCK_ERR_UNSUPPORTED, "%s: %s strides must be multiples of 8 elements (16-byte row alignment)", who, what);
+            return false;
+        }
+        if (stride[a] < least) { *st = fail(SABLOCK_ERR_INVALID_ARG, "%s: %s stride smaller than head_dim", who, what); return false; }
+    }
+    return true;
+}
+
+static sablock_status make_pages(const char *who, const sablock_pages *s, PageDims *d)
+{
+    if (!s) return fail(SABLOCK_ERR_INVALID_ARG, "%s: pages is NULL", who);
+    if (s->n_seq < 1 || s->n_layers < 1 || s->n_kv_heads < 1 || s->n_q_heads < 1)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_seq, n_layers, n_q_heads, n_kv_heads must be >= 1", who);
+    if (s->n_q_heads % s->n_kv_heads != 0)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_q_heads (%d) is not a multiple of n_kv_heads (%d)", who, s->n_q_heads, s->n_kv_heads);
+    if (s->dtype != SABLOCK_F32 && s->dtype != SABLOCK_BF16) return fail(SABLOCK_ERR_INVALID_ARG, "%s: unknown dtype %d", who, s->dtype);
+    if (s->head_dim < 8 || s->head_dim > 256 || s->head_dim % 8 != 0)
+        return fail(SABLOCK_ERR_UNSUPPORTED, "%s: head_dim %d: need a multiple of 8 in [8, 256]", who, s->head_dim);
+    if (s->n_pages < 1 || s->max_pages < 1 || s->page_size < 1)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: page_size, n_pages and max_pages must be >= 1", who);
+    if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1)))
+        return fail(SABLOCK_ERR_UNSUPPORTED, "%s: page_size %d: need a power of two in [16, 256]", who, s->page_size);
+    if (s->n_seq > MAX_PAGED_SEQ) return fail(SABLOCK_ERR_UNSUPPORTED, "%s: n_seq %d: at most %d per call", who, s->n_seq, MAX_PAGED_SEQ);
+    const int64_t P = (int64_t)s->n_seq * s->n_layers * s->n_kv_heads;
+    if (P > 65535) return fail(SABLOCK_ERR_UNSUPPORTED, "%s: n_seq*n_layers*n_kv_heads = %lld: at most 65535 per call", who, (long long)P);
+    if ((int64_t)s->max_pages * s->page_size > 1 << 30)
+        return fail(SABLOCK_ERR_UNSUPPORTED, "%s: max_pages * page_size: at most 2^30 rows per sequence", who);
+    if (s->compute_units < 0 || s->compute_units > 65536)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: compute_units %d: need 0 (ask the device) .. 65536", who, s->compute_units);
+    if (s->reserved[0] || s->reserved[1]) return fail(SABLOCK_ERR_INVALID_ARG, "%s: reserved must be 0", who);
+    sablock_status st = SABLOCK_OK;
+    const int32_t n[4] = {s->n_layers, s->n_pages, s->n_kv_heads, s->page_size};
+    if (!axes_ok(s->k_stride, n, s->head_dim, who, "K pool", &st) || !axes_ok(s->v_stride, n, s->head_dim, who, "V pool", &st)) return st;
+    d->cus = s->compute_units;
+    if (d->cus == 0) {
+        st = current_device_cus(&d->cus);
+        if (st != SABLOCK_OK) return st;
+    }
+    d->n_seq = s->n_seq; d->n_layers = s->n_layers; d->Hq = s->n_q_heads; d->Hkv = s->n_kv_heads; d->G = s->n_q_heads / s->n_kv_heads;
+    d->D = s->head_dim; d->dtype = s->dtype; d->page = s->page_size; d->shift = 0;
+    while ((1 << d->shift) < d->page) ++d->shift;
+    d->n_pages = s->n_pages; d->max_pages = s->max_pages; d->P = (int32_t)P;
+    d->inv_heads = inverse_of((uint32_t)d->Hkv);
+    d->inv_seq = inverse_of((uint32_t)(d->n_layers * d->Hkv));
+    for (int a = 0; a < 4; ++a) {
+        d->ks[a] = n[a] > 1 ? s->k_stride[a] : 0;
+        d->vs[a] = n[a] > 1 ? s->v_stride[a] : 0;
+    }
+    return SABLOCK_OK;
+}
+
+static sablock_status make_page_view(const char *who, const int32_t *table, const int32_t *lengths, const void *k, const void *v, const void *bounds,
+                                     PageView *pv)
+{
+    if (!table || !k || !v) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (!aligned16(k) || !aligned16(v) || !aligned16(bounds))
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: the pools and the bounds must be 16-byte aligned", who);
+    pv->table = table;
+    pv->lengths = lengths;
+    pv->k = static_cast<char *>(const_cast<void *>(k));
+    pv->v = static_cast<char *>(const_cast<void *>(v));
+    pv->bounds = static_cast<char *>(const_cast<void *>(bounds));
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_compact_paged(const sablock_shape *shape, const void *k, const void *v, const int32_t *idx, int32_t budget,
+                                     int32_t append_window, const sablock_pages *pages, const int32_t *page_table, void *k_pool, void *v_pool,
+                                     void *bounds, int32_t *lengths_out, void *stream)
+{
+    const char *who = "sablock_compact_paged";
+    Dims d;
+    sablock_status st = make_dims(shape, &d);
+    if (st != SABLOCK_OK) return st;
+    PageDims pd;
+    st = make_pages(who, pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    if (pd.n_seq != d.n_seq || pd.n_layers != d.n_layers || pd.Hkv != d.Hkv || pd.D != d.D || pd.dtype != d.dtype)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: shape and pages differ in n_seq, n_layers, n_kv_heads, head_dim or dtype", who);
+    if (budget < 0) return fail(SABLOCK_ERR_INVALID_ARG, "%s: budget < 0", who);
+    if (!k || !v || (!idx && budget > 0)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (!aligned16(k) || !aligned16(v)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: K and V must be 16-byte aligned", who);
+    if (shape->v_stride[3] < d.D) return fail(SABLOCK_ERR_INVALID_ARG, "%s: V token stride smaller than head_dim", who);
+    PageView pv;
+    st = make_page_view(who, page_table, nullptr, k_pool, v_pool, bounds, &pv);
+    if (st != SABLOCK_OK) return st;
+    const int64_t rows = (int64_t)std::min(budget, d.T) + (append_window ? d.W : 0);
+    if (rows > (int64_t)pd.max_pages * pd.page)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: %lld rows do not fit max_pages %d of %d rows", who, (long long)rows, pd.max_pages, pd.page);
+    return dev(launch_compact_paged(d, k, v, idx, budget, (int32_t)rows, pd, pv, lengths_out, static_cast<hipStream_t>(stream)), who);
+}
+
+sablock_status sablock_append_paged(const sablock_pages *pages, const sablock_new_tokens *tokens, const void *q, const void *k, const void *v,
+                                    const int32_t *counts, const int32_t *positions, const float *inv_freq, const int32_t *page_table,
+                                    const int32_t *lengths, void *q_out, void *k_pool, void *v_pool, void *bounds, void *stream)
+{
+    const char *who = "sablock_append_paged";
+    PageDims pd;
+    sablock_status st = make_pages(who, pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    if (!tokens || !k || !v || !lengths) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if ((q == nullptr) != (q_out == nullptr)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: q and q_out must both be given or both be NULL", who);
+    if (q && q == q_out) return fail(SABLOCK_ERR_INVALID_ARG, "%s: q_out may not overlap q", who);
+    if (tokens->n_new < 1) return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_new must be >= 1", who);
+    if (tokens->reserved) return fail(SABLOCK_ERR_INVALID_ARG, "%s: reserved must be 0", who);
+    if (tokens->interleaved != 0 && tokens->interleaved != 1) return fail(SABLOCK_ERR_INVALID_ARG, "%s: interleaved must be 0 or 1", who);
+    if (tokens->rotary_dim < 0 || tokens->rotary_dim > pd.D)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: need 0 <= rotary_dim <= head_dim (rotary_dim %d, head_dim %d)", who, tokens->rotary_dim, pd.D);
+    if (tokens->rotary_dim % 16) return fail(SABLOCK_ERR_UNSUPPORTED, "%s: rotary_dim %d: need a multiple of 16", who, tokens->rotary_dim);
+    if (tokens->rotary_dim > 0 && (!positions || !inv_freq)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: a rotation needs positions and inv_freq", who);
+    if (tokens->n_new > (int64_t)pd.max_pages * pd.page)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_new %d does not fit max_pages %d of %d rows", who, tokens->n_new, pd.max_pages, pd.page);
+    const int32_t nk[4] = {pd.n_seq, pd.n_layers, pd.Hkv, tokens->n_new}, nq[4] = {pd.n_seq, pd.n_layers, pd.Hq, tokens->n_new};
+    if (!axes_ok(tokens->k_stride, nk, 0, who, "k", &st) || !axes_ok(tokens->v_stride, nk, 0, who, "v", &st)) return st;
+    if (q && !axes_ok(tokens->q_stride, nq, 0, who, "q", &st)) return st;
+    if (tokens->n_new > 1 && (tokens->k_stride[3] < pd.D || tokens->v_stride[3] < pd.D || (q && tokens->q_stride[3] < pd.D)))
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: token stride smaller than head_dim", who);
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out))
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: q, k, v and q_out must be 16-byte aligned", who);
+    PageView pv;
+    st = make_page_view(who, page_table, lengths, k_pool, v_pool, bounds, &pv);
+    if (st != SABLOCK_OK) return st;
+    TokenDims td;
+    td.n_new = tokens->n_new; td.R = tokens->rotary_dim; td.interleaved = tokens->interleaved;
+    for (int a = 0; a < 4; ++a) {
+        td.qs[a] = nq[a] > 1 ? tokens->q_stride[a] : 0;
+        td.ks[a] = nk[a] > 1 ? tokens->k_stride[a] : 0;
+        td.vs[a] = nk[a] > 1 ? tokens->v_stride[a] : 0;
+    }
+    return dev(launch_append_paged(pd, td, q, k, v, counts, positions, inv_freq, pv, q_out, static_cast<hipStream_t>(stream)), who);
+}
+
+static sablock_status make_decode_pages(const char *who, const sablock_pages *pages, PageDims *pd)
+{
+    sablock_status st = make_pages(who, pages, pd);
+    if (st != SABLOCK_OK) return st;
+    if (!decode_paged_supported(*pd))
+        return fail(SABLOCK_ERR_UNSUPPORTED, "%s: need G <= 16 and head_dim a multiple of 32 (bf16) or 16 (fp32)", who);
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_decode_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out)
+{
+    if (!bytes_out) return fail(SABLOCK_ERR_INVALID_ARG, "bytes_out is NULL");
+    PageDims pd;
+    sablock_status st = make_decode_pages("sablock_decode_paged_workspace_bytes", pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    *bytes_out = decode_paged_ws_bytes(pd);
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_decode_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table,
+                                    const int32_t *lengths, const int32_t *page_list, int32_t n_listed, float *out, void *ws, size_t ws_bytes,
+                                    void *stream)
+{
+    const char *who = "sablock_decode_paged";
+    PageDims pd;
+    sablock_status st = make_decode_pages(who, pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    if (!q || !lengths || !out) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (!aligned16(q) || !aligned16(ws)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: q and the workspace must be 16-byte aligned", who);
+    if (page_list && n_listed < 1) return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_listed must be >= 1", who);
+    PageView pv;
+    st = make_page_view(who, page_table, lengths, k_pool, v_pool, nullptr, &pv);
+    if (st != SABLOCK_OK) return st;
+    const size_t need = decode_paged_ws_bytes(pd);
+    if (!ws || ws_bytes < need) return fail(SABLOCK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+    return dev(launch_decode_paged(pd, q, pv, page_list, page_list ? n_listed : 0, out, ws, static_cast<hipStream_t>(stream)), who);
+}
+
+sablock_status sablock_select_pages_workspace_bytes(const sablock_pages *pages, size_t *bytes_out)
+{
+    if (!bytes_out) return fail(SABLOCK_ERR_INVALID_ARG, "bytes_out is NULL");
+    PageDims pd;
+    sablock_status st = make_pages("sablock_select_pages_workspace_bytes", pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    *bytes_out = select_pages_ws_bytes(pd);
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_select_pages(const sablock_pages *pages, const void *q, const void *bounds, const int32_t *page_table, const int32_t *lengths,
+                                    int32_t n_pick, int32_t n_first, int32_t n_last, int32_t *list_out, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "sablock_select_pages";
+    PageDims pd;
+    sablock_status st = make_pages(who, pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    if (!q || !bounds || !page_table || !lengths || !list_out) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (!aligned16(q) || !aligned16(bounds) || !aligned16(ws))
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: q, the bounds and the workspace must be 16-byte aligned", who);
+    if (pd.G > 16) return fail(SABLOCK_ERR_UNSUPPORTED, "%s: need G <= 16", who);
+    if (n_pick < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > n_pick)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: need n_pick >= 1 and n_first + n_last <= n_pick, none negative", who);
+    const size_t need = select_pages_ws_bytes(pd);
+    if (!ws || ws_bytes < need) return fail(SABLOCK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+    PageView pv;
+    st = make_page_view(who, page_table, lengths, bounds, bounds, bounds, &pv);
+    if (st != SABLOCK_OK) return st;
+    return dev(launch_select_pages(pd, q, pv, n_pick, n_first, n_last, list_out, ws, static_cast<hipStream_t>(stream)), who);
+}
+
 }  // extern "C"

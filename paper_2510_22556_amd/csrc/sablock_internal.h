@@ -261,4 +261,48 @@ size_t decode_ws_bytes(const Dims &d);
 hipError_t launch_decode(const Dims &d, const void *q, const void *k, const void *v, const int32_t *n_sel,
                          int32_t budget, float *out, void *ws, hipStream_t st);
 
+// ---- the paged cache ----
+constexpr int MAX_PAGED_SEQ = 4096;
+struct PageDims {                                             // host-validated view of a sablock_pages
+    int32_t n_seq, n_layers, Hq, Hkv, G, D, dtype;
+    int32_t page, shift;                                      // rows per page, its binary logarithm
+    int32_t n_pages, max_pages, P, cus;
+    uint32_t inv_heads, inv_seq;                              // as in Dims
+    int64_t ks[4], vs[4];
+};
+struct PageView {                                             // the cache's device data
+    const int32_t *table, *lengths;
+    char *k, *v, *bounds;                                     // bounds: nullable
+};
+struct TokenDims { int32_t n_new, R, interleaved; int64_t qs[4], ks[4], vs[4]; };
+
+__host__ __device__ inline int32_t seq_of_problem(const PageDims &d, int32_t p) { return quotient(p, d.inv_seq); }
+__host__ __device__ inline int32_t head_of_problem(const PageDims &d, int32_t p) { return p - quotient(p, d.inv_heads) * d.Hkv; }
+__host__ __device__ inline int32_t layer_of_problem(const PageDims &d, int32_t p) { return quotient(p, d.inv_heads) - seq_of_problem(d, p) * d.n_layers; }
+__host__ __device__ inline int32_t elt_bytes(const PageDims &d) { return d.dtype == SABLOCK_F32 ? 4 : 2; }
+// rows of a sequence, whatever its length says
+__host__ __device__ inline int32_t rows_of(const PageDims &d, const int32_t *lengths, int32_t s)
+{
+    const int32_t n = lengths[s], most = d.max_pages << d.shift;
+    return n < 0 ? 0 : n < most ? n : most;
+}
+// page that holds place i of the sequence's row of the table, -1 for none
+__host__ __device__ inline int32_t page_at(const PageDims &d, const int32_t *table, int32_t s, int32_t i)
+{
+    const int32_t id = table[(int64_t)s * d.max_pages + i];
+    return (uint32_t)id < (uint32_t)d.n_pages ? id : -1;
+}
+
+hipError_t launch_compact_paged(const Dims &d, const void *k, const void *v, const int32_t *idx, int32_t budget, int32_t rows,
+                                const PageDims &pd, const PageView &pv, int32_t *lengths_out, hipStream_t st);
+hipError_t launch_append_paged(const PageDims &pd, const TokenDims &td, const void *q, const void *k, const void *v, const int32_t *counts,
+                               const int32_t *positions, const float *inv_freq, const PageView &pv, void *q_out, hipStream_t st);
+bool decode_paged_supported(const PageDims &pd);
+size_t decode_paged_ws_bytes(const PageDims &pd);
+hipError_t launch_decode_paged(const PageDims &pd, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out,
+                               void *ws, hipStream_t st);
+size_t select_pages_ws_bytes(const PageDims &pd);
+hipError_t launch_select_pages(const PageDims &pd, const void *q, const PageView &pv, int32_t n_pick, int32_t n_first, int32_t n_last,
+                               int32_t *list, void *ws, hipStream_t st);
+
 }  // namespace sablock
