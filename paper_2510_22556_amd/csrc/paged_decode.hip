@@ -1,80 +1,499 @@
 // Decode-time attention of one new token per sequence over a paged cache (Sec. 2.1 Eq. 1 for a single query position), over all
 // of a sequence's pages or over listed ones.
+//
+//   decode_paged_kernel   Work is counted in steps of 32 rows (bf16) or 16 (fp32), all problems' one behind the other; every workgroup
+//       takes an equal run of them, whatever the sequences' lengths, which only the device knows.  A run covers pieces of one or
+//       several problems; a problem that lies in one run is finished there, of a problem's piece (reference, denominator,
+//       numerators) go to the workspace, at most two per workgroup.
+//   decode_paged_merge_kernel   joins the pieces of each problem, and gives zeros to those without rows.
+//
+// A wavefront does a step alone, on matrix instructions of 16 x 16 whose 16 columns are the query heads of the KV head (G <= 16,
+// the rest zeros): S^T = K Q^T, then out^T += V^T P^T.  Both products take K and V as they lie in memory, without LDS:
+//   - K as A operand has a row per lane (lane & 15) and consecutive elements in it: 16-byte loads, four lanes per row.  The order in
+//     which the inner dimension is summed is free, so it is that of the loads.
+//   - The result has a head per lane and four rows in it, which is how P^T as B operand wants its inner dimension, the rows; bf16
+//     takes eight rows there: the A rows of two products are dealt out so that a lane's results are rows 8 (lane >> 4) + 0 .. 7.
+//   - V^T as A operand wants an element of V per lane and those rows in it.  A lane loads D / 16 consecutive elements of each of its
+//     rows, 16 lanes a whole row; element e of the lanes is the e-th product's operand, fp32 as it is, bf16 after one
+//     v_perm_b32 for two rows.  Product e then gives the elements D / 16 (lane & 15) + e.
+// Everything about a head, logits, reference, denominator and numerators, is in the lanes of its column: no exchange but a
+// maximum over four lanes where a reference moves.  References are set AHEAD (log2 domain) above the largest logit so far and move when
+// a logit passes them.  bf16 probabilities enter the second product in three parts of 8 bits, exactly: the result is as
+// good as in fp32 (rounded to bf16 they would be off by 2^-9), and the matrix pipe has the time.
 #include "sablock_internal.h"
+
+#include <cfloat>
 
 namespace sablock {
 namespace {
 
-constexpr int NT = 256;
+constexpr int NW = 4, NT = NW * 64;
+constexpr float AHEAD = 8.f;
+constexpr int LEAST_STEPS = 4;                 // of a workgroup's run: one per wavefront
 
-template <bool BF16> __device__ float element(const char *p, int64_t i)
-{
-    if constexpr (BF16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << 16);
-    else return reinterpret_cast<const float *>(p)[i];
-}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+template <int N> struct Words;                 // N dwords of a row that begin on any dword
+template <> struct Words<1> { typedef uint32_t T __attribute__((aligned(4))); };
+template <> struct Words<2> { typedef uint32_t T __attribute__((ext_vector_type(2), aligned(4))); };
+template <> struct Words<3> { typedef uint32_t T __attribute__((ext_vector_type(3), aligned(4))); };
+template <> struct Words<4> { typedef uint32_t T __attribute__((ext_vector_type(4), aligned(4))); };
 
-// grid (query heads of a KV head, problems): 256 rows at a time, one per thread for the logits, one column per thread for the
-// weighted sum
-template <bool BF16>
-__global__ void __launch_bounds__(NT)
-decode_paged_kernel(PageDims d, PageView pv, const char *q, const int32_t *list, int n_listed, float qscale, float *out)
+// N dwords from p into w; what is read once is non-temporal
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t *w, const char *p)
 {
-    __shared__ float qs[256], w[NT], red[NT / 64];
-    __shared__ int64_t place[NT];
-    const int p = blockIdx.y, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p), tid = threadIdx.x;
-    const int64_t qrow = (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G + blockIdx.x) * d.D;
-    if (tid < d.D) qs[tid] = element<BF16>(q, qrow + tid) * qscale;
-    const int len = rows_of(d, pv.lengths, s), pages = (len + d.page - 1) >> d.shift;
-    const int total = list ? min(n_listed, pages) << d.shift : len;
-    float m = -INFINITY, z = 0.f, acc = 0.f;
-    for (int r0 = 0; r0 < total; r0 += NT) {
-        const int r = r0 + tid;
-        int at = -1;                                           // page of the sequence
-        if (r < total) at = list ? list[(int64_t)p * n_listed + (r >> d.shift)] : r >> d.shift;
-        int id = -1;
-        if (at >= 0 && at < pages && (at << d.shift) + (r & (d.page - 1)) < len) id = page_at(d, pv.table, s, at);
-        __syncthreads();
-        place[tid] = id < 0 ? -1 : layer * d.vs[0] + id * d.vs[1] + head * d.vs[2] + (r & (d.page - 1)) * d.vs[3];
-        float x = -INFINITY;
-        if (id >= 0) {
-            const int64_t k = layer * d.ks[0] + id * d.ks[1] + head * d.ks[2] + (r & (d.page - 1)) * d.ks[3];
-            x = 0.f;
-            for (int c = 0; c < d.D; ++c) x = fmaf(qs[c], element<BF16>(pv.k, k + c), x);
-        }
-        float mx = x;
-        for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-        if ((tid & 63) == 0) red[tid >> 6] = mx;
-        __syncthreads();
-        for (int i = 0; i < NT / 64; ++i) mx = fmaxf(mx, red[i]);
-        mx = fmaxf(mx, m);
-        const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
-        w[tid] = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - mx);
-        m = mx;
-        __syncthreads();
-        z *= f;
-        acc *= f;
-        const int n = min(NT, total - r0);
-        for (int i = 0; i < n; ++i) {
-            if (place[i] < 0) continue;
-            z += w[i];
-            if (tid < d.D) acc = fmaf(w[i], element<BF16>(pv.v, place[i] + tid), acc);
-        }
+    if constexpr (N > 4) {
+        load_words<4>(w, p);
+        load_words<N - 4>(w + 4, p + 16);
+    } else if constexpr (N == 1) {
+        w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
+    } else {
+        const auto v = __builtin_nontemporal_load(reinterpret_cast<const typename Words<N>::T *>(p));
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = v[i];
     }
-    if (tid < d.D) out[qrow + tid] = z == 0.f ? 0.f : acc / z;
 }
+
+struct DecodePagedArgs {
+    PageDims d;
+    PageView pv;
+    const char *q;
+    const int32_t *list;
+    int n_listed;
+    float qscale;                // log2(e) / sqrt(D)
+    float *out;                  // [n_seq][n_layers][Hq][D]
+    float *weights;              // pieces [2 * workgroups][G][2]: reference (log2 domain), denominator
+    float *sums;                 // pieces [2 * workgroups][G][D]
+};
+
+// steps of a problem of sequence s
+template <int STEP>
+__device__ __forceinline__ int steps_of(const DecodePagedArgs &a, int s)
+{
+    const int len = rows_of(a.d, a.pv.lengths, s);
+    int rows = len;
+    if (a.list) {
+        const int pages = (len + a.d.page - 1) >> a.d.shift;
+        rows = min(a.n_listed, pages) << a.d.shift;
+    }
+    return (rows + STEP - 1) / STEP;
+}
+
+// Inclusive sum over the lanes.
+__device__ __forceinline__ int64_t scan(int64_t x, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(x, o);
+        if (lane >= o) x += u;
+    }
+    return x;
+}
+
+// Where the problems' steps lie in the row of all of them; a wavefront's view, each lane with the sums up to its share of the sequences.
+template <int STEP>
+struct Places {
+    const DecodePagedArgs &a;
+    int lane, share, heads;                    // sequences per lane, problems per sequence
+    int64_t upto, total;                       // steps of one problem of each sequence up to the lane's last, of all problems
+    __device__ Places(const DecodePagedArgs &args, int l) : a(args), lane(l)
+    {
+        heads = a.d.n_layers * a.d.Hkv;
+        share = (a.d.n_seq + 63) / 64;
+        int64_t sum = 0;
+        for (int i = 0; i < share; ++i)
+            if (lane * share + i < a.d.n_seq) sum += steps_of<STEP>(a, lane * share + i);
+        upto = a.d.n_seq > 1 ? scan(sum, lane) : sum;
+        total = (a.d.n_seq > 1 ? __shfl(upto, 63) : __shfl(upto, 0)) * heads;
+    }
+    // the sequence that step x of all lies in (x < total), the steps of one problem of those before it, and of its own
+    __device__ void find(int64_t x, int &seq, int64_t &before, int &steps) const
+    {
+        if (a.d.n_seq == 1) { seq = 0; before = 0; steps = __shfl((int)upto, 0); return; }
+        int first = __ffsll((unsigned long long)__ballot(upto * heads > x)) - 1;
+        int64_t at = first > 0 ? __shfl(upto, first - 1) : 0;
+        if (share == 1) {
+            seq = first;
+            before = at;
+            steps = (int)(__shfl(upto, first) - at);
+            return;
+        }
+        const int s = first * share + lane;
+        const int own = lane < share && s < a.d.n_seq ? steps_of<STEP>(a, s) : 0;
+        const int64_t inner = scan((int64_t)own, lane) + at;
+        const int j = __ffsll((unsigned long long)__ballot(inner * heads > x)) - 1;
+        seq = first * share + j;
+        steps = __shfl(own, j);
+        before = __shfl(inner, j) - steps;
+    }
+    // the same for a given sequence
+    __device__ void of(int seq, int64_t &before, int &steps) const
+    {
+        const int first = seq / share;
+        before = first > 0 ? __shfl(upto, first - 1) : 0;
+        for (int s = first * share; s < seq; ++s) before += steps_of<STEP>(a, s);
+        steps = steps_of<STEP>(a, seq);
+    }
+};
+__device__ __forceinline__ int64_t run_of(int64_t total, int workgroups)
+{
+    if (total < 1 << 30) return max(LEAST_STEPS, ((int)total + workgroups - 1) / workgroups);
+    return (total + workgroups - 1) / workgroups;
+}
+
+__device__ __forceinline__ float over_quarters(float x, bool take_max)        // lanes l, l ^ 16, l ^ 32, l ^ 48
+{
+    float y = __shfl_xor(x, 16);
+    x = take_max ? fmaxf(x, y) : x + y;
+    y = __shfl_xor(x, 32);
+    return take_max ? fmaxf(x, y) : x + y;
+}
+
+// EP: elements of a row per lane in the second product, D / 16
+template <bool BF16, int EP>
+__global__ void __launch_bounds__(NT)
+decode_paged_kernel(DecodePagedArgs a)
+{
+    constexpr int D = EP * 16, ELT = BF16 ? 2 : 4, STEP = BF16 ? 32 : 16, R = STEP / 4;      // R: rows per lane in the second product
+    constexpr int KT = BF16 ? 2 : 1;                           // products of 16 rows per step
+    constexpr int KC = D * ELT / 64;                           // 16-byte pieces of a row per lane in the first product
+    constexpr int VW = EP * ELT / 4;                           // dwords of a row per lane in the second
+    constexpr int KEEP = D / 4 + 2;                            // registers of a lane that wavefronts join
+    __shared__ float sh[(NW - 1) * KEEP * 64];
+    const PageDims &d = a.d;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = lane & 15, c = lane >> 4;
+    const Places<STEP> places(a, lane);
+    const int64_t run = run_of(places.total, gridDim.x), run_from = blockIdx.x * run, run_to = min(run_from + run, places.total);
+    // a lane's rows of a step: of K as operand (bf16: and that row + 4), of the results and of V from `row` on
+    const int krow = BF16 ? (m >> 2) * 8 + (m & 3) : m, row = R * c;
+    const int64_t kstep = d.ks[3] * ELT, vstep = d.vs[3] * ELT;
+
+    for (int64_t x = run_from; x < run_to;) {
+        int s, n;
+        int64_t before;
+        places.find(x, s, before, n);
+        s = __builtin_amdgcn_readfirstlane(s);
+        n = __builtin_amdgcn_readfirstlane(n);
+        const int64_t in_seq = x - before * places.heads;
+        const int problem = __builtin_amdgcn_readfirstlane(in_seq < 1 << 30 ? (int)in_seq / n : (int)(in_seq / n));
+        const int off = __builtin_amdgcn_readfirstlane((int)(in_seq - (int64_t)problem * n));
+        const int piece = (int)min((int64_t)(n - off), run_to - x);
+        const int layer = problem / d.Hkv, head = problem - layer * d.Hkv, p = s * places.heads + problem;
+        const int len = rows_of(d, a.pv.lengths, s), pages = (len + d.page - 1) >> d.shift;
+        const int entries = a.list ? min(a.n_listed, pages) : pages;
+        const int64_t qrow = (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G) * D;
+
+        u32x4 q[KC];
+#pragma unroll
+        for (int j = 0; j < KC; ++j)
+            q[j] = m < d.G ? *reinterpret_cast<const u32x4 *>(a.q + (qrow + m * D) * ELT + j * 64 + c * 16) : u32x4{0, 0, 0, 0};
+        float ref = -FLT_MAX, den = 0.f;
+        f32x4 acc[EP];
+#pragma unroll
+        for (int e = 0; e < EP; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        const int from = off + (int)((int64_t)piece * wave / NW), to = off + (int)((int64_t)piece * (wave + 1) / NW);
+        // the page and the rows of it that count, of 64 entries at a time, one per lane
+        int ids = 0, held = 0, base = -1 << 30;
+        const char *kat = nullptr, *vat = nullptr;
+        int limit = 0;                                         // of this lane's rows of the step, so many count (from the first on)
+        bool whole = false;                                    // all rows of the step count
+        auto locate = [&](int st) {
+            const int r0 = st * STEP, e0 = r0 >> d.shift;
+            if (e0 - base >= 64) {
+                base = e0;
+                const int e = e0 + lane;
+                int at = e;
+                if (a.list && e < entries) at = a.list[(int64_t)p * a.n_listed + e];
+                ids = held = 0;
+                if (e < entries && (uint32_t)at < (uint32_t)pages) {
+                    const int id = page_at(d, a.pv.table, s, at);
+                    if (id >= 0) {
+                        ids = id;
+                        held = min(d.page, len - (at << d.shift));
+                    }
+                }
+            }
+            const int at = e0 - base, in_page = r0 & (d.page - 1);
+            int idk = __builtin_amdgcn_readlane(ids, at), idv = idk, n_held = __builtin_amdgcn_readlane(held, at);
+            int rk = in_page + krow, rv = in_page + row;
+            whole = in_page + STEP <= n_held;
+            if (BF16 && d.shift == 4) {                        // two pages; a lane's rows lie in one of them
+                const int id1 = __builtin_amdgcn_readlane(ids, at + 1), held1 = __builtin_amdgcn_readlane(held, at + 1);
+                whole = n_held == 16 && held1 == 16;
+                idk = krow < 16 ? idk : id1;
+                idv = row < 16 ? idv : id1;
+                n_held = row < 16 ? n_held : held1;
+                rk &= 15;
+                rv &= 15;
+            }
+            limit = n_held - rv;
+            kat = a.pv.k + (layer * d.ks[0] + idk * d.ks[1] + head * d.ks[2]) * ELT + rk * kstep + c * 16;
+            vat = a.pv.v + (layer * d.vs[0] + idv * d.vs[1] + head * d.vs[2]) * ELT + rv * vstep + m * EP * ELT;
+        };
+        u32x4 k[KT][KC];
+        uint32_t v[R][VW];
+        auto load_k = [&]() {
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int j = 0; j < KC; ++j)
+                    k[t][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kat + t * 4 * kstep + j * 64));
+        };
+        auto load_v = [&]() {
+#pragma unroll
+            for (int i = 0; i < R; ++i) load_words<VW>(v[i], vat + i * vstep);
+        };
+        if (from < to) {
+            locate(from);
+            load_k();
+            load_v();
+        }
+        for (int st = from; st < to; ++st) {
+            float z[R];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                f32x4 r{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < KC; ++j) {
+                    if constexpr (BF16) {
+                        r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][j]), __builtin_bit_cast(bf16x8, q[j]), r, 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            r = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][j][e]), __uint_as_float(q[j][e]), r, 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[4 * t + i] = r[i];
+            }
+            const bool now_whole = whole;
+            const int now_limit = limit;
+            const bool more = st + 1 < to;
+            if (more) {
+                locate(st + 1);
+                load_k();
+            }
+            if (!now_whole) {
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+                    if (i >= now_limit) {
+                        z[i] = -INFINITY;
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) v[i][w] = 0;             // zero times what lies there may be no number
+                    }
+            }
+            float most = z[0];
+#pragma unroll
+            for (int i = 1; i < R; ++i) most = fmaxf(most, z[i]);
+            most *= a.qscale;
+            if (__ballot(most > ref) != 0ull) {
+                const float top = over_quarters(most, true), to_ref = top > ref ? top + AHEAD : ref;
+                const float f = __builtin_amdgcn_exp2f(ref - to_ref);
+                ref = to_ref;
+                den *= f;
+#pragma unroll
+                for (int e = 0; e < EP; ++e) acc[e] *= f;
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                z[i] = __builtin_amdgcn_exp2f(fmaf(z[i], a.qscale, -ref));
+                den += z[i];
+            }
+            if constexpr (BF16) {
+                u32x4 part[3];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t lo = __float_as_uint(z[2 * i]), hi = __float_as_uint(z[2 * i + 1]);
+#pragma unroll
+                    for (int t = 0; t < 3; ++t) {
+                        part[t][i] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
+                        lo = __float_as_uint(__uint_as_float(lo) - __uint_as_float(lo & 0xffff0000u));
+                        hi = __float_as_uint(__uint_as_float(hi) - __uint_as_float(hi & 0xffff0000u));
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < EP; ++e) {
+                    u32x4 o;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        o[i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], e % 2 ? 0x07060302 : 0x05040100);
+#pragma unroll
+                    for (int t = 2; t >= 0; --t)
+                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part[t]), acc[e], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int e = 0; e < EP; ++e)
+                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e]), z[i], acc[e], 0, 0, 0);
+            }
+            if (more) load_v();
+        }
+        den = over_quarters(den, false);
+
+        // the wavefronts' shares, lane by lane; the first one joins them
+        __syncthreads();                                       // of the piece before
+        if (wave > 0) {
+            float *o = sh + (wave - 1) * KEEP * 64 + lane;
+            o[0] = ref;
+            o[64] = den;
+#pragma unroll
+            for (int e = 0; e < EP; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[(2 + 4 * e + i) * 64] = acc[e][i];
+        }
+        __syncthreads();
+        if (wave == 0) {
+            float w[NW], top = ref;
+#pragma unroll
+            for (int u = 1; u < NW; ++u) { w[u] = sh[(u - 1) * KEEP * 64 + lane]; top = fmaxf(top, w[u]); }
+            w[0] = __builtin_amdgcn_exp2f(ref - top);
+            den *= w[0];
+#pragma unroll
+            for (int u = 1; u < NW; ++u) {
+                w[u] = __builtin_amdgcn_exp2f(w[u] - top);
+                den += sh[((u - 1) * KEEP + 1) * 64 + lane] * w[u];
+            }
+#pragma unroll
+            for (int e = 0; e < EP; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float t = acc[e][i] * w[0];
+#pragma unroll
+                    for (int u = 1; u < NW; ++u) t = fmaf(sh[((u - 1) * KEEP + 2 + 4 * e + i) * 64 + lane], w[u], t);
+                    acc[e][i] = t;
+                }
+            if (m < d.G) {                                     // elements EP (4 c + i) + e of head m
+                float *o;
+                float f = 1.f;
+                if (piece == n) {                              // the whole problem
+                    o = a.out + qrow + m * D;
+                    f = den == 0.f ? 0.f : 1.f / den;
+                } else {
+                    const int64_t slot = 2 * (int64_t)blockIdx.x + (off == 0);
+                    o = a.sums + (slot * d.G + m) * D;
+                    if (c == 0) {
+                        a.weights[(slot * d.G + m) * 2] = top;
+                        a.weights[(slot * d.G + m) * 2 + 1] = den;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < EP; ++e) o[EP * (4 * c + i) + e] = acc[e][i] * f;
+            }
+        }
+        x += piece;
+    }
+}
+
+// grid (G, problems): the pieces' weights first, then their weighted sum, four elements per thread, the pieces dealt out to groups of threads
+constexpr int MERGE_T = 256, MAX_PIECES = 1024;
+template <int STEP>
+__global__ void __launch_bounds__(MERGE_T)
+decode_paged_merge_kernel(DecodePagedArgs a, int workgroups)
+{
+    __shared__ float w_sh[MAX_PIECES], red[2 * (MERGE_T / 64)];
+    __shared__ f32x4 sum[MERGE_T];
+    const PageDims &d = a.d;
+    const int g = blockIdx.x, p = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const Places<STEP> places(a, lane);
+    const int seq = seq_of_problem(d, p);
+    int n;
+    int64_t before;
+    places.of(seq, before, n);
+    float *out = a.out + ((((int64_t)seq * d.n_layers + layer_of_problem(d, p)) * d.Hq) + head_of_problem(d, p) * d.G + g) * d.D;
+    if (n == 0) {
+        for (int i = tid; i < d.D; i += MERGE_T) out[i] = 0.f;
+        return;
+    }
+    const int64_t run = run_of(places.total, workgroups), at = before * places.heads + (int64_t)(p - seq * places.heads) * n;
+    const int64_t first = at / run, pieces64 = (at + n - 1) / run - first + 1;
+    if (pieces64 == 1) return;                                 // finished where it was computed
+    const int pieces = (int)pieces64;
+    auto slot = [&](int i) { return (2 * (first + i) + (i == 0)) * d.G + g; };
+    float m = -FLT_MAX;
+    for (int i = tid; i < pieces; i += MERGE_T) m = fmaxf(m, a.weights[slot(i) * 2]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) red[tid >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MERGE_T / 64; ++i) m = fmaxf(m, red[i]);
+    float den = 0.f;
+    for (int i = tid; i < pieces; i += MERGE_T) {
+        const float f = __builtin_amdgcn_exp2f(a.weights[slot(i) * 2] - m);
+        w_sh[i] = f;
+        den += a.weights[slot(i) * 2 + 1] * f;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
+    if (lane == 0) red[MERGE_T / 64 + (tid >> 6)] = den;
+    __syncthreads();
+    den = 0.f;
+#pragma unroll
+    for (int i = 0; i < MERGE_T / 64; ++i) den += red[MERGE_T / 64 + i];
+    const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
+    f32x4 t{0.f, 0.f, 0.f, 0.f};
+    if (group < groups) {
+#pragma unroll 4
+        for (int i = group; i < pieces; i += groups) t += *reinterpret_cast<const f32x4 *>(a.sums + slot(i) * d.D + 4 * c) * w_sh[i];
+    }
+    sum[tid] = t;
+    __syncthreads();
+    if (group > 0) return;
+    for (int i = 1; i < groups; ++i) t += sum[i * per + c];
+    *reinterpret_cast<f32x4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
+}
+
+// workgroups per compute unit that the registers leave room for
+int resident(const PageDims &d)
+{
+    return d.D <= 64 ? 3 : d.D <= 128 ? 2 : 1;
+}
+int workgroups_of(const PageDims &d) { return std::min(d.cus * resident(d), MAX_PIECES - 1); }
 
 }  // namespace
 
 bool decode_paged_supported(const PageDims &d) { return d.G <= 16 && d.D % (d.dtype == SABLOCK_F32 ? 16 : 32) == 0; }
 
-size_t decode_paged_ws_bytes(const PageDims &) { return 256; }
+size_t decode_paged_ws_bytes(const PageDims &d)
+{
+    const size_t rows = 2 * (size_t)workgroups_of(d) * d.G;
+    return align256(rows * 8) + align256(rows * d.D * 4);
+}
 
 hipError_t launch_decode_paged(const PageDims &d, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out,
-                               void *, hipStream_t st)
+                               void *ws, hipStream_t st)
 {
-    const float qscale = (float)(1.4426950408889634 / sqrt((double)d.D));
-    hipLaunchKernelGGL(d.dtype == SABLOCK_BF16 ? decode_paged_kernel<true> : decode_paged_kernel<false>, dim3(d.G, d.P), dim3(NT), 0, st, d, pv,
-                       static_cast<const char *>(q), list, n_listed, qscale, out);
+    DecodePagedArgs a;
+    a.d = d;
+    a.pv = pv;
+    a.q = static_cast<const char *>(q);
+    a.list = list;
+    a.n_listed = n_listed;
+    a.qscale = (float)(1.4426950408889634 / sqrt((double)d.D));
+    a.out = out;
+    const int workgroups = workgroups_of(d);
+    a.weights = static_cast<float *>(ws);
+    a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups * d.G * 8));
+    const bool bf = d.dtype == SABLOCK_BF16;
+    using Kern = void (*)(DecodePagedArgs);
+    Kern fn = nullptr;
+#define SABLOCK_PAGED_F(EV) if (!bf && d.D == EV * 16) fn = decode_paged_kernel<false, EV>;
+#define SABLOCK_PAGED_B(EV) if (bf && d.D == EV * 16) fn = decode_paged_kernel<true, EV>; SABLOCK_PAGED_F(EV)
+    SABLOCK_PAGED_F(1) SABLOCK_PAGED_B(2) SABLOCK_PAGED_F(3) SABLOCK_PAGED_B(4) SABLOCK_PAGED_F(5) SABLOCK_PAGED_B(6) SABLOCK_PAGED_F(7) SABLOCK_PAGED_B(8)
+    SABLOCK_PAGED_F(9) SABLOCK_PAGED_B(10) SABLOCK_PAGED_F(11) SABLOCK_PAGED_B(12) SABLOCK_PAGED_F(13) SABLOCK_PAGED_B(14) SABLOCK_PAGED_F(15) SABLOCK_PAGED_B(16)
+#undef SABLOCK_PAGED_B
+#undef SABLOCK_PAGED_F
+    if (!fn) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(fn, dim3(workgroups), dim3(NT), 0, st, a);
+    hipLaunchKernelGGL(bf ? decode_paged_merge_kernel<32> : decode_paged_merge_kernel<16>, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a, workgroups);
     return hipGetLastError();
 }
 
