@@ -35,25 +35,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // 16 bytes that are read once: non-temporal
 __device__ inline u32x4 load16(const char *p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
 
-// value of lane ^ M
-template <int M>
-__device__ inline float xor_lane(float x)
-{
-    const int v = __float_as_int(x);
-    if constexpr (M == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true));
-    if constexpr (M == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true));
-    if constexpr (M == 4) {                                    // banks 0, 2 from four lanes up, banks 1, 3 from four lanes down
-        const int a = __builtin_amdgcn_update_dpp(v, v, 0x104, 0xF, 0x5, false);
-        return __int_as_float(__builtin_amdgcn_update_dpp(a, v, 0x114, 0xF, 0xA, false));
-    }
-    if constexpr (M == 8) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true));
-    if constexpr (M == 16) {
-        const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
-        return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
-    }
-    const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
-}
 // value of the lane with the same place in the groups of S = 4, whose place inside the four is H
 template <int H>
 __device__ inline float quad_bcast(float x)

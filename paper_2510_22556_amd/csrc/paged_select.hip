@@ -1,129 +1,316 @@
 // The pages that a decode step over a paged cache reads when it may not read all: a score per page from the bounds of its keys,
 // then the best of them per KV head.
+//
+//   page_scores_kernel   max(q lo, q hi) is q+ hi + q- lo with q+ = max(q, 0), q- = min(q, 0): two products per element and head,
+//       formed and summed in fp64.  The products of two bf16 values and their sum over a head are exact there (but for
+//       elements some 2^30 apart), so that which of two pages comes first does not hang on the order of a sum.  A page's row of bounds
+//       is spread over LP lanes, 16 bytes of lo and of hi each, several pages in flight; the sums of up to four heads over the
+//       lanes hand each lane one head, which it rounds to fp32 and turns into a whole number of the same order, and the maximum
+//       over the heads is one of whole numbers, in which what is no number can be the largest.
+//   pick_pages_kernel    a workgroup per problem; the keys stay in registers.  The last key that is taken is found digit by digit, 11 bits
+//       of its distance from the least key at a time (the keys of a problem share their upper bits), and one prefix sum places the pages in order.
 #include "sablock_internal.h"
 
 namespace sablock {
 namespace {
 
 constexpr int NT = 256, PICK_NT = 1024;
-constexpr uint32_t FORCED = 0xffffffffu, NOT_A_NUMBER = 0xfffffffeu;       // above every number's key
+constexpr int FLIGHT = 4;                      // pages in flight per lane
+constexpr uint32_t NOT_A_NUMBER = 0xfffffffeu; // above every number's key
 
-template <bool BF16> __device__ double element(const char *p, int64_t i)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <bool BF16> struct Piece;             // 16 bytes of a row
+template <> struct Piece<true> {
+    static constexpr int N = 8;
+    static __device__ double get(const u32x4 &v, int e) { return (double)__uint_as_float((e & 1) ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16); }
+};
+template <> struct Piece<false> {
+    static constexpr int N = 4;
+    static __device__ double get(const u32x4 &v, int e) { return (double)__uint_as_float(v[e]); }
+};
+
+template <int M> __device__ __forceinline__ uint32_t xor_lane_u(uint32_t x) { return __float_as_uint(xor_lane<M>(__uint_as_float(x))); }
+template <int M> __device__ __forceinline__ double xor_lane_d(double x)
 {
-    if constexpr (BF16) return (double)__uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << 16);
-    else return (double)reinterpret_cast<const float *>(p)[i];
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)xor_lane_u<M>((uint32_t)(u >> 32)) << 32 | xor_lane_u<M>((uint32_t)u));
 }
 
-// grid (parts of a sequence's pages, problems): keys [P][max_pages], in the order of the scores.  max(q lo, q hi) is q+ hi + q- lo; the sum of
-// products of bf16 values in fp64 is exact but for values some 2^30 apart, so its order does not depend on how it is formed.
-template <bool BF16>
-__global__ void __launch_bounds__(NT)
-page_scores_kernel(PageDims d, PageView pv, const char *q, int n_first, int n_last, uint32_t *keys)
+// x[0 .. N) summed over LP lanes: lane l gets the entries l % S + S j, S = min(N, LP), in x[j]
+template <int B, int S, int LP, int N>
+__device__ __forceinline__ void sum_lanes(double (&x)[N])
 {
-    const int p = blockIdx.y, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p);
-    const int i = blockIdx.x * NT + threadIdx.x, n = (rows_of(d, pv.lengths, s) + d.page - 1) >> d.shift;
-    if (i >= n) return;
-    const int id = page_at(d, pv.table, s, i);
-    uint32_t key = ordered_key(-INFINITY);
-    if (i < n_first || i >= n - n_last) key = FORCED;
-    else if (id >= 0) {
-        const int64_t b = (((int64_t)layer * d.n_pages + id) * d.Hkv + head) * 2 * d.D;
-        double most = -INFINITY;
-        bool number = true;
-        for (int g = 0; g < d.G; ++g) {
-            const int64_t qrow = (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G + g) * d.D;
-            double x = 0.0;
-            for (int c = 0; c < d.D; ++c) {
-                const double v = element<BF16>(q, qrow + c);
-                x = fma(fmax(v, 0.0), element<BF16>(pv.bounds, b + d.D + c), fma(fmin(v, 0.0), element<BF16>(pv.bounds, b + c), x));
+    if constexpr (B < LP) {
+        if constexpr (B < S) {
+            const bool up = threadIdx.x & B;
+#pragma unroll
+            for (int i = 0; i < N / (2 * B); ++i) {
+                const double own = up ? x[2 * i + 1] : x[2 * i], other = up ? x[2 * i] : x[2 * i + 1];
+                x[i] = own + xor_lane_d<B>(other);
             }
-            number = number && x == x;
-            most = fmax(most, x);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N / S; ++j) x[j] += xor_lane_d<B>(x[j]);
         }
-        key = number ? ordered_key((float)most) : NOT_A_NUMBER;
+        sum_lanes<2 * B, S, LP, N>(x);
     }
-    keys[(int64_t)p * d.max_pages + i] = key;
+}
+template <int B, int S> __device__ __forceinline__ uint32_t most_of_lanes(uint32_t x)
+{
+    if constexpr (B < S) return most_of_lanes<2 * B, S>(max(x, xor_lane_u<B>(x)));
+    else return x;
 }
 
-// grid P: the n_pick largest keys of a problem, the lower page first where they are equal.  The n_pick-th largest key is found digit by
-// digit (8 bits, counts in LDS); a thread then has a run of consecutive pages, and one prefix sum over the threads places theirs.
-__global__ void __launch_bounds__(PICK_NT)
-pick_pages_kernel(PageDims d, PageView pv, int n_pick, const uint32_t *keys_all, int32_t *list_all)
+struct ScoreArgs {
+    PageDims d;
+    PageView pv;
+    const char *q;
+    int stride;                  // of a problem's keys
+    uint32_t *keys;
+};
+
+// grid (parts of a sequence's pages, problems).  HB heads at a time, in registers; more heads (MANY) are more walks over the pages in
+// flight.
+template <bool BF16, int LP, int HB, bool MANY>
+__global__ void __launch_bounds__(NT, 2)
+page_scores_kernel(ScoreArgs a)
 {
-    __shared__ int hist[256], wave_gt[PICK_NT / 64], wave_eq[PICK_NT / 64];
-    __shared__ uint32_t s_prefix;
-    __shared__ int s_left;
-    const int p = blockIdx.x, tid = threadIdx.x, n = (rows_of(d, pv.lengths, seq_of_problem(d, p)) + d.page - 1) >> d.shift;
+    using Pc = Piece<BF16>;
+    constexpr int E = Pc::N, ELT = 16 / E, PW = 64 / LP, S = HB < LP ? HB : LP;
+    const PageDims &d = a.d;
+    const int p = blockIdx.y, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % LP, place = lane / LP;
+    const int n = (rows_of(d, a.pv.lengths, s) + d.page - 1) >> d.shift;
+    const bool mine = c * E < d.D;                             // lanes behind the row's end are padding
+    const char *q = a.q + (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G) * d.D * ELT + c * 16;
+    const int64_t row = (int64_t)d.D * ELT;
+    const char *bounds = a.pv.bounds + ((int64_t)layer * d.n_pages * d.Hkv + head) * 2 * row + c * 16;
+    double up[HB][E], down[HB][E];                             // q+ and q-
+    auto load_heads = [&](int g0) {
+#pragma unroll
+        for (int g = 0; g < HB; ++g) {
+            u32x4 x{0, 0, 0, 0};
+            if (mine && g0 + g < d.G) x = *reinterpret_cast<const u32x4 *>(q + (g0 + g) * row);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const double v = Pc::get(x, e);
+                up[g][e] = fmax(v, 0.0);
+                down[g][e] = fmin(v, 0.0);
+                if (v != v) up[g][e] = v;                      // what is no number stays one
+            }
+        }
+    };
+    if constexpr (!MANY) load_heads(0);
+    for (int i0 = (blockIdx.x * (NT / 64) + wave) * PW * FLIGHT; i0 < n; i0 += gridDim.x * (NT / 64) * PW * FLIGHT) {
+        int id[FLIGHT];
+        u32x4 lo[FLIGHT], hi[FLIGHT];
+        uint32_t key[FLIGHT];
+#pragma unroll
+        for (int u = 0; u < FLIGHT; ++u) {
+            const int i = i0 + u * PW + place;
+            id[u] = i < n ? page_at(d, a.pv.table, s, i) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < FLIGHT; ++u) {
+            lo[u] = hi[u] = u32x4{0, 0, 0, 0};
+            key[u] = 0;
+            if (id[u] >= 0 && mine) {
+                const char *b = bounds + (int64_t)id[u] * d.Hkv * 2 * row;
+                lo[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(b));
+                hi[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(b + row));
+            }
+        }
+        for (int g0 = 0; g0 < (MANY ? d.G : 1); g0 += HB) {
+            if constexpr (MANY) {
+                load_heads(g0);
+#pragma unroll
+                for (int u = 0; u < FLIGHT; ++u)               // converted anew for every walk: in fp64 they would not fit the registers
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(lo[u][i]), "+v"(hi[u][i]));
+            }
+#pragma unroll
+            for (int u = 0; u < FLIGHT; ++u) {
+                double x[HB];
+#pragma unroll
+                for (int g = 0; g < HB; ++g) x[g] = 0.0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const double l = Pc::get(lo[u], e), h = Pc::get(hi[u], e);
+#pragma unroll
+                    for (int g = 0; g < HB; ++g) x[g] = fma(up[g][e], h, fma(down[g][e], l, x[g]));
+                }
+                sum_lanes<1, S, LP, HB>(x);
+#pragma unroll
+                for (int j = 0; j < HB / S; ++j)
+                    if (g0 + c % S + S * j < d.G) key[u] = max(key[u], x[j] == x[j] ? ordered_key((float)x[j]) : NOT_A_NUMBER);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < FLIGHT; ++u) {
+            const int i = i0 + u * PW + place;
+            const uint32_t x = most_of_lanes<1, S>(key[u]);
+            if (c == 0 && i < n) a.keys[(int64_t)p * a.stride + i] = id[u] >= 0 ? x : ordered_key(-INFINITY);
+        }
+    }
+}
+
+__device__ __forceinline__ int sum_upto(int x, int lane)       // inclusive, over the lanes
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(x, o);
+        if (lane >= o) x += u;
+    }
+    return x;
+}
+
+constexpr int DIGIT = 11, BINS = 1 << DIGIT;
+
+// grid P: the first and the last pages and the best of the others, the lower page first where keys are equal.  A thread has RUN consecutive pages,
+// or (RUN = 0) as many as it takes, read again in every pass.
+template <int RUN>
+__global__ void __launch_bounds__(PICK_NT)
+pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, const uint32_t *keys_all, int stride, int32_t *list_all)
+{
+    constexpr int NWV = PICK_NT / 64;
+    __shared__ int hist[BINS], red[2 * NWV];
+    __shared__ uint32_t extreme[2 * NWV];
+    __shared__ int found[3];                                   // bin, taken from it, its size
+    const int p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = (rows_of(d, pv.lengths, seq_of_problem(d, p)) + d.page - 1) >> d.shift;
     int32_t *list = list_all + (int64_t)p * n_pick;
     if (n <= n_pick) {
         for (int i = tid; i < n_pick; i += PICK_NT) list[i] = i < n ? i : -1;
         return;
     }
-    const uint32_t *keys = keys_all + (int64_t)p * d.max_pages;
-    uint32_t prefix = 0;
-    int left = n_pick;                                         // of the pages whose upper digits are the prefix's
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += PICK_NT) {
-            const uint32_t x = keys[i];
-            if (shift == 24 || (x >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(x >> shift) & 255], 1);
+    const uint32_t *keys = keys_all + (int64_t)p * stride;
+    const int run = RUN ? RUN : ((n + PICK_NT - 1) / PICK_NT + 3) & ~3, from = (int)min((int64_t)n, (int64_t)tid * run), to = min(n, from + run);
+    const int rest0 = n_first, rest1 = n - n_last;             // the pages that have to be ranked
+    uint32_t own[RUN ? RUN : 1];
+    if constexpr (RUN > 0) {
+#pragma unroll
+        for (int j = 0; j < RUN; j += 4) {
+            u32x4 x{0, 0, 0, 0};
+            if (from + j < to) x = *reinterpret_cast<const u32x4 *>(keys + from + j);          // the row's end is padded
+#pragma unroll
+            for (int i = 0; i < 4; ++i) own[j + i] = x[i];
         }
-        __syncthreads();
-        if (tid < 64) {                                        // lane l has the digits 255 - 4 l .. 252 - 4 l
-            int c[4], sum = 0;
-            for (int j = 0; j < 4; ++j) { c[j] = hist[255 - 4 * tid - j]; sum += c[j]; }
-            int upto = sum;
-            for (int o = 1; o < 64; o <<= 1) {
-                const int u = __shfl_up(upto, o);
-                if (tid >= o) upto += u;
-            }
-            int before = upto - sum;
-            if (before < left && upto >= left)                 // one lane
-                for (int j = 0; j < 4; ++j) {
-                    if (before < left && before + c[j] >= left) {
-                        s_prefix = prefix | (uint32_t)(255 - 4 * tid - j) << shift;
-                        s_left = left - before;
-                    }
-                    before += c[j];
-                }
-        }
-        __syncthreads();
-        prefix = s_prefix;
-        left = s_left;
     }
-    const int run = (n + PICK_NT - 1) / PICK_NT, from = min(n, tid * run), to = min(n, from + run);
+    auto ranked = [&](auto &&f) {                              // f(key, page) for the thread's pages that have to be ranked
+        if constexpr (RUN > 0) {
+#pragma unroll
+            for (int j = 0; j < RUN; ++j)
+                if (from + j >= rest0 && from + j < min(to, rest1)) f(own[j], from + j);
+        } else {
+            for (int i = max(from, rest0); i < min(to, rest1); ++i) f(keys[i], i);
+        }
+    };
+    uint32_t least = 0xffffffffu, most = 0;
+    ranked([&](uint32_t x, int) { least = min(least, x); most = max(most, x); });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { least = min(least, (uint32_t)__shfl_xor((int)least, o)); most = max(most, (uint32_t)__shfl_xor((int)most, o)); }
+    if (lane == 0) { extreme[wave] = least; extreme[NWV + wave] = most; }
+    for (int i = tid; i < BINS; i += PICK_NT) hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) { least = min(least, extreme[w]); most = max(most, extreme[NWV + w]); }
+    // the last key that is taken lies in [least, least + 2^bits)
+    int left = n_pick - n_first - n_last, bits = most > least ? 32 - __clz((int)(most - least)) : 0, inside = rest1 - rest0;
+    while (left > 0 && left < inside && bits > 0) {
+        const int shift = max(0, bits - DIGIT);
+        ranked([&](uint32_t x, int) {
+            const uint32_t at = x - least;
+            if (x >= least && (bits == 32 || at >> bits == 0)) atomicAdd(&hist[at >> shift], 1);
+        });
+        __syncthreads();
+        const int b0 = BINS - 1 - 2 * tid, h0 = hist[b0], h1 = hist[b0 - 1];   // two bins per thread, the largest first
+        const int upto = sum_upto(h0 + h1, lane);
+        if (lane == 63) red[wave] = upto;
+        __syncthreads();
+        int before = upto - h0 - h1;
+#pragma unroll
+        for (int w = 0; w < NWV; ++w) before += w < wave ? red[w] : 0;
+        if (before < left && before + h0 >= left) { found[0] = b0; found[1] = left - before; found[2] = h0; }
+        else if (before + h0 < left && before + h0 + h1 >= left) { found[0] = b0 - 1; found[1] = left - before - h0; found[2] = h1; }
+        hist[b0] = hist[b0 - 1] = 0;
+        __syncthreads();
+        least += (uint32_t)found[0] << shift;
+        left = found[1];
+        inside = found[2];
+        bits = shift;
+        __syncthreads();
+    }
+    // taken: above [least, least + 2^bits), and of those inside all (left == inside) or the first `left` (bits == 0) or none
+    const bool all = left == inside;
     int gt = 0, eq = 0;
-    for (int i = from; i < to; ++i) { gt += keys[i] > prefix; eq += keys[i] == prefix; }
-    int gt_upto = gt, eq_upto = eq;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int a = __shfl_up(gt_upto, o), b = __shfl_up(eq_upto, o);
-        if ((tid & 63) >= o) { gt_upto += a; eq_upto += b; }
-    }
-    if ((tid & 63) == 63) { wave_gt[tid >> 6] = gt_upto; wave_eq[tid >> 6] = eq_upto; }
+    auto inside_of = [&](uint32_t x) { return x >= least && (bits == 32 || (x - least) >> bits == 0); };
+    ranked([&](uint32_t x, int) {
+        const bool in = inside_of(x);
+        gt += in ? all : x >= least;
+        eq += in && !all;
+    });
+    gt += max(0, min(to, rest0) - from) + max(0, to - max(from, rest1));       // those that are taken in any case
+    const int gt_upto = sum_upto(gt, lane), eq_upto = sum_upto(eq, lane);
+    if (lane == 63) { red[wave] = gt_upto; red[NWV + wave] = eq_upto; }
     __syncthreads();
     int gt_before = gt_upto - gt, eq_before = eq_upto - eq;
-    for (int w = 0; w < tid >> 6; ++w) { gt_before += wave_gt[w]; eq_before += wave_eq[w]; }
-    for (int i = from; i < to; ++i) {
-        const uint32_t x = keys[i];
-        if (x > prefix || (x == prefix && eq_before < left)) list[gt_before + min(eq_before, left)] = i;
-        gt_before += x > prefix;
-        eq_before += x == prefix;
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) {
+        gt_before += w < wave ? red[w] : 0;
+        eq_before += w < wave ? red[NWV + w] : 0;
     }
+    const int some = all ? 0 : left;                           // of those inside, in the order of their pages
+    int at = gt_before + min(eq_before, some);
+    for (int i = from; i < min(to, rest0); ++i) list[at++] = i;
+    ranked([&](uint32_t x, int i) {
+        const bool in = inside_of(x);
+        if (in ? all || eq_before < some : x >= least) list[at++] = i;
+        eq_before += in && !all;
+    });
+    for (int i = max(from, rest1); i < to; ++i) list[at++] = i;
+}
+
+int key_stride(const PageDims &d) { return (d.max_pages + 3) & ~3; }
+
+template <bool BF16, int LP>
+void (*scores_for(int G))(ScoreArgs)
+{
+    return G == 1 ? page_scores_kernel<BF16, LP, 1, false> : G == 2 ? page_scores_kernel<BF16, LP, 2, false>
+         : G <= 4 ? page_scores_kernel<BF16, LP, 4, false> : page_scores_kernel<BF16, LP, 4, true>;
 }
 
 }  // namespace
 
-size_t select_pages_ws_bytes(const PageDims &d) { return align256((size_t)d.P * d.max_pages * 4); }
+size_t select_pages_ws_bytes(const PageDims &d) { return align256((size_t)d.P * key_stride(d) * 4); }
 
 hipError_t launch_select_pages(const PageDims &d, const void *q, const PageView &pv, int32_t n_pick, int32_t n_first, int32_t n_last,
                                int32_t *list, void *ws, hipStream_t st)
 {
-    uint32_t *keys = static_cast<uint32_t *>(ws);
-    if (d.max_pages > n_pick)                                  // otherwise every list is whole
-        hipLaunchKernelGGL(d.dtype == SABLOCK_BF16 ? page_scores_kernel<true> : page_scores_kernel<false>, dim3((d.max_pages + NT - 1) / NT, d.P),
-                           dim3(NT), 0, st, d, pv, static_cast<const char *>(q), n_first, n_last, keys);
-    hipLaunchKernelGGL(pick_pages_kernel, dim3(d.P), dim3(PICK_NT), 0, st, d, pv, n_pick, keys, list);
+    ScoreArgs a;
+    a.d = d;
+    a.pv = pv;
+    a.q = static_cast<const char *>(q);
+    a.stride = key_stride(d);
+    a.keys = static_cast<uint32_t *>(ws);
+    if (d.max_pages > n_pick) {                                // otherwise every list is whole
+        const int pieces = d.D * elt_bytes(d) / 16;
+        int lp = 1;
+        while (lp < pieces) lp *= 2;
+        const bool bf = d.dtype == SABLOCK_BF16;
+        void (*fn)(ScoreArgs) = nullptr;
+        // bf16 rows of up to 32 pieces, fp32 rows of 2 to 64: twice as many for the same heads
+#define SABLOCK_SCORES(LV) if (bf && lp == LV) fn = scores_for<true, LV>(d.G); if (!bf && lp == 2 * LV) fn = scores_for<false, 2 * LV>(d.G);
+        SABLOCK_SCORES(1) SABLOCK_SCORES(2) SABLOCK_SCORES(4) SABLOCK_SCORES(8) SABLOCK_SCORES(16) SABLOCK_SCORES(32)
+#undef SABLOCK_SCORES
+        if (!fn) return hipErrorInvalidValue;
+        const int pages = NT / lp * FLIGHT;                    // of a workgroup at a time
+        const int parts = std::max(1, std::min((d.max_pages + pages - 1) / pages, (4 * d.cus + d.P - 1) / d.P));
+        hipLaunchKernelGGL(fn, dim3(parts, d.P), dim3(NT), 0, st, a);
+    }
+    const int run = (d.max_pages + PICK_NT - 1) / PICK_NT;     // per thread
+    const auto pick = run <= 4 ? pick_pages_kernel<4> : run <= 8 ? pick_pages_kernel<8> : run <= 16 ? pick_pages_kernel<16> : pick_pages_kernel<0>;
+    hipLaunchKernelGGL(pick, dim3(d.P), dim3(PICK_NT), 0, st, d, pv, n_pick, n_first, n_last, a.keys, a.stride, list);
     return hipGetLastError();
 }
 

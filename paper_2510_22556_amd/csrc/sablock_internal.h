@@ -161,6 +161,26 @@ inline ChunkPlan plan_chunks(int64_t P, int64_t L, int64_t slots, int step, int 
     return {(int)best_len, (int)((L + best_len - 1) / best_len), by_chunk};
 }
 
+// value of lane ^ M
+template <int M>
+__device__ __forceinline__ float xor_lane(float x)
+{
+    const int v = __float_as_int(x);
+    if constexpr (M == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true));
+    if constexpr (M == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true));
+    if constexpr (M == 4) {                                    // banks 0, 2 from four lanes up, banks 1, 3 from four lanes down
+        const int a = __builtin_amdgcn_update_dpp(v, v, 0x104, 0xF, 0x5, false);
+        return __int_as_float(__builtin_amdgcn_update_dpp(a, v, 0x114, 0xF, 0xA, false));
+    }
+    if constexpr (M == 8) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true));
+    if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+        return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
+    }
+    const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ---- kernel launchers (each returns the hipError_t of its launches) ----

@@ -448,7 +448,7 @@ def test_select_of_equal_scores_and_of_what_is_no_number(torch_cuda):  # noqa: F
     assert c.select(q, 1999, 0, 0)[0].tolist() == [i for i in range(2000) if i != 700]
 
 
-@pytest.mark.parametrize("rows", [65536 * 16 + 1, 20000 * 16])
+@pytest.mark.parametrize("rows", [65536 * 16 + 1, 20000 * 16, 5000 * 16 + 7, 12001 * 16])
 def test_select_among_many_pages(torch_cuda, rows):  # noqa: F811
     torch = torch_cuda
     c = Cache(torch, 3, [rows], heads=1, group=1, D=8)
