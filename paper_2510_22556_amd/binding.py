@@ -143,8 +143,35 @@ def _stream(stream) -> Optional[int]:
     import torch
 
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the handle alone: torch.cuda.current_stream() builds an object around it, 2.8 us
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
     return stream.cuda_stream or None
+
+
+def _here(*tensors):
+    """The calls on a paged cache take tensors of the current device: another one's, or the host's, the kernels could not follow."""
+    import torch
+
+    for t in tensors:
+        if t is not None and t.get_device() < 0:
+            raise ValueError("a tensor on the host: the calls take device memory")
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"a tensor on cuda:{t.get_device()} while cuda:{at} is the current device")
+
+
+def _dense(dtype, n: int, *tensors):
+    """Dense tensors of at least n elements: what the calls index without strides."""
+    for t in tensors:
+        if t is not None and not (t.dtype is dtype and t.is_contiguous() and t.numel() >= n):
+            raise ValueError(f"need a dense {dtype} tensor of at least {n} elements, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _cache_dtype(c):
+    import torch
+
+    return torch.float32 if c.dtype == SABLOCK_F32 else torch.bfloat16
 
 
 def make_shape(q, k, v=None, **tuning) -> CShape:
@@ -410,6 +437,13 @@ def make_new_tokens(k, v, q=None, rotary_dim: Optional[int] = None, interleaved:
 
 def sablock_compact_paged(shape: CShape, k, v, idx, budget: int, append_window: bool, pages: CPages, page_table, k_pool, v_pool, bounds=None,
                           lengths_out=None, stream=None):
+    import torch
+
+    _here(k, v, idx, page_table, k_pool, v_pool, bounds, lengths_out)
+    _dense(torch.int32, n_problems(shape) * budget, idx)
+    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
+    _dense(torch.int32, pages.n_seq, lengths_out)
+    _dense(_cache_dtype(pages), pages.n_layers * pages.n_pages * pages.n_kv_heads * 2 * pages.head_dim, bounds)
     _check(load().sablock_compact_paged(ctypes.byref(shape), _ptr(k), _ptr(v), _ptr(idx), budget, 1 if append_window else 0, ctypes.byref(pages),
                                         _ptr(page_table), _ptr(k_pool), _ptr(v_pool), _ptr(bounds), _ptr(lengths_out), _stream(stream)))
 
@@ -417,6 +451,16 @@ def sablock_compact_paged(shape: CShape, k, v, idx, budget: int, append_window: 
 def sablock_append_paged(pages: CPages, tokens: CNewTokens, k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q=None, q_out=None,
                          counts=None, bounds=None, stream=None):
     """``lengths`` are the rows of every sequence WITH the new tokens."""
+    import torch
+
+    _here(k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q, q_out, counts, bounds)
+    _dense(torch.int32, pages.n_seq, positions, lengths, counts)
+    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
+    _dense(torch.float32, tokens.rotary_dim // 2, inv_freq)
+    _dense(_cache_dtype(pages), pages.n_seq * pages.n_layers * pages.n_q_heads * tokens.n_new * pages.head_dim, q_out)
+    _dense(_cache_dtype(pages), pages.n_layers * pages.n_pages * pages.n_kv_heads * 2 * pages.head_dim, bounds)
+    if not (k.dtype is v.dtype is k_pool.dtype and (q is None or q.dtype is k.dtype)):
+        raise ValueError("q, k and v are of the cache's dtype")
     _check(load().sablock_append_paged(ctypes.byref(pages), ctypes.byref(tokens), _ptr(q), _ptr(k), _ptr(v), _ptr(counts), _ptr(positions),
                                        _ptr(inv_freq), _ptr(page_table), _ptr(lengths), _ptr(q_out), _ptr(k_pool), _ptr(v_pool), _ptr(bounds),
                                        _stream(stream)))
@@ -430,9 +474,18 @@ def sablock_decode_paged_workspace_bytes(pages: CPages) -> int:
 
 def sablock_decode_paged(pages: CPages, q, k_pool, v_pool, page_table, lengths, out, ws, page_list=None, stream=None):
     """``page_list [P, n]`` int32, dense: the pages to read (``sablock_select_pages``); None = all."""
+    import torch
+
+    _here(q, k_pool, v_pool, page_table, lengths, out, ws, page_list)
+    n = 0 if page_list is None else page_list.shape[-1]
+    queries = pages.n_seq * pages.n_layers * pages.n_q_heads * pages.head_dim
+    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
+    _dense(torch.int32, pages.n_seq, lengths)
+    _dense(torch.int32, n_problems(pages) * n, page_list)
+    _dense(_cache_dtype(pages), queries, q)
+    _dense(torch.float32, queries, out)
     _check(load().sablock_decode_paged(ctypes.byref(pages), _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(lengths),
-                                       _ptr(page_list), 0 if page_list is None else page_list.shape[-1], _ptr(out), _ptr(ws),
-                                       ws.numel() * ws.element_size(), _stream(stream)))
+                                       _ptr(page_list), n, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def sablock_select_pages_workspace_bytes(pages: CPages) -> int:
@@ -442,6 +495,14 @@ def sablock_select_pages_workspace_bytes(pages: CPages) -> int:
 
 
 def sablock_select_pages(pages: CPages, q, bounds, page_table, lengths, n_pick: int, list_out, ws, n_first: int = 1, n_last: int = 1, stream=None):
+    import torch
+
+    _here(q, bounds, page_table, lengths, list_out, ws)
+    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
+    _dense(torch.int32, pages.n_seq, lengths)
+    _dense(torch.int32, n_problems(pages) * n_pick, list_out)
+    _dense(_cache_dtype(pages), pages.n_seq * pages.n_layers * pages.n_q_heads * pages.head_dim, q)
+    _dense(_cache_dtype(pages), pages.n_layers * pages.n_pages * pages.n_kv_heads * 2 * pages.head_dim, bounds)
     _check(load().sablock_select_pages(ctypes.byref(pages), _ptr(q), _ptr(bounds), _ptr(page_table), _ptr(lengths), n_pick, n_first, n_last,
                                        _ptr(list_out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 

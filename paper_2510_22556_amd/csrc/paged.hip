@@ -89,22 +89,31 @@ template <bool BF16> struct Bounds {                           // of the element
     }
 };
 
-// bounds of a chunk over the row groups of a workgroup: sh[group][chunk]; what the first group's threads get is joined
-template <bool BF16>
-__device__ void join_groups(Bounds<BF16> &b, Bounds<BF16> *sh, int groups, int per_group, int group, int place, bool active)
+// Bounds of a workgroup's chunks over its row groups, sh[group][place], written where at(place) says (nullptr: nowhere), joined with what is
+// there if `extend`.  A thread joins one dword of one place: consecutive lanes, consecutive banks.
+template <bool BF16, typename At>
+__device__ void store_joined(const Bounds<BF16> &b, uint32_t *sh, int groups, int places, int group, int place, bool active, int row_bytes, bool extend, At &&at)
 {
+    using E = Elem<BF16>;
     __syncthreads();
-    if (active) sh[group * per_group + place] = b;
+    if (active) {
+        u32x4 *o = reinterpret_cast<u32x4 *>(sh) + (group * places + place) * 2;
+        o[0] = b.lo;
+        o[1] = b.hi;
+    }
     __syncthreads();
-    if (active && group == 0)
-        for (int g = 1; g < groups; ++g) {
-            const Bounds<BF16> o = sh[g * per_group + place];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                b.lo[i] = Elem<BF16>::lower(b.lo[i], o.lo[i]);
-                b.hi[i] = Elem<BF16>::upper(b.hi[i], o.hi[i]);
-            }
-        }
+    for (int i = threadIdx.x; i < places * 8; i += NT) {
+        const int w = i & 7;
+        char *dst = at(i >> 3);
+        if (!dst) continue;
+        uint32_t x = sh[i];
+        auto join = [&](uint32_t y) { x = w < 4 ? E::lower(x, y) : E::upper(x, y); };
+#pragma unroll 4
+        for (int g = 1; g < groups; ++g) join(sh[g * places * 8 + i]);
+        uint32_t *word = reinterpret_cast<uint32_t *>(dst + (w < 4 ? 0 : row_bytes)) + (w & 3);
+        if (extend) join(E::ordered(*word));
+        *word = E::ordered(x);
+    }
 }
 
 __device__ __forceinline__ char *bounds_at(const PageDims &d, const PageView &v, int32_t layer, int32_t id, int32_t head)
@@ -119,7 +128,7 @@ compact_paged_kernel(Dims d, PageDims pd, PageView pv, const char *k, const char
                      int chunks, int32_t *lengths_out)
 {
     using E = Elem<BF16>;
-    __shared__ Bounds<BF16> sh[NT];
+    __shared__ __attribute__((aligned(16))) uint32_t sh[NT * 8];
     const int p = blockIdx.y, s = seq_of_problem(pd, p), layer = layer_of_problem(pd, p), head = head_of_problem(pd, p);
     if (lengths_out && blockIdx.x == 0 && layer == 0 && head == 0 && threadIdx.x == 0) lengths_out[s] = rows;
     const int r0 = blockIdx.x << pd.shift, n = min(pd.page, rows - r0);
@@ -146,11 +155,13 @@ compact_paged_kernel(Dims d, PageDims pd, PageView pv, const char *k, const char
             b.add(x);
         }
     if (!pv.bounds) return;
-    join_groups<BF16>(b, sh, groups, chunks, group, c, active);
-    if (group == 0) b.store(bounds_at(pd, pv, layer, id, head) + c * 16, pd.D * E::BYTES);
+    char *at = bounds_at(pd, pv, layer, id, head);
+    store_joined<BF16>(b, sh, groups, chunks, group, c, active, pd.D * E::BYTES, false, [&](int place) { return at + place * 16; });
 }
 
 constexpr int ANGLES = 4096;                   // (token, pair) whose sine and cosine LDS holds at a time
+constexpr int BATCH = 4;                       // rows of a thread in flight, twice
+constexpr int APPEND_WGS = 8;                  // workgroups per compute unit, if the head rows allow
 
 struct AppendArgs {
     PageDims d;
@@ -167,14 +178,21 @@ struct AppendArgs {
 
 // grid (touched pages, sequences x layers, parts of the head rows).  The angle of a (token, pair) is the same for all heads: formed
 // once per workgroup, position * inv_freq in whole turns in fp64 (at position 131 072 an angle in fp32 is off by up to 2^-8), the
-// fraction of a turn in fp32.
-template <bool BF16>
-__global__ void __launch_bounds__(NT)
+// fraction of a turn in fp32.  A thread has one chunk of every groups-th row of a head; half of a pair that lies in another chunk is read
+// as well, which the cache serves.  The rows of the next step are on their way while one is turned and stored, the first
+// ones while the angles are formed.
+// ONE: a token per sequence, and a workgroup has no more head rows than it does at a time.  SPLIT: the two elements of a pair lie half a rotation
+// apart, in different chunks.
+// Loads of a step are issued whatever the lane has to do there (at the nearest place that exists): behind a branch the compiler could
+// not count the loads in flight and would wait for all of them.  A step whose rows all exist stores without a branch for the same reason.
+template <bool BF16, bool ONE, bool SPLIT>
+__global__ void __launch_bounds__(NT, ONE ? 4 : 3)
 append_paged_kernel(AppendArgs a)
 {
     using E = Elem<BF16>;
-    __shared__ Bounds<BF16> sh[NT];
-    __shared__ float2 turn[ANGLES];                            // cosine, sine
+    constexpr int B = ONE ? 1 : BATCH;
+    __shared__ __attribute__((aligned(16))) uint32_t sh[ONE ? 1 : NT * 8];
+    __shared__ __attribute__((aligned(16))) float2 turn[ONE ? 128 : ANGLES];               // cosine, sine
     const PageDims &d = a.d;
     const int s = blockIdx.y / d.n_layers, layer = blockIdx.y - s * d.n_layers, tid = threadIdx.x;
     const int len = rows_of(d, a.pv.lengths, s);
@@ -184,78 +202,147 @@ append_paged_kernel(AppendArgs a)
     const int begin = max(first, page << d.shift), end = min(len, (page + 1) << d.shift);
     if (begin >= end) return;
     const int id = page_at(d, a.pv.table, s, page);
-    const int half = a.t.R / 2, pair_chunks = half / E::N, rotated = a.t.R / E::N;
-    const int c = tid % a.chunks, at = tid / a.chunks, group = at % a.groups, lane_slot = at / a.groups;
+    // K and V of a page that does not exist go nowhere
+    const int slot0 = id < 0 ? max((int)blockIdx.z * a.per, 2 * d.Hkv) : blockIdx.z * a.per, slot_end = min(a.slots, ((int)blockIdx.z + 1) * a.per);
+    if (slot0 >= slot_end) return;
+    const int half = a.t.R / 2, pair_chunks = half / E::N;
+    const int c = tid % a.chunks, place = tid / a.chunks, group = place % a.groups, lane_slot = place / a.groups;
     const bool active = lane_slot < a.side;
-    const int slot_end = min(a.slots, ((int)blockIdx.z + 1) * a.per);
     const int64_t position0 = a.t.R ? (int64_t)a.positions[s] : 0;
+    // this chunk's part in the rotation: where its angles lie, and the chunk of the other elements of its pairs
+    const bool turned = c < 2 * pair_chunks, upper = SPLIT && turned && c >= pair_chunks;
+    const int angle = SPLIT ? (upper ? c - pair_chunks : c) * E::N : c * (E::N / 2);
+    const int partner = !turned ? 0 : (upper ? -pair_chunks : pair_chunks) * 16;
+
+    struct Source { const char *at; int64_t step; bool is_v; };
+    auto source = [&](int base) {
+        const int slot = min(base + lane_slot, slot_end - 1);
+        const bool is_k = slot < d.Hkv, is_v = !is_k && slot < 2 * d.Hkv;
+        const int head = is_k ? slot : is_v ? slot - d.Hkv : slot - 2 * d.Hkv;
+        const int64_t *st = is_k ? a.t.ks : is_v ? a.t.vs : a.t.qs;
+        return Source{(is_k ? a.k : is_v ? a.v : a.q) + (s * st[0] + layer * st[1] + head * st[2]) * E::BYTES + c * 16, st[3] * E::BYTES, is_v};
+    };
+    // the thread's pair of the angles, which it forms for every angle_step-th token
+    const int angle_step = half ? NT / half : 1, pair = half ? tid % half : 0, angle_tok = half ? tid / half : angle_step;
+    double turns_per = 0.0;
+    if (angle_tok < angle_step) turns_per = (double)a.inv_freq[pair] * 0.15915494309189535;
     for (int t0 = begin; t0 < end; t0 += a.tile) {
-        const int n = min(a.tile, end - t0);
-        if (a.t.R) {
-            __syncthreads();
-            for (int i = tid; i < n * half; i += NT) {
-                const int tok = i / half, pair = i - tok * half;
-                const double turns = (double)(position0 + t0 - first + tok) * ((double)a.inv_freq[pair] * 0.15915494309189535);
-                float sn, cs;
-                sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
-                turn[i] = make_float2(cs, sn);
+        const int n = min(a.tile, end - t0), rows = B * a.groups, batches = (n + rows - 1) / rows;
+        u32x4 x[B], o[SPLIT ? B : 1];
+        auto load = [&](int base, int b, u32x4 (&x)[B], u32x4 (&o)[SPLIT ? B : 1]) {
+            const Source r = source(base);
+            const char *from = r.at + (t0 - first) * r.step;
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                const char *p = from + min(group + (b * B + i) * a.groups, n - 1) * r.step;
+                x[i] = *reinterpret_cast<const u32x4 *>(p);
+                if constexpr (SPLIT) o[i] = *reinterpret_cast<const u32x4 *>(p + (r.is_v ? 0 : partner));
             }
+        };
+        load(slot0, 0, x, o);
+        if (a.t.R) {
+            if (t0 > begin) __syncthreads();
+            if (angle_tok < angle_step)
+                for (int tok = angle_tok; tok < n; tok += angle_step) {
+                    const double turns = (double)(position0 + t0 - first + tok) * turns_per;
+                    float sn, cs;
+                    sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
+                    turn[tok * half + pair] = make_float2(cs, sn);
+                }
             __syncthreads();
         }
-        for (int base = blockIdx.z * a.per; base < slot_end; base += a.side) {
+        Bounds<BF16> b;
+        b.clear();
+        for (int base = slot0, bt = 0;;) {
+            const bool slot_done = bt + 1 == batches;
+            const int next_base = slot_done ? base + a.side : base, next_bt = slot_done ? 0 : bt + 1;
+            u32x4 xn[B], on[SPLIT ? B : 1];
+            if constexpr (!ONE) load(next_base, next_bt, xn, on);              // behind the last: the last again
             const int slot = base + lane_slot;
-            const bool live = active && slot < slot_end, is_k = slot < d.Hkv, is_v = !is_k && slot < 2 * d.Hkv;
+            const bool is_k = slot < d.Hkv, is_v = !is_k && slot < 2 * d.Hkv, live = active && slot < slot_end;
             const int head = is_k ? slot : is_v ? slot - d.Hkv : slot - 2 * d.Hkv;
-            const int64_t *st = is_k ? a.t.ks : is_v ? a.t.vs : a.t.qs;
-            const char *src = (is_k ? a.k : is_v ? a.v : a.q) + (s * st[0] + layer * st[1] + head * st[2]) * E::BYTES;
-            Bounds<BF16> b;
-            b.clear();
-            if (live)
-                for (int r = group; r < n; r += a.groups) {
-                    const int row = t0 + r, tok = row - first;
-                    const char *x_at = src + tok * st[3] * E::BYTES;
-                    u32x4 x = *reinterpret_cast<const u32x4 *>(x_at + c * 16);
-                    if (!is_v && c < rotated) {
-                        float y[E::N];
-                        if (a.t.interleaved) {
+            char *dst;                                         // row t0
+            int64_t step;
+            if (is_k || is_v) {
+                const int64_t *ps = is_k ? d.ks : d.vs;
+                step = ps[3] * E::BYTES;
+                dst = (is_k ? a.pv.k : a.pv.v) + (layer * ps[0] + id * ps[1] + head * ps[2]) * E::BYTES + (t0 & (d.page - 1)) * step + c * 16;
+            } else {
+                step = d.D * E::BYTES;
+                dst = a.q_out + ((((int64_t)s * d.n_layers + layer) * d.Hq + head) * a.t.n_new + t0 - first) * step + c * 16;
+            }
+            auto turn_row = [&](int i) {
+                u32x4 w = x[i];
+                if (!turned || is_v) return w;
+                float y[E::N];
+                const float4 *angles = reinterpret_cast<const float4 *>(turn + min(group + (bt * B + i) * a.groups, n - 1) * half + angle);
+                if constexpr (SPLIT) {
 #pragma unroll
-                            for (int e = 0; e < E::N; e += 2) {
-                                const float2 w = turn[r * half + (c * E::N + e) / 2];
-                                const float u = E::get(x, e), z = E::get(x, e + 1);
-                                y[e] = u * w.x - z * w.y;
-                                y[e + 1] = z * w.x + u * w.y;
-                            }
-                        } else {
-                            const bool up = c >= pair_chunks;
-                            const u32x4 o = *reinterpret_cast<const u32x4 *>(x_at + (up ? c - pair_chunks : c + pair_chunks) * 16);
-#pragma unroll
-                            for (int e = 0; e < E::N; ++e) {
-                                const float2 w = turn[r * half + (up ? c - pair_chunks : c) * E::N + e];
-                                const float u = E::get(x, e), z = E::get(o, e);
-                                y[e] = u * w.x + (up ? z : -z) * w.y;
-                            }
-                        }
-                        x = E::pack(y);
+                    for (int e = 0; e < E::N; e += 2) {
+                        const float4 t = angles[e / 2];
+                        const float z0 = E::get(o[i], e), z1 = E::get(o[i], e + 1);
+                        y[e] = E::get(w, e) * t.x + (upper ? z0 : -z0) * t.y;
+                        y[e + 1] = E::get(w, e + 1) * t.z + (upper ? z1 : -z1) * t.w;
                     }
-                    if (is_k || is_v) {
-                        if (id < 0) continue;
-                        const int64_t *ps = is_k ? d.ks : d.vs;
-                        char *dst = (is_k ? a.pv.k : a.pv.v) + (layer * ps[0] + id * ps[1] + head * ps[2] + (row & (d.page - 1)) * ps[3]) * E::BYTES;
-                        *reinterpret_cast<u32x4 *>(dst + c * 16) = x;
-                        if (is_k) b.add(x);
-                    } else {
-                        const int64_t out_row = (((int64_t)s * d.n_layers + layer) * d.Hq + head) * a.t.n_new + tok;
-                        *reinterpret_cast<u32x4 *>(a.q_out + out_row * d.D * E::BYTES + c * 16) = x;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E::N; e += 4) {
+                        const float4 t = angles[e / 4];
+                        const float u0 = E::get(w, e), z0 = E::get(w, e + 1), u1 = E::get(w, e + 2), z1 = E::get(w, e + 3);
+                        y[e] = u0 * t.x - z0 * t.y;
+                        y[e + 1] = z0 * t.x + u0 * t.y;
+                        y[e + 2] = u1 * t.z - z1 * t.w;
+                        y[e + 3] = z1 * t.z + u1 * t.w;
                     }
                 }
-            if (!a.pv.bounds || base >= d.Hkv) continue;       // the same for the whole workgroup
-            if (a.groups > 1) join_groups<BF16>(b, sh, a.groups, a.chunks * a.side, group, lane_slot * a.chunks + c, active);
-            if (live && is_k && group == 0 && id >= 0) {
-                char *at_bounds = bounds_at(d, a.pv, layer, id, head) + c * 16;
-                if (t0 & (d.page - 1))                         // rows in front of these
-                    b.merge_stored(*reinterpret_cast<const u32x4 *>(at_bounds), *reinterpret_cast<const u32x4 *>(at_bounds + d.D * E::BYTES));
-                b.store(at_bounds, d.D * E::BYTES);
+                return E::pack(y);
+            };
+            if (!ONE && a.side == 1 && a.chunks * a.groups == NT && (bt + 1) * rows <= n) {
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    x[i] = turn_row(i);
+                    *reinterpret_cast<u32x4 *>(dst + (group + (bt * B + i) * a.groups) * step) = x[i];
+                }
+                if (is_k) {
+#pragma unroll
+                    for (int i = 0; i < B; ++i) b.add(x[i]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    const int at = group + (bt * B + i) * a.groups;
+                    const u32x4 w = turn_row(i);
+                    if (live && at < n) {
+                        *reinterpret_cast<u32x4 *>(dst + at * step) = w;
+                        if (is_k) b.add(w);
+                    }
+                }
             }
+            if (slot_done && a.pv.bounds && base < d.Hkv) {    // the same for the whole workgroup
+                const bool extend = t0 & (d.page - 1);         // rows in front of these
+                if constexpr (ONE) {
+                    if (live && is_k) {
+                        char *at = bounds_at(d, a.pv, layer, id, head) + c * 16;
+                        if (extend) b.merge_stored(*reinterpret_cast<const u32x4 *>(at), *reinterpret_cast<const u32x4 *>(at + d.D * E::BYTES));
+                        b.store(at, d.D * E::BYTES);
+                    }
+                } else {
+                    store_joined<BF16>(b, sh, a.groups, a.chunks * a.side, group, lane_slot * a.chunks + c, active, d.D * E::BYTES, extend, [&](int place) {
+                        const int slot = base + place / a.chunks;
+                        return slot < min(slot_end, d.Hkv) ? bounds_at(d, a.pv, layer, id, slot) + place % a.chunks * 16 : nullptr;
+                    });
+                }
+                b.clear();
+            }
+            if constexpr (ONE) break;
+            if (next_base >= slot_end) break;
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                x[i] = xn[i];
+                if constexpr (SPLIT) o[i] = on[i];
+            }
+            base = next_base;
+            bt = next_bt;
         }
     }
 }
@@ -293,10 +380,16 @@ hipError_t launch_append_paged(const PageDims &pd, const TokenDims &td, const vo
     a.slots = 2 * pd.Hkv + (q ? pd.Hq : 0);
     const int64_t pages = (td.n_new + (int64_t)pd.page - 2) / pd.page + 1, units = pages * pd.n_seq * pd.n_layers;
     const int steps = (a.slots + a.side - 1) / a.side;         // of a workgroup that had them all
-    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(steps, 4 * pd.cus / units));
+    const bool one = td.n_new == 1, bf = pd.dtype == SABLOCK_BF16;
+    const int parts = one ? steps : (int)std::max<int64_t>(1, std::min<int64_t>(steps, APPEND_WGS * pd.cus / units));
     a.per = (steps + parts - 1) / parts * a.side;
     const dim3 grid((unsigned)pages, pd.n_seq * pd.n_layers, (a.slots + a.per - 1) / a.per);
-    hipLaunchKernelGGL(pd.dtype == SABLOCK_BF16 ? append_paged_kernel<true> : append_paged_kernel<false>, grid, dim3(NT), 0, st, a);
+    const bool split = td.R > 0 && !td.interleaved;
+#define SABLOCK_APPEND(SV) (one ? (bf ? append_paged_kernel<true, true, SV> : append_paged_kernel<false, true, SV>) \
+                                : (bf ? append_paged_kernel<true, false, SV> : append_paged_kernel<false, false, SV>))
+    const auto fn = split ? SABLOCK_APPEND(true) : SABLOCK_APPEND(false);
+#undef SABLOCK_APPEND
+    hipLaunchKernelGGL(fn, grid, dim3(NT), 0, st, a);
     return hipGetLastError();
 }
 

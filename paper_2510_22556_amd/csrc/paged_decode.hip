@@ -23,6 +23,7 @@
 #include "sablock_internal.h"
 
 #include <cfloat>
+#include <type_traits>
 
 namespace sablock {
 namespace {
@@ -63,6 +64,8 @@ struct DecodePagedArgs {
     const int32_t *list;
     int n_listed;
     float qscale;                // log2(e) / sqrt(D)
+    int workgroups;              // that share the long problems' steps
+    int limit;                   // steps of the longest problem that a workgroup takes alone
     float *out;                  // [n_seq][n_layers][Hq][D]
     float *weights;              // pieces [2 * workgroups][G][2]: reference (log2 domain), denominator
     float *sums;                 // pieces [2 * workgroups][G][D]
@@ -80,6 +83,13 @@ __device__ __forceinline__ int steps_of(const DecodePagedArgs &a, int s)
     }
     return (rows + STEP - 1) / STEP;
 }
+// the same of a problem whose steps are shared, 0 of one that is not
+template <int STEP>
+__device__ __forceinline__ int shared_steps_of(const DecodePagedArgs &a, int s)
+{
+    const int n = steps_of<STEP>(a, s);
+    return n > a.limit ? n : 0;
+}
 
 // Inclusive sum over the lanes.
 __device__ __forceinline__ int64_t scan(int64_t x, int lane)
@@ -92,7 +102,7 @@ __device__ __forceinline__ int64_t scan(int64_t x, int lane)
     return x;
 }
 
-// Where the problems' steps lie in the row of all of them; a wavefront's view, each lane with the sums up to its share of the sequences.
+// Where the long problems' steps lie in the row of all of them; a wavefront's view, each lane with the sums up to its share of the sequences.
 template <int STEP>
 struct Places {
     const DecodePagedArgs &a;
@@ -102,16 +112,21 @@ struct Places {
     {
         heads = a.d.n_layers * a.d.Hkv;
         share = (a.d.n_seq + 63) / 64;
+        if (a.d.n_seq == 1) {
+            upto = shared_steps_of<STEP>(a, 0);
+            total = upto * heads;
+            return;
+        }
         int64_t sum = 0;
         for (int i = 0; i < share; ++i)
-            if (lane * share + i < a.d.n_seq) sum += steps_of<STEP>(a, lane * share + i);
-        upto = a.d.n_seq > 1 ? scan(sum, lane) : sum;
-        total = (a.d.n_seq > 1 ? __shfl(upto, 63) : __shfl(upto, 0)) * heads;
+            if (lane * share + i < a.d.n_seq) sum += shared_steps_of<STEP>(a, lane * share + i);
+        upto = scan(sum, lane);
+        total = __shfl(upto, 63) * heads;
     }
     // the sequence that step x of all lies in (x < total), the steps of one problem of those before it, and of its own
     __device__ void find(int64_t x, int &seq, int64_t &before, int &steps) const
     {
-        if (a.d.n_seq == 1) { seq = 0; before = 0; steps = __shfl((int)upto, 0); return; }
+        if (a.d.n_seq == 1) { seq = 0; before = 0; steps = (int)upto; return; }
         int first = __ffsll((unsigned long long)__ballot(upto * heads > x)) - 1;
         int64_t at = first > 0 ? __shfl(upto, first - 1) : 0;
         if (share == 1) {
@@ -121,7 +136,7 @@ struct Places {
             return;
         }
         const int s = first * share + lane;
-        const int own = lane < share && s < a.d.n_seq ? steps_of<STEP>(a, s) : 0;
+        const int own = lane < share && s < a.d.n_seq ? shared_steps_of<STEP>(a, s) : 0;
         const int64_t inner = scan((int64_t)own, lane) + at;
         const int j = __ffsll((unsigned long long)__ballot(inner * heads > x)) - 1;
         seq = first * share + j;
@@ -133,14 +148,19 @@ struct Places {
     {
         const int first = seq / share;
         before = first > 0 ? __shfl(upto, first - 1) : 0;
-        for (int s = first * share; s < seq; ++s) before += steps_of<STEP>(a, s);
-        steps = steps_of<STEP>(a, seq);
+        for (int s = first * share; s < seq; ++s) before += shared_steps_of<STEP>(a, s);
+        steps = shared_steps_of<STEP>(a, seq);
     }
 };
+// x / n of whole numbers; 64 bits are a hundred instructions, and hardly ever needed
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t n)
+{
+    return (uint64_t)(x | n) >> 32 ? x / n : (int64_t)((uint32_t)x / (uint32_t)n);
+}
+// steps of a workgroup's run
 __device__ __forceinline__ int64_t run_of(int64_t total, int workgroups)
 {
-    if (total < 1 << 30) return max(LEAST_STEPS, ((int)total + workgroups - 1) / workgroups);
-    return (total + workgroups - 1) / workgroups;
+    return max((int64_t)LEAST_STEPS, quotient(total + workgroups - 1, workgroups));
 }
 
 __device__ __forceinline__ float over_quarters(float x, bool take_max)        // lanes l, l ^ 16, l ^ 32, l ^ 48
@@ -165,23 +185,13 @@ decode_paged_kernel(DecodePagedArgs a)
     const PageDims &d = a.d;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, c = lane >> 4;
-    const Places<STEP> places(a, lane);
-    const int64_t run = run_of(places.total, gridDim.x), run_from = blockIdx.x * run, run_to = min(run_from + run, places.total);
     // a lane's rows of a step: of K as operand (bf16: and that row + 4), of the results and of V from `row` on
     const int krow = BF16 ? (m >> 2) * 8 + (m & 3) : m, row = R * c;
     const int64_t kstep = d.ks[3] * ELT, vstep = d.vs[3] * ELT;
 
-    for (int64_t x = run_from; x < run_to;) {
-        int s, n;
-        int64_t before;
-        places.find(x, s, before, n);
-        s = __builtin_amdgcn_readfirstlane(s);
-        n = __builtin_amdgcn_readfirstlane(n);
-        const int64_t in_seq = x - before * places.heads;
-        const int problem = __builtin_amdgcn_readfirstlane(in_seq < 1 << 30 ? (int)in_seq / n : (int)(in_seq / n));
-        const int off = __builtin_amdgcn_readfirstlane((int)(in_seq - (int64_t)problem * n));
-        const int piece = (int)min((int64_t)(n - off), run_to - x);
-        const int layer = problem / d.Hkv, head = problem - layer * d.Hkv, p = s * places.heads + problem;
+    // a piece: steps off .. off + count of the n of problem p
+    auto piece = [&](int p, int s, int off, int count, int n) __attribute__((always_inline)) {
+        const int layer = layer_of_problem(d, p), head = head_of_problem(d, p);
         const int len = rows_of(d, a.pv.lengths, s), pages = (len + d.page - 1) >> d.shift;
         const int entries = a.list ? min(a.n_listed, pages) : pages;
         const int64_t qrow = (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G) * D;
@@ -195,7 +205,7 @@ decode_paged_kernel(DecodePagedArgs a)
 #pragma unroll
         for (int e = 0; e < EP; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        const int from = off + (int)((int64_t)piece * wave / NW), to = off + (int)((int64_t)piece * (wave + 1) / NW);
+        const int from = off + (int)((int64_t)count * wave / NW), to = off + (int)((int64_t)count * (wave + 1) / NW);
         // the page and the rows of it that count, of 64 entries at a time, one per lane
         int ids = 0, held = 0, base = -1 << 30;
         const char *kat = nullptr, *vat = nullptr;
@@ -252,7 +262,9 @@ decode_paged_kernel(DecodePagedArgs a)
             load_k();
             load_v();
         }
-        for (int st = from; st < to; ++st) {
+        // `more`: another step follows, whose loads are issued here.  Known to the compiler: behind a branch it could not count
+        // the loads in flight, and would wait for all of them.
+        auto step = [&](int st, auto more) __attribute__((always_inline)) {
             float z[R];
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
@@ -272,8 +284,7 @@ decode_paged_kernel(DecodePagedArgs a)
             }
             const bool now_whole = whole;
             const int now_limit = limit;
-            const bool more = st + 1 < to;
-            if (more) {
+            if constexpr (more.value) {
                 locate(st + 1);
                 load_k();
             }
@@ -332,7 +343,11 @@ decode_paged_kernel(DecodePagedArgs a)
                     for (int e = 0; e < EP; ++e)
                         acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e]), z[i], acc[e], 0, 0, 0);
             }
-            if (more) load_v();
+            if constexpr (more.value) load_v();
+        };
+        if (from < to) {
+            for (int st = from; st + 1 < to; ++st) step(st, std::true_type{});
+            step(to - 1, std::false_type{});
         }
         den = over_quarters(den, false);
 
@@ -348,7 +363,7 @@ decode_paged_kernel(DecodePagedArgs a)
                 for (int i = 0; i < 4; ++i) o[(2 + 4 * e + i) * 64] = acc[e][i];
         }
         __syncthreads();
-        if (wave == 0) {
+        if (wave == 0 && m < d.G) {                            // elements EP (4 c + i) + e of head m
             float w[NW], top = ref;
 #pragma unroll
             for (int u = 1; u < NW; ++u) { w[u] = sh[(u - 1) * KEEP * 64 + lane]; top = fmaxf(top, w[u]); }
@@ -359,44 +374,65 @@ decode_paged_kernel(DecodePagedArgs a)
                 w[u] = __builtin_amdgcn_exp2f(w[u] - top);
                 den += sh[((u - 1) * KEEP + 1) * 64 + lane] * w[u];
             }
+            float *o;
+            float f = 1.f;
+            if (count == n) {                                  // the whole problem
+                o = a.out + qrow + m * D;
+                f = den == 0.f ? 0.f : 1.f / den;
+            } else {
+                const int64_t slot = 2 * (int64_t)(blockIdx.x - d.P) + (off == 0);
+                o = a.sums + (slot * d.G + m) * D;
+                if (c == 0) {
+                    a.weights[(slot * d.G + m) * 2] = top;
+                    a.weights[(slot * d.G + m) * 2 + 1] = den;
+                }
+            }
 #pragma unroll
-            for (int e = 0; e < EP; ++e)
+            for (int u = 0; u < NW; ++u) w[u] *= f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int e = 0; e < EP; ++e) {
                     float t = acc[e][i] * w[0];
 #pragma unroll
                     for (int u = 1; u < NW; ++u) t = fmaf(sh[((u - 1) * KEEP + 2 + 4 * e + i) * 64 + lane], w[u], t);
-                    acc[e][i] = t;
+                    o[EP * (4 * c + i) + e] = t;
                 }
-            if (m < d.G) {                                     // elements EP (4 c + i) + e of head m
-                float *o;
-                float f = 1.f;
-                if (piece == n) {                              // the whole problem
-                    o = a.out + qrow + m * D;
-                    f = den == 0.f ? 0.f : 1.f / den;
-                } else {
-                    const int64_t slot = 2 * (int64_t)blockIdx.x + (off == 0);
-                    o = a.sums + (slot * d.G + m) * D;
-                    if (c == 0) {
-                        a.weights[(slot * d.G + m) * 2] = top;
-                        a.weights[(slot * d.G + m) * 2 + 1] = den;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < EP; ++e) o[EP * (4 * c + i) + e] = acc[e][i] * f;
+                asm volatile("" ::: "memory");                 // a quarter at a time: all of the others' sums do not fit the registers
             }
         }
-        x += piece;
+    };
+    if ((int)blockIdx.x < a.d.P) {
+        const int p = blockIdx.x, s = seq_of_problem(d, p), n = steps_of<STEP>(a, s);
+        if (n <= a.limit) piece(p, s, 0, n, n);
+        return;
+    }
+    const int me = blockIdx.x - d.P;
+    const Places<STEP> places(a, lane);
+    const int64_t run = run_of(places.total, a.workgroups), run_to = min((me + 1) * run, places.total);
+    int s = 0, n = 0;
+    int64_t seq_from = 0, seq_to = 0;                          // all steps of sequence s
+    for (int64_t x = me * run; x < run_to;) {
+        if (x >= seq_to) {
+            int64_t before;
+            places.find(x, s, before, n);
+            s = __builtin_amdgcn_readfirstlane(s);
+            n = __builtin_amdgcn_readfirstlane(n);
+            seq_from = before * places.heads;
+            seq_to = seq_from + (int64_t)n * places.heads;
+        }
+        const int problem = __builtin_amdgcn_readfirstlane((int)quotient(x - seq_from, n));
+        const int off = __builtin_amdgcn_readfirstlane((int)(x - seq_from - (int64_t)problem * n)), count = (int)min((int64_t)(n - off), run_to - x);
+        piece(s * places.heads + problem, s, off, count, n);
+        x += count;
     }
 }
 
 // grid (G, problems): the pieces' weights first, then their weighted sum, four elements per thread, the pieces dealt out to groups of threads
-constexpr int MERGE_T = 256, MAX_PIECES = 1024;
+constexpr int MERGE_T = 256, MAX_PIECES = 1024, EARLY = 2;
 template <int STEP>
 __global__ void __launch_bounds__(MERGE_T)
-decode_paged_merge_kernel(DecodePagedArgs a, int workgroups)
+decode_paged_merge_kernel(DecodePagedArgs a)
 {
     __shared__ float w_sh[MAX_PIECES], red[2 * (MERGE_T / 64)];
     __shared__ f32x4 sum[MERGE_T];
@@ -408,15 +444,18 @@ decode_paged_merge_kernel(DecodePagedArgs a, int workgroups)
     int64_t before;
     places.of(seq, before, n);
     float *out = a.out + ((((int64_t)seq * d.n_layers + layer_of_problem(d, p)) * d.Hq) + head_of_problem(d, p) * d.G + g) * d.D;
-    if (n == 0) {
-        for (int i = tid; i < d.D; i += MERGE_T) out[i] = 0.f;
-        return;
-    }
-    const int64_t run = run_of(places.total, workgroups), at = before * places.heads + (int64_t)(p - seq * places.heads) * n;
-    const int64_t first = at / run, pieces64 = (at + n - 1) / run - first + 1;
-    if (pieces64 == 1) return;                                 // finished where it was computed
-    const int pieces = (int)pieces64;
+    if (n == 0) return;                                        // a workgroup's alone
+    const int64_t run = run_of(places.total, a.workgroups), at = before * places.heads + (int64_t)(p - seq * places.heads) * n;
+    const int64_t first = quotient(at, run);
+    const int pieces = (int)(quotient(at + n - 1, run) - first) + 1;
+    if (pieces == 1) return;                                   // finished where it was computed
     auto slot = [&](int i) { return (2 * (first + i) + (i == 0)) * d.G + g; };
+    const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
+    // the first of the numerators are on their way while the weights are formed
+    auto part = [&](int i) { return *reinterpret_cast<const f32x4 *>(a.sums + slot(min(i, pieces - 1)) * d.D + 4 * c); };
+    f32x4 early[EARLY];
+#pragma unroll
+    for (int j = 0; j < EARLY; ++j) early[j] = part(group + j * groups);
     float m = -FLT_MAX;
     for (int i = tid; i < pieces; i += MERGE_T) m = fmaxf(m, a.weights[slot(i) * 2]);
 #pragma unroll
@@ -438,11 +477,13 @@ decode_paged_merge_kernel(DecodePagedArgs a, int workgroups)
     den = 0.f;
 #pragma unroll
     for (int i = 0; i < MERGE_T / 64; ++i) den += red[MERGE_T / 64 + i];
-    const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
     f32x4 t{0.f, 0.f, 0.f, 0.f};
     if (group < groups) {
+#pragma unroll
+        for (int j = 0; j < EARLY; ++j)
+            if (group + j * groups < pieces) t += early[j] * w_sh[group + j * groups];
 #pragma unroll 4
-        for (int i = group; i < pieces; i += groups) t += *reinterpret_cast<const f32x4 *>(a.sums + slot(i) * d.D + 4 * c) * w_sh[i];
+        for (int i = group + EARLY * groups; i < pieces; i += groups) t += part(i) * w_sh[i];
     }
     sum[tid] = t;
     __syncthreads();
@@ -454,9 +495,11 @@ decode_paged_merge_kernel(DecodePagedArgs a, int workgroups)
 // workgroups per compute unit that the registers leave room for
 int resident(const PageDims &d)
 {
-    return d.D <= 64 ? 3 : d.D <= 128 ? 2 : 1;
+    return d.D <= 96 ? 3 : d.D <= 192 ? 2 : 1;
 }
 int workgroups_of(const PageDims &d) { return std::min(d.cus * resident(d), MAX_PIECES - 1); }
+// rows of the longest problem that a workgroup takes alone
+int rows_alone(const PageDims &d) { return (d.P >= d.cus ? 1 << 19 : 1 << 18) / (2 * d.D * elt_bytes(d)); }
 
 }  // namespace
 
@@ -479,7 +522,10 @@ hipError_t launch_decode_paged(const PageDims &d, const void *q, const PageView 
     a.n_listed = n_listed;
     a.qscale = (float)(1.4426950408889634 / sqrt((double)d.D));
     a.out = out;
-    const int workgroups = workgroups_of(d);
+    const int64_t capacity = (int64_t)(list ? std::min(n_listed, d.max_pages) : d.max_pages) * d.page;
+    const int workgroups = workgroups_of(d), step = d.dtype == SABLOCK_BF16 ? 32 : 16;
+    a.limit = rows_alone(d) / step;
+    a.workgroups = capacity > (int64_t)a.limit * step ? workgroups : 0;        // no problem can be longer: all are taken alone
     a.weights = static_cast<float *>(ws);
     a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups * d.G * 8));
     const bool bf = d.dtype == SABLOCK_BF16;
@@ -492,8 +538,8 @@ hipError_t launch_decode_paged(const PageDims &d, const void *q, const PageView 
 #undef SABLOCK_PAGED_B
 #undef SABLOCK_PAGED_F
     if (!fn) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(fn, dim3(workgroups), dim3(NT), 0, st, a);
-    hipLaunchKernelGGL(bf ? decode_paged_merge_kernel<32> : decode_paged_merge_kernel<16>, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a, workgroups);
+    hipLaunchKernelGGL(fn, dim3(a.workgroups + d.P), dim3(NT), 0, st, a);
+    if (a.workgroups) hipLaunchKernelGGL(bf ? decode_paged_merge_kernel<32> : decode_paged_merge_kernel<16>, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
     return hipGetLastError();
 }
 
