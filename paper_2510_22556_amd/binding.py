@@ -10,12 +10,13 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsablock.so")
-_lib = None
+_lib = _torch = None
 
 SABLOCK_OK = 0
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "WORKSPACE_TOO_SMALL", 4: "DEVICE"}
@@ -75,7 +76,7 @@ class CNewTokens(ctypes.Structure):
 
 def load():
     """Load the HIP library (built in-tree by ``paper_2510_22556_amd.build``); raises if absent."""
-    global _lib
+    global _lib, _torch
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise FileNotFoundError(
@@ -83,8 +84,9 @@ def load():
                 "(there is no fallback path)")
         # torch first: it ships its own copy of the HIP runtime, and a process must hold one runtime only (device
         # pointers and streams of torch are meaningless to a second copy loaded through this library)
-        import torch  # noqa: F401
+        import torch
 
+        _torch = torch
         lib = ctypes.CDLL(LIB_PATH)
         vp, i32, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
         sp = ctypes.POINTER(CShape)
@@ -140,38 +142,34 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
-    import torch
-
     if stream is None:
         # the handle alone: torch.cuda.current_stream() builds an object around it, 2.8 us
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device()) or None
     return stream.cuda_stream or None
 
 
-def _here(*tensors):
-    """The calls on a paged cache take tensors of the current device: another one's, or the host's, the kernels could not follow."""
-    import torch
-
+def _pointers(*tensors):
+    """Device pointers (None stays) of tensors that are all on the current device: another one's, or the host's, the kernels could not
+    follow."""
+    at = tensors[0].get_device()
+    out = []
     for t in tensors:
-        if t is not None and t.get_device() < 0:
-            raise ValueError("a tensor on the host: the calls take device memory")
-    at = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != at:
-            raise ValueError(f"a tensor on cuda:{t.get_device()} while cuda:{at} is the current device")
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != at or at < 0:
+            raise ValueError(f"tensors on {tensors[0].device} and {t.device}: the calls take device memory, of one device")
+        out.append(t.data_ptr())
+    if at != _torch.cuda.current_device():
+        raise ValueError(f"tensors on cuda:{at} while cuda:{_torch.cuda.current_device()} is the current device")
+    return out
 
 
 def _dense(dtype, n: int, *tensors):
     """Dense tensors of at least n elements: what the calls index without strides."""
     for t in tensors:
-        if t is not None and not (t.dtype is dtype and t.is_contiguous() and t.numel() >= n):
+        if t is not None and (t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
             raise ValueError(f"need a dense {dtype} tensor of at least {n} elements, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
-
-
-def _cache_dtype(c):
-    import torch
-
-    return torch.float32 if c.dtype == SABLOCK_F32 else torch.bfloat16
 
 
 def make_shape(q, k, v=None, **tuning) -> CShape:
@@ -435,35 +433,48 @@ def make_new_tokens(k, v, q=None, rotary_dim: Optional[int] = None, interleaved:
     return t
 
 
+_PAGES_INTS = struct.Struct("9i")              # n_seq .. max_pages: one read, a structure's fields one by one cost as much as the launch
+
+
+def _cache_sizes(c: CPages):
+    """Type of a cache's elements, sequences, problems, entries of the page table, elements of the bounds and of one query per head."""
+    n_seq, n_layers, n_q_heads, n_kv_heads, head_dim, dtype, _, n_pages, max_pages = _PAGES_INTS.unpack_from(c)
+    d = n_layers * head_dim
+    return (_torch.float32 if dtype == SABLOCK_F32 else _torch.bfloat16, n_seq, n_seq * n_layers * n_kv_heads, n_seq * max_pages,
+            2 * d * n_pages * n_kv_heads, d * n_seq * n_q_heads)
+
+
 def sablock_compact_paged(shape: CShape, k, v, idx, budget: int, append_window: bool, pages: CPages, page_table, k_pool, v_pool, bounds=None,
                           lengths_out=None, stream=None):
-    import torch
-
-    _here(k, v, idx, page_table, k_pool, v_pool, bounds, lengths_out)
-    _dense(torch.int32, n_problems(shape) * budget, idx)
-    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
-    _dense(torch.int32, pages.n_seq, lengths_out)
-    _dense(_cache_dtype(pages), pages.n_layers * pages.n_pages * pages.n_kv_heads * 2 * pages.head_dim, bounds)
-    _check(load().sablock_compact_paged(ctypes.byref(shape), _ptr(k), _ptr(v), _ptr(idx), budget, 1 if append_window else 0, ctypes.byref(pages),
-                                        _ptr(page_table), _ptr(k_pool), _ptr(v_pool), _ptr(bounds), _ptr(lengths_out), _stream(stream)))
+    lib = load()
+    k_at, v_at, idx_at, table, kp, vp, b, lengths = _pointers(k, v, idx, page_table, k_pool, v_pool, bounds, lengths_out)
+    dtype, n_seq, problems, entries, n_bounds, _ = _cache_sizes(pages)
+    i32 = _torch.int32
+    _dense(i32, problems * budget, idx)
+    _dense(i32, entries, page_table)
+    _dense(i32, n_seq, lengths_out)
+    _dense(dtype, n_bounds, bounds)
+    _check(lib.sablock_compact_paged(ctypes.byref(shape), k_at, v_at, idx_at, budget, 1 if append_window else 0, ctypes.byref(pages), table, kp, vp,
+                                     b, lengths, _stream(stream)))
 
 
 def sablock_append_paged(pages: CPages, tokens: CNewTokens, k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q=None, q_out=None,
                          counts=None, bounds=None, stream=None):
     """``lengths`` are the rows of every sequence WITH the new tokens."""
-    import torch
-
-    _here(k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q, q_out, counts, bounds)
-    _dense(torch.int32, pages.n_seq, positions, lengths, counts)
-    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
-    _dense(torch.float32, tokens.rotary_dim // 2, inv_freq)
-    _dense(_cache_dtype(pages), pages.n_seq * pages.n_layers * pages.n_q_heads * tokens.n_new * pages.head_dim, q_out)
-    _dense(_cache_dtype(pages), pages.n_layers * pages.n_pages * pages.n_kv_heads * 2 * pages.head_dim, bounds)
+    lib = load()
+    k_at, v_at, pos, freq, table, rows, kp, vp, q_at, out, c, b = _pointers(k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q,
+                                                                            q_out, counts, bounds)
+    dtype, n_seq, _, entries, n_bounds, queries = _cache_sizes(pages)
+    i32 = _torch.int32
+    _dense(i32, n_seq, positions, lengths, counts)
+    _dense(i32, entries, page_table)
+    _dense(_torch.float32, tokens.rotary_dim // 2, inv_freq)
+    _dense(dtype, queries * tokens.n_new, q_out)
+    _dense(dtype, n_bounds, bounds)
     if not (k.dtype is v.dtype is k_pool.dtype and (q is None or q.dtype is k.dtype)):
         raise ValueError("q, k and v are of the cache's dtype")
-    _check(load().sablock_append_paged(ctypes.byref(pages), ctypes.byref(tokens), _ptr(q), _ptr(k), _ptr(v), _ptr(counts), _ptr(positions),
-                                       _ptr(inv_freq), _ptr(page_table), _ptr(lengths), _ptr(q_out), _ptr(k_pool), _ptr(v_pool), _ptr(bounds),
-                                       _stream(stream)))
+    _check(lib.sablock_append_paged(ctypes.byref(pages), ctypes.byref(tokens), q_at, k_at, v_at, c, pos, freq, table, rows, out, kp, vp, b,
+                                    _stream(stream)))
 
 
 def sablock_decode_paged_workspace_bytes(pages: CPages) -> int:
@@ -474,18 +485,18 @@ def sablock_decode_paged_workspace_bytes(pages: CPages) -> int:
 
 def sablock_decode_paged(pages: CPages, q, k_pool, v_pool, page_table, lengths, out, ws, page_list=None, stream=None):
     """``page_list [P, n]`` int32, dense: the pages to read (``sablock_select_pages``); None = all."""
-    import torch
-
-    _here(q, k_pool, v_pool, page_table, lengths, out, ws, page_list)
+    lib = load()
+    q_at, kp, vp, table, rows, o, ws_at, listed = _pointers(q, k_pool, v_pool, page_table, lengths, out, ws, page_list)
     n = 0 if page_list is None else page_list.shape[-1]
-    queries = pages.n_seq * pages.n_layers * pages.n_q_heads * pages.head_dim
-    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
-    _dense(torch.int32, pages.n_seq, lengths)
-    _dense(torch.int32, n_problems(pages) * n, page_list)
-    _dense(_cache_dtype(pages), queries, q)
-    _dense(torch.float32, queries, out)
-    _check(load().sablock_decode_paged(ctypes.byref(pages), _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(lengths),
-                                       _ptr(page_list), n, _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    dtype, n_seq, problems, entries, _, queries = _cache_sizes(pages)
+    i32 = _torch.int32
+    _dense(i32, entries, page_table)
+    _dense(i32, n_seq, lengths)
+    _dense(i32, problems * n, page_list)
+    _dense(dtype, queries, q)
+    _dense(_torch.float32, queries, out)
+    _check(lib.sablock_decode_paged(ctypes.byref(pages), q_at, kp, vp, table, rows, listed, n, o, ws_at, ws.numel() * ws.element_size(),
+                                    _stream(stream)))
 
 
 def sablock_select_pages_workspace_bytes(pages: CPages) -> int:
@@ -495,16 +506,17 @@ def sablock_select_pages_workspace_bytes(pages: CPages) -> int:
 
 
 def sablock_select_pages(pages: CPages, q, bounds, page_table, lengths, n_pick: int, list_out, ws, n_first: int = 1, n_last: int = 1, stream=None):
-    import torch
-
-    _here(q, bounds, page_table, lengths, list_out, ws)
-    _dense(torch.int32, pages.n_seq * pages.max_pages, page_table)
-    _dense(torch.int32, pages.n_seq, lengths)
-    _dense(torch.int32, n_problems(pages) * n_pick, list_out)
-    _dense(_cache_dtype(pages), pages.n_seq * pages.n_layers * pages.n_q_heads * pages.head_dim, q)
-    _dense(_cache_dtype(pages), pages.n_layers * pages.n_pages * pages.n_kv_heads * 2 * pages.head_dim, bounds)
-    _check(load().sablock_select_pages(ctypes.byref(pages), _ptr(q), _ptr(bounds), _ptr(page_table), _ptr(lengths), n_pick, n_first, n_last,
-                                       _ptr(list_out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    lib = load()
+    q_at, b, table, rows, listed, ws_at = _pointers(q, bounds, page_table, lengths, list_out, ws)
+    dtype, n_seq, problems, entries, n_bounds, queries = _cache_sizes(pages)
+    i32 = _torch.int32
+    _dense(i32, entries, page_table)
+    _dense(i32, n_seq, lengths)
+    _dense(i32, problems * n_pick, list_out)
+    _dense(dtype, queries, q)
+    _dense(dtype, n_bounds, bounds)
+    _check(lib.sablock_select_pages(ctypes.byref(pages), q_at, b, table, rows, n_pick, n_first, n_last, listed, ws_at,
+                                    ws.numel() * ws.element_size(), _stream(stream)))
 
 
 class PagedCache:

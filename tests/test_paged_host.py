@@ -180,20 +180,14 @@ def test_descriptors_from_tensors():
     assert (t.n_new, t.rotary_dim, t.interleaved) == (5, 64, 1) and list(t.q_stride) == [5 * 2 * 20 * 64, 20 * 64, 64, 2 * 20 * 64]
 
 
-def test_binding_refuses_tensors_that_the_kernels_could_not_follow():
+def test_binding_refuses_tensors_that_the_kernels_could_not_follow(lib):  # noqa: F811
     i32 = dict(dtype=torch.int32)
-    with pytest.raises(ValueError, match="on the host"):
-        B._here(None, torch.zeros(3))
     for bad in (torch.zeros(3), torch.zeros(3, dtype=torch.int64), torch.zeros(2, **i32), torch.zeros((3, 2), **i32)[:, 0], torch.zeros((2, 3), **i32).t()):
         with pytest.raises(ValueError, match="dense"):
             B._dense(torch.int32, 3, None, bad)
     B._dense(torch.int32, 3, None, torch.zeros(3, **i32), torch.zeros((2, 3), **i32))
     pages, k = _pages(), torch.zeros((1, 1, 2, 1, 64), dtype=torch.bfloat16)
-    with pytest.raises(ValueError, match="on the host"):       # every wrapper, before the library is asked
-        B.sablock_append_paged(pages, _tokens(), k, k, None, None, k, k, k, k)
-    with pytest.raises(ValueError, match="on the host"):
-        B.sablock_decode_paged(pages, k, k, k, k, k, k, k)
-    with pytest.raises(ValueError, match="on the host"):
-        B.sablock_select_pages(pages, k, k, k, k, 3, k, k)
-    with pytest.raises(ValueError, match="on the host"):
-        B.sablock_compact_paged(_shape(), k, k, k, 3, True, pages, k, k, k)
+    for call in (lambda: B.sablock_append_paged(pages, _tokens(), k, k, None, None, k, k, k, k), lambda: B.sablock_decode_paged(pages, k, k, k, k, k, k, k),
+                 lambda: B.sablock_select_pages(pages, k, k, k, k, 3, k, k), lambda: B.sablock_compact_paged(_shape(), k, k, k, 3, True, pages, k, k, k)):
+        with pytest.raises(ValueError, match="device memory"):  # before the library is asked
+            call()
