@@ -151,18 +151,12 @@ def _stream(stream) -> Optional[int]:
 def _pointers(*tensors):
     """Device pointers (None stays) of tensors that are all on the current device: another one's, or the host's, the kernels could not
     follow."""
-    at = tensors[0].get_device()
-    out = []
-    for t in tensors:
-        if t is None:
-            out.append(None)
-            continue
-        if t.get_device() != at or at < 0:
-            raise ValueError(f"tensors on {tensors[0].device} and {t.device}: the calls take device memory, of one device")
-        out.append(t.data_ptr())
-    if at != _torch.cuda.current_device():
-        raise ValueError(f"tensors on cuda:{at} while cuda:{_torch.cuda.current_device()} is the current device")
-    return out
+    at = {t.get_device() for t in tensors if t is not None}
+    if len(at) != 1 or -1 in at:
+        raise ValueError(f"tensors on {[str(t.device) for t in tensors if t is not None]}: the calls take device memory, of one device")
+    if at != {_torch.cuda.current_device()}:
+        raise ValueError(f"tensors on cuda:{at.pop()} while cuda:{_torch.cuda.current_device()} is the current device")
+    return [None if t is None else t.data_ptr() for t in tensors]
 
 
 def _dense(dtype, n: int, *tensors):

@@ -161,7 +161,7 @@ compact_paged_kernel(Dims d, PageDims pd, PageView pv, const char *k, const char
 
 constexpr int ANGLES = 4096;                   // (token, pair) whose sine and cosine LDS holds at a time
 constexpr int BATCH = 4;                       // rows of a thread in flight, twice
-constexpr int APPEND_WGS = 8;                  // workgroups per compute unit, if the head rows allow
+constexpr int APPEND_WGS = 12;                 // workgroups per compute unit, if the head rows allow
 
 struct AppendArgs {
     PageDims d;
@@ -172,21 +172,22 @@ struct AppendArgs {
     const float *inv_freq;
     char *q_out;
     int slots, per;             // head rows: K's heads, V's, q's; of a workgroup
-    int chunks, groups, side;   // 16-byte chunks of a row; rows and head rows that a workgroup does at a time
+    int chunks, lanes;          // 16-byte chunks of a row, the next power of two
+    int groups, side;           // rows and head rows that a workgroup does at a time
     int tile;                   // tokens whose angles LDS holds
 };
 
 // grid (touched pages, sequences x layers, parts of the head rows).  The angle of a (token, pair) is the same for all heads: formed
 // once per workgroup, position * inv_freq in whole turns in fp64 (at position 131 072 an angle in fp32 is off by up to 2^-8), the
-// fraction of a turn in fp32.  A thread has one chunk of every groups-th row of a head; half of a pair that lies in another chunk is read
-// as well, which the cache serves.  The rows of the next step are on their way while one is turned and stored, the first
+// fraction of a turn in fp32.  A thread has one chunk of every groups-th row of a head, a row's chunks lie in the lanes of one wavefront, where
+// the other halves of pairs come from.  The rows of the next step are on their way while one is turned and stored, the first
 // ones while the angles are formed.
 // ONE: a token per sequence, and a workgroup has no more head rows than it does at a time.  SPLIT: the two elements of a pair lie half a rotation
 // apart, in different chunks.
 // Loads of a step are issued whatever the lane has to do there (at the nearest place that exists): behind a branch the compiler could
 // not count the loads in flight and would wait for all of them.  A step whose rows all exist stores without a branch for the same reason.
 template <bool BF16, bool ONE, bool SPLIT>
-__global__ void __launch_bounds__(NT, ONE ? 4 : 3)
+__global__ void __launch_bounds__(NT, ONE || SPLIT ? 4 : 3)
 append_paged_kernel(AppendArgs a)
 {
     using E = Elem<BF16>;
@@ -206,21 +207,21 @@ append_paged_kernel(AppendArgs a)
     const int slot0 = id < 0 ? max((int)blockIdx.z * a.per, 2 * d.Hkv) : blockIdx.z * a.per, slot_end = min(a.slots, ((int)blockIdx.z + 1) * a.per);
     if (slot0 >= slot_end) return;
     const int half = a.t.R / 2, pair_chunks = half / E::N;
-    const int c = tid % a.chunks, place = tid / a.chunks, group = place % a.groups, lane_slot = place / a.groups;
-    const bool active = lane_slot < a.side;
+    const int c = tid & (a.lanes - 1), place = tid / a.lanes, group = place % a.groups, lane_slot = place / a.groups;
+    const bool active = lane_slot < a.side && c < a.chunks;
     const int64_t position0 = a.t.R ? (int64_t)a.positions[s] : 0;
     // this chunk's part in the rotation: where its angles lie, and the chunk of the other elements of its pairs
     const bool turned = c < 2 * pair_chunks, upper = SPLIT && turned && c >= pair_chunks;
     const int angle = SPLIT ? (upper ? c - pair_chunks : c) * E::N : c * (E::N / 2);
-    const int partner = !turned ? 0 : (upper ? -pair_chunks : pair_chunks) * 16;
+    const int partner = !turned ? tid : upper ? tid - pair_chunks : tid + pair_chunks;     // lane
 
-    struct Source { const char *at; int64_t step; bool is_v; };
+    struct Source { const char *at; int64_t step; };
     auto source = [&](int base) {
         const int slot = min(base + lane_slot, slot_end - 1);
         const bool is_k = slot < d.Hkv, is_v = !is_k && slot < 2 * d.Hkv;
         const int head = is_k ? slot : is_v ? slot - d.Hkv : slot - 2 * d.Hkv;
         const int64_t *st = is_k ? a.t.ks : is_v ? a.t.vs : a.t.qs;
-        return Source{(is_k ? a.k : is_v ? a.v : a.q) + (s * st[0] + layer * st[1] + head * st[2]) * E::BYTES + c * 16, st[3] * E::BYTES, is_v};
+        return Source{(is_k ? a.k : is_v ? a.v : a.q) + (s * st[0] + layer * st[1] + head * st[2]) * E::BYTES + min(c, a.chunks - 1) * 16, st[3] * E::BYTES};
     };
     // the thread's pair of the angles, which it forms for every angle_step-th token
     const int angle_step = half ? NT / half : 1, pair = half ? tid % half : 0, angle_tok = half ? tid / half : angle_step;
@@ -228,18 +229,14 @@ append_paged_kernel(AppendArgs a)
     if (angle_tok < angle_step) turns_per = (double)a.inv_freq[pair] * 0.15915494309189535;
     for (int t0 = begin; t0 < end; t0 += a.tile) {
         const int n = min(a.tile, end - t0), rows = B * a.groups, batches = (n + rows - 1) / rows;
-        u32x4 x[B], o[SPLIT ? B : 1];
-        auto load = [&](int base, int b, u32x4 (&x)[B], u32x4 (&o)[SPLIT ? B : 1]) {
+        u32x4 x[B];
+        auto load = [&](int base, int b, u32x4 (&x)[B]) {
             const Source r = source(base);
             const char *from = r.at + (t0 - first) * r.step;
 #pragma unroll
-            for (int i = 0; i < B; ++i) {
-                const char *p = from + min(group + (b * B + i) * a.groups, n - 1) * r.step;
-                x[i] = *reinterpret_cast<const u32x4 *>(p);
-                if constexpr (SPLIT) o[i] = *reinterpret_cast<const u32x4 *>(p + (r.is_v ? 0 : partner));
-            }
+            for (int i = 0; i < B; ++i) x[i] = *reinterpret_cast<const u32x4 *>(from + min(group + (b * B + i) * a.groups, n - 1) * r.step);
         };
-        load(slot0, 0, x, o);
+        load(slot0, 0, x);
         if (a.t.R) {
             if (t0 > begin) __syncthreads();
             if (angle_tok < angle_step)
@@ -256,8 +253,8 @@ append_paged_kernel(AppendArgs a)
         for (int base = slot0, bt = 0;;) {
             const bool slot_done = bt + 1 == batches;
             const int next_base = slot_done ? base + a.side : base, next_bt = slot_done ? 0 : bt + 1;
-            u32x4 xn[B], on[SPLIT ? B : 1];
-            if constexpr (!ONE) load(next_base, next_bt, xn, on);              // behind the last: the last again
+            u32x4 xn[B];
+            if constexpr (!ONE) load(next_base, next_bt, xn);  // behind the last: the last again
             const int slot = base + lane_slot;
             const bool is_k = slot < d.Hkv, is_v = !is_k && slot < 2 * d.Hkv, live = active && slot < slot_end;
             const int head = is_k ? slot : is_v ? slot - d.Hkv : slot - 2 * d.Hkv;
@@ -272,7 +269,11 @@ append_paged_kernel(AppendArgs a)
                 dst = a.q_out + ((((int64_t)s * d.n_layers + layer) * d.Hq + head) * a.t.n_new + t0 - first) * step + c * 16;
             }
             auto turn_row = [&](int i) {
-                u32x4 w = x[i];
+                u32x4 w = x[i], o{0, 0, 0, 0};
+                if constexpr (SPLIT) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = (uint32_t)__shfl((int)w[e], partner);
+                }
                 if (!turned || is_v) return w;
                 float y[E::N];
                 const float4 *angles = reinterpret_cast<const float4 *>(turn + min(group + (bt * B + i) * a.groups, n - 1) * half + angle);
@@ -280,7 +281,7 @@ append_paged_kernel(AppendArgs a)
 #pragma unroll
                     for (int e = 0; e < E::N; e += 2) {
                         const float4 t = angles[e / 2];
-                        const float z0 = E::get(o[i], e), z1 = E::get(o[i], e + 1);
+                        const float z0 = E::get(o, e), z1 = E::get(o, e + 1);
                         y[e] = E::get(w, e) * t.x + (upper ? z0 : -z0) * t.y;
                         y[e + 1] = E::get(w, e + 1) * t.z + (upper ? z1 : -z1) * t.w;
                     }
@@ -297,7 +298,7 @@ append_paged_kernel(AppendArgs a)
                 }
                 return E::pack(y);
             };
-            if (!ONE && a.side == 1 && a.chunks * a.groups == NT && (bt + 1) * rows <= n) {
+            if (!ONE && a.side * a.chunks * a.groups == NT && base + a.side <= slot_end && (bt + 1) * rows <= n) {
 #pragma unroll
                 for (int i = 0; i < B; ++i) {
                     x[i] = turn_row(i);
@@ -337,10 +338,7 @@ append_paged_kernel(AppendArgs a)
             if constexpr (ONE) break;
             if (next_base >= slot_end) break;
 #pragma unroll
-            for (int i = 0; i < B; ++i) {
-                x[i] = xn[i];
-                if constexpr (SPLIT) o[i] = on[i];
-            }
+            for (int i = 0; i < B; ++i) x[i] = xn[i];
             base = next_base;
             bt = next_bt;
         }
@@ -374,8 +372,10 @@ hipError_t launch_append_paged(const PageDims &pd, const TokenDims &td, const vo
     a.inv_freq = inv_freq;
     a.q_out = static_cast<char *>(q_out);
     a.chunks = pd.D * elt_bytes(pd) / 16;
-    a.groups = std::min(std::min(td.n_new, pd.page), NT / a.chunks);
-    a.side = NT / (a.chunks * a.groups);
+    a.lanes = 1;
+    while (a.lanes < a.chunks) a.lanes *= 2;
+    a.groups = std::min(std::min(td.n_new, pd.page / BATCH), NT / a.lanes);    // BATCH rows per thread in a whole page
+    a.side = NT / (a.lanes * a.groups);
     a.tile = td.R ? std::min(pd.page, ANGLES / (td.R / 2)) : pd.page;
     a.slots = 2 * pd.Hkv + (q ? pd.Hq : 0);
     const int64_t pages = (td.n_new + (int64_t)pd.page - 2) / pd.page + 1, units = pages * pd.n_seq * pd.n_layers;
