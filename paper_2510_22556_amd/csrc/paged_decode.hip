@@ -35,6 +35,7 @@ constexpr int LEAST_STEPS = 4;                 // of a workgroup's run: one per 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 template <int N> struct Words;                 // N dwords of a row that begin on any dword
 template <> struct Words<1> { typedef uint32_t T __attribute__((aligned(4))); };
 template <> struct Words<2> { typedef uint32_t T __attribute__((ext_vector_type(2), aligned(4))); };
@@ -56,6 +57,12 @@ __device__ __forceinline__ void load_words(uint32_t *w, const char *p)
         for (int i = 0; i < N; ++i) w[i] = v[i];
     }
 }
+
+// Rows of a step.  bf16 takes 32, but 16 of rows of more than 256 bytes, so that what is in flight leaves room for a second workgroup on
+// the compute unit (heads of 256, 4 x 65 536 rows: 399 -> 382 us), and 16 of rows of more than 128 bytes where every problem is one
+// workgroup's: a third one fits, and there the latencies of many short ones count (heads of 128: 1 024 problems of up to
+// 256 rows 23.7 -> 20.6 us, 64 of 512 rows 12.3 -> 11.0; heads of 64, 64 problems of 512 rows: 7.3 -> 8.3; shared, 4 x 131 072 rows: 345 -> 349).
+constexpr int step_rows(bool bf16, int D, bool alone) { return bf16 && D <= 128 && !(alone && D > 64) ? 32 : 16; }
 
 struct DecodePagedArgs {
     PageDims d;
@@ -172,12 +179,12 @@ __device__ __forceinline__ float over_quarters(float x, bool take_max)        //
 }
 
 // EP: elements of a row per lane in the second product, D / 16
-template <bool BF16, int EP>
+template <bool BF16, int EP, int STEP>
 __global__ void __launch_bounds__(NT)
 decode_paged_kernel(DecodePagedArgs a)
 {
-    constexpr int D = EP * 16, ELT = BF16 ? 2 : 4, STEP = BF16 ? 32 : 16, R = STEP / 4;      // R: rows per lane in the second product
-    constexpr int KT = BF16 ? 2 : 1;                           // products of 16 rows per step
+    constexpr int D = EP * 16, ELT = BF16 ? 2 : 4, R = STEP / 4;            // R: rows per lane in the second product
+    constexpr int KT = STEP / 16;                              // products of 16 rows per step
     constexpr int KC = D * ELT / 64;                           // 16-byte pieces of a row per lane in the first product
     constexpr int VW = EP * ELT / 4;                           // dwords of a row per lane in the second
     constexpr int KEEP = D / 4 + 2;                            // registers of a lane that wavefronts join
@@ -186,7 +193,7 @@ decode_paged_kernel(DecodePagedArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, c = lane >> 4;
     // a lane's rows of a step: of K as operand (bf16: and that row + 4), of the results and of V from `row` on
-    const int krow = BF16 ? (m >> 2) * 8 + (m & 3) : m, row = R * c;
+    const int krow = KT == 2 ? (m >> 2) * 8 + (m & 3) : m, row = R * c;
     const int64_t kstep = d.ks[3] * ELT, vstep = d.vs[3] * ELT;
 
     // a piece: steps off .. off + count of the n of problem p
@@ -231,7 +238,7 @@ decode_paged_kernel(DecodePagedArgs a)
             int idk = __builtin_amdgcn_readlane(ids, at), idv = idk, n_held = __builtin_amdgcn_readlane(held, at);
             int rk = in_page + krow, rv = in_page + row;
             whole = in_page + STEP <= n_held;
-            if (BF16 && d.shift == 4) {                        // two pages; a lane's rows lie in one of them
+            if (KT == 2 && d.shift == 4) {                      // two pages; a lane's rows lie in one of them
                 const int id1 = __builtin_amdgcn_readlane(ids, at + 1), held1 = __builtin_amdgcn_readlane(held, at + 1);
                 whole = n_held == 16 && held1 == 16;
                 idk = krow < 16 ? idk : id1;
@@ -280,8 +287,12 @@ decode_paged_kernel(DecodePagedArgs a)
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[4 * t + i] = r[i];
+                for (int i = 0; i < 4; ++i) z[4 * t + i] = r[i] * a.qscale;
             }
+            // The products' results are read here, before any branch: the compiler puts the wait states between a product and the
+            // first read of its result, but where a branch came in between it was found to leave some out, and old values were read.
+#pragma unroll
+            for (int i = 0; i < R; ++i) asm volatile("" : "+v"(z[i]));
             const bool now_whole = whole;
             const int now_limit = limit;
             if constexpr (more.value) {
@@ -300,7 +311,6 @@ decode_paged_kernel(DecodePagedArgs a)
             float most = z[0];
 #pragma unroll
             for (int i = 1; i < R; ++i) most = fmaxf(most, z[i]);
-            most *= a.qscale;
             if (__ballot(most > ref) != 0ull) {
                 const float top = over_quarters(most, true), to_ref = top > ref ? top + AHEAD : ref;
                 const float f = __builtin_amdgcn_exp2f(ref - to_ref);
@@ -311,13 +321,14 @@ decode_paged_kernel(DecodePagedArgs a)
             }
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                z[i] = __builtin_amdgcn_exp2f(fmaf(z[i], a.qscale, -ref));
+                z[i] = __builtin_amdgcn_exp2f(z[i] - ref);
                 den += z[i];
             }
             if constexpr (BF16) {
-                u32x4 part[3];
+                typedef uint32_t Operand __attribute__((ext_vector_type(R / 2)));
+                Operand part[3];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < R / 2; ++i) {
                     uint32_t lo = __float_as_uint(z[2 * i]), hi = __float_as_uint(z[2 * i + 1]);
 #pragma unroll
                     for (int t = 0; t < 3; ++t) {
@@ -328,13 +339,17 @@ decode_paged_kernel(DecodePagedArgs a)
                 }
 #pragma unroll
                 for (int e = 0; e < EP; ++e) {
-                    u32x4 o;
+                    Operand o;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < R / 2; ++i)
                         o[i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], e % 2 ? 0x07060302 : 0x05040100);
 #pragma unroll
-                    for (int t = 2; t >= 0; --t)
-                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part[t]), acc[e], 0, 0, 0);
+                    for (int t = 2; t >= 0; --t) {
+                        if constexpr (R == 8)
+                            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part[t]), acc[e], 0, 0, 0);
+                        else
+                            acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, o), __builtin_bit_cast(s16x4, part[t]), acc[e], 0, 0, 0);
+                    }
                 }
             } else {
 #pragma unroll
@@ -495,7 +510,8 @@ decode_paged_merge_kernel(DecodePagedArgs a)
 // workgroups per compute unit that the registers leave room for
 int resident(const PageDims &d)
 {
-    return d.D <= 96 ? 3 : d.D <= 192 ? 2 : 1;
+    if (d.dtype == SABLOCK_BF16) return d.D <= 64 ? 3 : 2;
+    return d.D <= 80 ? 3 : d.D <= 160 ? 2 : 1;
 }
 int workgroups_of(const PageDims &d) { return std::min(d.cus * resident(d), MAX_PIECES - 1); }
 // rows of the longest problem that a workgroup takes alone
@@ -523,23 +539,26 @@ hipError_t launch_decode_paged(const PageDims &d, const void *q, const PageView 
     a.qscale = (float)(1.4426950408889634 / sqrt((double)d.D));
     a.out = out;
     const int64_t capacity = (int64_t)(list ? std::min(n_listed, d.max_pages) : d.max_pages) * d.page;
-    const int workgroups = workgroups_of(d), step = d.dtype == SABLOCK_BF16 ? 32 : 16;
-    a.limit = rows_alone(d) / step;
-    a.workgroups = capacity > (int64_t)a.limit * step ? workgroups : 0;        // no problem can be longer: all are taken alone
+    const bool bf = d.dtype == SABLOCK_BF16, alone = capacity <= rows_alone(d);               // no problem can be longer
+    const int workgroups = workgroups_of(d), step = step_rows(bf, d.D, alone);
+    a.limit = (rows_alone(d) + step - 1) / step;
+    a.workgroups = alone ? 0 : workgroups;
     a.weights = static_cast<float *>(ws);
     a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups * d.G * 8));
-    const bool bf = d.dtype == SABLOCK_BF16;
     using Kern = void (*)(DecodePagedArgs);
     Kern fn = nullptr;
-#define SABLOCK_PAGED_F(EV) if (!bf && d.D == EV * 16) fn = decode_paged_kernel<false, EV>;
-#define SABLOCK_PAGED_B(EV) if (bf && d.D == EV * 16) fn = decode_paged_kernel<true, EV>; SABLOCK_PAGED_F(EV)
+#define SABLOCK_PAGED_F(EV) if (!bf && d.D == EV * 16) fn = decode_paged_kernel<false, EV, 16>;
+#define SABLOCK_PAGED_B(EV)                                                                                              \
+    if (bf && d.D == EV * 16)                                                                                             \
+        fn = alone ? decode_paged_kernel<true, EV, step_rows(true, EV * 16, true)> : decode_paged_kernel<true, EV, step_rows(true, EV * 16, false)>; \
+    SABLOCK_PAGED_F(EV)
     SABLOCK_PAGED_F(1) SABLOCK_PAGED_B(2) SABLOCK_PAGED_F(3) SABLOCK_PAGED_B(4) SABLOCK_PAGED_F(5) SABLOCK_PAGED_B(6) SABLOCK_PAGED_F(7) SABLOCK_PAGED_B(8)
     SABLOCK_PAGED_F(9) SABLOCK_PAGED_B(10) SABLOCK_PAGED_F(11) SABLOCK_PAGED_B(12) SABLOCK_PAGED_F(13) SABLOCK_PAGED_B(14) SABLOCK_PAGED_F(15) SABLOCK_PAGED_B(16)
 #undef SABLOCK_PAGED_B
 #undef SABLOCK_PAGED_F
     if (!fn) return hipErrorInvalidValue;
     hipLaunchKernelGGL(fn, dim3(a.workgroups + d.P), dim3(NT), 0, st, a);
-    if (a.workgroups) hipLaunchKernelGGL(bf ? decode_paged_merge_kernel<32> : decode_paged_merge_kernel<16>, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
+    if (a.workgroups) hipLaunchKernelGGL(step == 32 ? decode_paged_merge_kernel<32> : decode_paged_merge_kernel<16>, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
     return hipGetLastError();
 }
 
