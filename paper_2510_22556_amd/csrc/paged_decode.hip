@@ -159,6 +159,8 @@ struct Places {
         steps = shared_steps_of<STEP>(a, seq);
     }
 };
+// a number that is the same in all lanes, for the scalar registers: what comes from memory or another lane is not known to be
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // x / n of whole numbers; 64 bits are a hundred instructions, and hardly ever needed
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t n)
 {
@@ -199,6 +201,7 @@ decode_paged_kernel(DecodePagedArgs a)
     // a piece: steps off .. off + count of the n of problem p
     auto piece = [&](int p, int s, int off, int count, int n) __attribute__((always_inline)) {
         const int layer = layer_of_problem(d, p), head = head_of_problem(d, p);
+        // not made uniform: with the length in a scalar register the compiler's order of the loop is 2 % slower
         const int len = rows_of(d, a.pv.lengths, s), pages = (len + d.page - 1) >> d.shift;
         const int entries = a.list ? min(a.n_listed, pages) : pages;
         const int64_t qrow = (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G) * D;
@@ -418,7 +421,7 @@ decode_paged_kernel(DecodePagedArgs a)
         }
     };
     if ((int)blockIdx.x < a.d.P) {
-        const int p = blockIdx.x, s = seq_of_problem(d, p), n = steps_of<STEP>(a, s);
+        const int p = blockIdx.x, s = seq_of_problem(d, p), n = uniform(steps_of<STEP>(a, s));
         if (n <= a.limit) piece(p, s, 0, n, n);
         return;
     }
@@ -431,13 +434,13 @@ decode_paged_kernel(DecodePagedArgs a)
         if (x >= seq_to) {
             int64_t before;
             places.find(x, s, before, n);
-            s = __builtin_amdgcn_readfirstlane(s);
-            n = __builtin_amdgcn_readfirstlane(n);
+            s = uniform(s);
+            n = uniform(n);
             seq_from = before * places.heads;
             seq_to = seq_from + (int64_t)n * places.heads;
         }
-        const int problem = __builtin_amdgcn_readfirstlane((int)quotient(x - seq_from, n));
-        const int off = __builtin_amdgcn_readfirstlane((int)(x - seq_from - (int64_t)problem * n)), count = (int)min((int64_t)(n - off), run_to - x);
+        const int problem = uniform((int)quotient(x - seq_from, n)), off = uniform((int)(x - seq_from - (int64_t)problem * n));
+        const int count = uniform((int)min((int64_t)(n - off), run_to - x));
         piece(s * places.heads + problem, s, off, count, n);
         x += count;
     }

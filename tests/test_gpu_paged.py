@@ -292,6 +292,26 @@ def test_decode_groups_heads_pages_and_lengths(torch_cuda, G, D, dtype, page, le
     _check_decode(c, c.normal((c.n, 2, 2 * G, D)))
 
 
+@pytest.mark.parametrize("D,dtype,page,n,most", [(128, "bf16", 16, 150, 90), (128, "bf16", 32, 150, 1500), (64, "f32", 16, 70, 900), (256, "bf16", 16, 300, 700), (32, "bf16", 16, 4096, 40)])
+def test_decode_many_sequences(torch_cuda, D, dtype, page, n, most):  # noqa: F811
+    # more sequences than lanes, empty ones among them, first and last; most short, some longer than a workgroup takes alone
+    torch = torch_cuda
+    rng = np.random.default_rng(n + most)
+    lengths = [0 if rng.random() < 0.15 else int(rng.integers(1, most if rng.random() < 0.2 else 50)) for _ in range(n)]
+    lengths[0] = lengths[-1] = 0
+    lengths[n // 2] = 5 * most
+    c = Cache(torch, n, lengths, heads=1 if n > 1000 else 3, group=2, D=D, dtype=dtype, page=page, k_axes=(0, 2, 1, 3))
+    # one fill for all pages: the rows behind the sequences' ends are then ordinary numbers, garbage is the other tests'
+    c.k_pool.copy_(c.normal(c.k_pool.shape))
+    c.v_pool.copy_(c.normal(c.v_pool.shape))
+    q = c.normal((n, 1, 2 * c.H, D))
+    got, ref = c.decode(q).double().cpu(), _ref_decode(c, q)
+    assert bool(((got - ref).abs() <= 2.0 ** -16 * 6).all())
+    lst = torch.randint(0, 12, (n * c.H, 6), generator=c.gen, device="cuda", dtype=torch.int32)
+    got, ref = c.decode(q, lst).double().cpu(), _ref_decode(c, q, lst.cpu())
+    assert bool(((got - ref).abs() <= 2.0 ** -16 * 6).all())
+
+
 @pytest.mark.parametrize("G,D,dtype,page", [(4, 128, "bf16", 16), (7, 64, "bf16", 128), (16, 256, "bf16", 32), (3, 64, "f32", 16), (8, 256, "f32", 64)])
 def test_decode_counts_every_row_once(torch_cuda, G, D, dtype, page):  # noqa: F811
     # equal logits: the mean of V.  V[r] = 1 in column r % D and 0 elsewhere, so a row that is lost, comes twice, or is not the
