@@ -73,6 +73,7 @@ struct DecodePagedArgs {
     float qscale;                // log2(e) / sqrt(D)
     int workgroups;              // that share the long problems' steps
     int limit;                   // steps of the longest problem that a workgroup takes alone
+    bool narrow;                 // 32 bits hold all sequences' steps
     float *out;                  // [n_seq][n_layers][Hq][D]
     float *weights;              // pieces [2 * workgroups][G][2]: reference (log2 domain), denominator
     float *sums;                 // pieces [2 * workgroups][G][D]
@@ -98,9 +99,28 @@ __device__ __forceinline__ int shared_steps_of(const DecodePagedArgs &a, int s)
     return n > a.limit ? n : 0;
 }
 
-// Inclusive sum over the lanes.
-__device__ __forceinline__ int64_t scan(int64_t x, int lane)
+// a number that is the same in all lanes, for the scalar registers: what comes from memory or another lane is not known to be
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// the value of one lane, the same one for all
+__device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ int64_t of_lane(int64_t x, int lane)
 {
+    return (int64_t)((uint64_t)(uint32_t)of_lane((int)(x >> 32), lane) << 32 | (uint32_t)of_lane((int)x, lane));
+}
+// inclusive sums over the lanes: in 32 bits by lane shifts inside a row of 16 and the rows' ends into the next ones
+__device__ __forceinline__ int scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+__device__ __forceinline__ int64_t scan(int64_t x, int lane, bool narrow)
+{
+    if (narrow) return scan((int)x);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int64_t u = __shfl_up(x, o);
@@ -127,40 +147,38 @@ struct Places {
         int64_t sum = 0;
         for (int i = 0; i < share; ++i)
             if (lane * share + i < a.d.n_seq) sum += shared_steps_of<STEP>(a, lane * share + i);
-        upto = scan(sum, lane);
-        total = __shfl(upto, 63) * heads;
+        upto = scan(sum, lane, a.narrow);
+        total = of_lane(upto, 63) * heads;
     }
     // the sequence that step x of all lies in (x < total), the steps of one problem of those before it, and of its own
     __device__ void find(int64_t x, int &seq, int64_t &before, int &steps) const
     {
         if (a.d.n_seq == 1) { seq = 0; before = 0; steps = (int)upto; return; }
-        int first = __ffsll((unsigned long long)__ballot(upto * heads > x)) - 1;
-        int64_t at = first > 0 ? __shfl(upto, first - 1) : 0;
+        const int first = uniform(__ffsll((unsigned long long)__ballot(upto * heads > x)) - 1);
+        const int64_t at = first > 0 ? of_lane(upto, first - 1) : 0;
         if (share == 1) {
             seq = first;
             before = at;
-            steps = (int)(__shfl(upto, first) - at);
+            steps = (int)(of_lane(upto, first) - at);
             return;
         }
         const int s = first * share + lane;
         const int own = lane < share && s < a.d.n_seq ? shared_steps_of<STEP>(a, s) : 0;
-        const int64_t inner = scan((int64_t)own, lane) + at;
-        const int j = __ffsll((unsigned long long)__ballot(inner * heads > x)) - 1;
+        const int64_t inner = scan((int64_t)own, lane, a.narrow) + at;
+        const int j = uniform(__ffsll((unsigned long long)__ballot(inner * heads > x)) - 1);
         seq = first * share + j;
-        steps = __shfl(own, j);
-        before = __shfl(inner, j) - steps;
+        steps = of_lane(own, j);
+        before = of_lane(inner, j) - steps;
     }
     // the same for a given sequence
     __device__ void of(int seq, int64_t &before, int &steps) const
     {
-        const int first = seq / share;
-        before = first > 0 ? __shfl(upto, first - 1) : 0;
+        const int first = uniform(seq / share);
+        before = first > 0 ? of_lane(upto, first - 1) : 0;
         for (int s = first * share; s < seq; ++s) before += shared_steps_of<STEP>(a, s);
         steps = shared_steps_of<STEP>(a, seq);
     }
 };
-// a number that is the same in all lanes, for the scalar registers: what comes from memory or another lane is not known to be
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // x / n of whole numbers; 64 bits are a hundred instructions, and hardly ever needed
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t n)
 {
@@ -434,8 +452,6 @@ decode_paged_kernel(DecodePagedArgs a)
         if (x >= seq_to) {
             int64_t before;
             places.find(x, s, before, n);
-            s = uniform(s);
-            n = uniform(n);
             seq_from = before * places.heads;
             seq_to = seq_from + (int64_t)n * places.heads;
         }
@@ -546,6 +562,7 @@ hipError_t launch_decode_paged(const PageDims &d, const void *q, const PageView 
     const int workgroups = workgroups_of(d), step = step_rows(bf, d.D, alone);
     a.limit = (rows_alone(d) + step - 1) / step;
     a.workgroups = alone ? 0 : workgroups;
+    a.narrow = d.n_seq * (capacity / step + 1) < INT32_MAX;
     a.weights = static_cast<float *>(ws);
     a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups * d.G * 8));
     using Kern = void (*)(DecodePagedArgs);

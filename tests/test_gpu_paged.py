@@ -312,6 +312,18 @@ def test_decode_many_sequences(torch_cuda, D, dtype, page, n, most):  # noqa: F8
     assert bool(((got - ref).abs() <= 2.0 ** -16 * 6).all())
 
 
+def test_decode_tables_for_more_steps_than_32_bits_count(torch_cuda):  # noqa: F811
+    # 40 sequences with room for 2^30 rows each: their steps are summed in 64 bits
+    torch = torch_cuda
+    c = Cache(torch, 3, [3000 if s % 7 == 3 else s * 11 for s in range(40)], heads=1, group=2, D=16, dtype="f32", page=256).fill()
+    q = c.normal((40, 1, 2, 16))
+    ref = _ref_decode(c, q)
+    wide = torch.full((40, 1 << 22), -1, dtype=torch.int32, device="cuda")
+    wide[:, : c.width] = c.table
+    c.table, c.pages = wide, c.B.make_pages(c.k_pool, c.v_pool, wide, 2)
+    assert bool(((c.decode(q).double().cpu() - ref).abs() <= 2.0 ** -16 * 6).all())
+
+
 @pytest.mark.parametrize("G,D,dtype,page", [(4, 128, "bf16", 16), (7, 64, "bf16", 128), (16, 256, "bf16", 32), (3, 64, "f32", 16), (8, 256, "f32", 64)])
 def test_decode_counts_every_row_once(torch_cuda, G, D, dtype, page):  # noqa: F811
     # equal logits: the mean of V.  V[r] = 1 in column r % D and 0 elsewhere, so a row that is lost, comes twice, or is not the
