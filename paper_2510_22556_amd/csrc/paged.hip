@@ -380,8 +380,8 @@ hipError_t launch_append_paged(const PageDims &pd, const TokenDims &td, const vo
     a.slots = 2 * pd.Hkv + (q ? pd.Hq : 0);
     const int64_t pages = (td.n_new + (int64_t)pd.page - 2) / pd.page + 1, units = pages * pd.n_seq * pd.n_layers;
     const int steps = (a.slots + a.side - 1) / a.side;         // of a workgroup that had them all
-    const bool one = td.n_new == 1, bf = pd.dtype == SABLOCK_BF16;
-    const int parts = one ? steps : (int)std::max<int64_t>(1, std::min<int64_t>(steps, APPEND_WGS * pd.cus / units));
+    const bool one = td.n_new == 1 && steps <= (int)GRID_Y_MOST, bf = pd.dtype == SABLOCK_BF16;               // a grid's third axis has as many places
+    const int parts = one ? steps : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(steps, (int)GRID_Y_MOST), APPEND_WGS * pd.cus / units));
     a.per = (steps + parts - 1) / parts * a.side;
     const dim3 grid((unsigned)pages, pd.n_seq * pd.n_layers, (a.slots + a.per - 1) / a.per);
     const bool split = td.R > 0 && !td.interleaved;

@@ -18,8 +18,9 @@
 //     v_perm_b32 for two rows.  Product e then gives the elements D / 16 (lane & 15) + e.
 // Everything about a head, logits, reference, denominator and numerators, is in the lanes of its column: no exchange but a
 // maximum over four lanes where a reference moves.  References are set AHEAD (log2 domain) above the largest logit so far and move when
-// a logit passes them.  bf16 probabilities enter the second product in three parts of 8 bits, exactly: the result is as
-// good as in fp32 (rounded to bf16 they would be off by 2^-9), and the matrix pipe has the time.
+// a logit passes them.  bf16 probabilities enter the second product in three parts of 8 bits (each part but the first 2^-28 of the
+// whole too large, so that none is zero): the result is as good as in fp32 (rounded to bf16 they would be off by
+// 2^-9), and the matrix pipe has the time.
 #include "sablock_internal.h"
 
 #include <cfloat>
@@ -30,6 +31,7 @@ namespace {
 
 constexpr int NW = 4, NT = NW * 64;
 constexpr float AHEAD = 8.f;
+constexpr float PART_LEAST = 0x1p-28f;         // a part of a probability that would be zero times an infinite value would be no number
 constexpr int LEAST_STEPS = 4;                 // of a workgroup's run: one per wavefront
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -145,8 +147,11 @@ struct Places {
             return;
         }
         int64_t sum = 0;
-        for (int i = 0; i < share; ++i)
-            if (lane * share + i < a.d.n_seq) sum += shared_steps_of<STEP>(a, lane * share + i);
+#pragma unroll 8
+        for (int i = 0; i < share; ++i) {                      // loads without a branch, several at a time
+            const int s = lane * share + i, n = shared_steps_of<STEP>(a, min(s, a.d.n_seq - 1));
+            sum += s < a.d.n_seq ? n : 0;
+        }
         upto = scan(sum, lane, a.narrow);
         total = of_lane(upto, 63) * heads;
     }
@@ -350,12 +355,12 @@ decode_paged_kernel(DecodePagedArgs a)
                 Operand part[3];
 #pragma unroll
                 for (int i = 0; i < R / 2; ++i) {
-                    uint32_t lo = __float_as_uint(z[2 * i]), hi = __float_as_uint(z[2 * i + 1]);
+                    float lo = z[2 * i], hi = z[2 * i + 1];
 #pragma unroll
                     for (int t = 0; t < 3; ++t) {
-                        part[t][i] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
-                        lo = __float_as_uint(__uint_as_float(lo) - __uint_as_float(lo & 0xffff0000u));
-                        hi = __float_as_uint(__uint_as_float(hi) - __uint_as_float(hi & 0xffff0000u));
+                        part[t][i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+                        lo = fmaf(z[2 * i], PART_LEAST, lo - __uint_as_float(__float_as_uint(lo) & 0xffff0000u));
+                        hi = fmaf(z[2 * i + 1], PART_LEAST, hi - __uint_as_float(__float_as_uint(hi) & 0xffff0000u));
                     }
                 }
 #pragma unroll

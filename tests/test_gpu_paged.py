@@ -360,6 +360,17 @@ def test_decode_logits_that_rise_late_and_values_near_the_ends(torch_cuda, dtype
     assert bool(((got - ref).abs() <= 2.0 ** -15 * most).all())         # logits up to 2^8.8 in the log2 domain: 2^-16 in a share
 
 
+def test_append_of_more_heads_than_a_grid_has_places(torch_cuda):  # noqa: F811
+    # one token of 60 000 KV heads and 960 000 query heads
+    torch = torch_cuda
+    c = Cache(torch, 4, [3], heads=60000, group=16, D=8, dtype="f32")
+    k, v, q = c.normal((1, 1, 60000, 1, 8)), c.normal((1, 1, 60000, 1, 8)), c.normal((1, 1, 960000, 1, 8))
+    q_out = torch.empty_like(q)
+    c.B.sablock_append_paged(c.pages, c.B.make_new_tokens(k, v, q, rotary_dim=0), k, v, None, None, c.table, c.lengths, c.k_pool, c.v_pool, q=q, q_out=q_out)
+    at = int(c.table[0, 0])
+    assert torch.equal(q_out, q) and torch.equal(c.k_pool[0, at, :, 2], k[0, 0, :, 0]) and torch.equal(c.v_pool[0, at, :, 2], v[0, 0, :, 0])
+
+
 @pytest.mark.parametrize("dtype,at", [("bf16", 0), ("bf16", 99), ("f32", 50)])
 def test_decode_a_row_that_is_not_a_number_stays_with_its_head(torch_cuda, dtype, at):  # noqa: F811
     torch = torch_cuda
@@ -370,6 +381,22 @@ def test_decode_a_row_that_is_not_a_number_stays_with_its_head(torch_cuda, dtype
     got = c.decode(q)
     assert bool(torch.isnan(got[1, 0, 2:]).all())
     got[1, 0, 2:] = clean[1, 0, 2:]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [20, 3000])
+def test_decode_an_infinite_value_stays_infinite(torch_cuda, dtype, rows):  # noqa: F811
+    # in its column, for every head; also where the row's probability is a power of two, whose lower bits are zeros
+    torch = torch_cuda
+    c = Cache(torch, 4, [rows, rows], heads=2, group=3, D=64, dtype=dtype).fill()
+    q = c.normal((2, 1, 6, 64))
+    q[0, 0, 1] = 0.0
+    clean = c.decode(q)
+    c.v_pool[0, int(c.table[0, 0]), 0, 7, 3], c.v_pool[0, int(c.table[0, 1]), 0, 1, 60] = float("inf"), float("-inf")
+    got = c.decode(q)
+    assert bool((got[0, 0, :3, 3] == float("inf")).all()) and bool((got[0, 0, :3, 60] == float("-inf")).all())
+    got[0, 0, :3, 3], got[0, 0, :3, 60] = clean[0, 0, :3, 3], clean[0, 0, :3, 60]
     assert torch.equal(got, clean)
 
 
