@@ -1,11 +1,13 @@
 // Decode-time attention of one new token per sequence over a paged cache (Sec. 2.1 Eq. 1 for a single query position), over all
 // of a sequence's pages or over listed ones.
 //
-//   decode_paged_kernel   Work is counted in steps of 32 rows (bf16) or 16 (fp32), all problems' one behind the other; every workgroup
-//       takes an equal run of them, whatever the sequences' lengths, which only the device knows.  A run covers pieces of one or
-//       several problems; a problem that lies in one run is finished there, of a problem's piece (reference, denominator,
-//       numerators) go to the workspace, at most two per workgroup.
-//   decode_paged_merge_kernel   joins the pieces of each problem, and gives zeros to those without rows.
+//   decode_paged_kernel   Work is counted in steps of 32 or 16 rows.  A short problem (a sequence's KV head in a layer) is one
+//       workgroup's, which finishes it; the first n_seq * n_layers * Hkv workgroups see to those, and write zeros where there is no row.  The
+//       steps of the long ones are counted one behind the other and dealt out in equal runs to as many workgroups as reside at a
+//       time: the lengths, which only the device knows, do not matter.  A run covers pieces of one or several problems; a
+//       problem inside one run is finished there, of another's piece (reference, denominator, numerators) go to the workspace,
+//       at most two per workgroup.
+//   decode_paged_merge_kernel   joins the pieces of each problem.  Not launched where no sequence has room to be long.
 //
 // A wavefront does a step alone, on matrix instructions of 16 x 16 whose 16 columns are the query heads of the KV head (G <= 16,
 // the rest zeros): S^T = K Q^T, then out^T += V^T P^T.  Both products take K and V as they lie in memory, without LDS:
@@ -21,6 +23,13 @@
 // a logit passes them.  bf16 probabilities enter the second product in three parts of 8 bits (each part but the first 2^-28 of the
 // whole too large, so that none is zero): the result is as good as in fp32 (rounded to bf16 they would be off by
 // 2^-9), and the matrix pipe has the time.
+//
+// What bounds it: HBM.  4 x 8 heads x 131 072 rows of 128 bf16 elements (2.15 GB, four query heads or eight): 325-340 us, 6.3-6.6 TB/s,
+// what the dense cache's kernel reaches over the same rows (330 us); every byte fetched once; the matrix pipe is busy 8 % of
+// the time, the vector pipe 14 %.  Few rows: the chain of dependent loads (length, table, rows), 7.5 us, and the second kernel,
+// 3.5 us (8 heads x 1 056 rows).  A wavefront holds one step's K and one step's V in flight, the next one's as soon as the products
+// have taken their operands; a third workgroup per compute unit, spilling, was slower (375 us), ordinary loads in place of non-temporal ones
+// as well (378).
 #include "sablock_internal.h"
 
 #include <cfloat>
@@ -467,7 +476,7 @@ decode_paged_kernel(DecodePagedArgs a)
     }
 }
 
-// grid (G, problems): the pieces' weights first, then their weighted sum, four elements per thread, the pieces dealt out to groups of threads
+// grid (G, problems) of the long ones: the pieces' weights first, then their weighted sum, four elements per thread, the pieces dealt out to groups of threads
 constexpr int MERGE_T = 256, MAX_PIECES = 1024, EARLY = 2;
 template <int STEP>
 __global__ void __launch_bounds__(MERGE_T)
@@ -531,14 +540,19 @@ decode_paged_merge_kernel(DecodePagedArgs a)
     *reinterpret_cast<f32x4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
 }
 
-// workgroups per compute unit that the registers leave room for
+// Workgroups per compute unit that the registers leave room for.  The long problems are dealt out to just as many: with two of three
+// 64 sequences of up to 8 192 rows took 218 us in place of 184.
 int resident(const PageDims &d)
 {
     if (d.dtype == SABLOCK_BF16) return d.D <= 64 ? 3 : 2;
     return d.D <= 80 ? 3 : d.D <= 160 ? 2 : 1;
 }
 int workgroups_of(const PageDims &d) { return std::min(d.cus * resident(d), MAX_PIECES - 1); }
-// rows of the longest problem that a workgroup takes alone
+// Rows of the longest problem that a workgroup takes alone: 256 KB of K and V, or 512 KB where the problems fill the compute units by
+// themselves.  Alone against dealt out, rows of 256 bytes, 4 query heads: 8 problems of 512 rows 9.2 and 10.4 us, of 1 024 14.0 and
+// 11.0; 64 of 512 12.2 and 12.8, of 1 024 20.9 and 15.9; 256 of 1 024 26.5 and 32.0; lengths spread up to the given ones:
+// 1 024 problems of 256 22.5 and 50.4, of 1 024 57.7 and 81.2.  With 1 MB the longest are waited for: 256 problems of up to
+// 4 096 76.8 us, with 512 KB 63.4.
 int rows_alone(const PageDims &d) { return (d.P >= d.cus ? 1 << 19 : 1 << 18) / (2 * d.D * elt_bytes(d)); }
 
 }  // namespace
