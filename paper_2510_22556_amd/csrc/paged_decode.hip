@@ -41,6 +41,7 @@ namespace {
 constexpr int NW = 4, NT = NW * 64;
 constexpr float AHEAD = 8.f;
 constexpr float PART_LEAST = 0x1p-28f;         // a part of a probability that would be zero times an infinite value would be no number
+constexpr int SPARE = 4;
 constexpr int LEAST_STEPS = 4;                 // of a workgroup's run: one per wavefront
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -140,69 +141,106 @@ __device__ __forceinline__ int64_t scan(int64_t x, int lane, bool narrow)
     return x;
 }
 
-// Where the long problems' steps lie in the row of all of them; a wavefront's view, each lane with the sums up to its share of the sequences.
-template <int STEP>
-struct Places {
-    const DecodePagedArgs &a;
-    int lane, share, heads;                    // sequences per lane, problems per sequence
-    int64_t upto, total;                       // steps of one problem of each sequence up to the lane's last, of all problems
-    __device__ Places(const DecodePagedArgs &args, int l) : a(args), lane(l)
-    {
-        heads = a.d.n_layers * a.d.Hkv;
-        share = (a.d.n_seq + 63) / 64;
-        if (a.d.n_seq == 1) {
-            upto = shared_steps_of<STEP>(a, 0);
-            total = upto * heads;
-            return;
-        }
-        int64_t sum = 0;
-#pragma unroll 8
-        for (int i = 0; i < share; ++i) {                      // loads without a branch, several at a time
-            const int s = lane * share + i, n = shared_steps_of<STEP>(a, min(s, a.d.n_seq - 1));
-            sum += s < a.d.n_seq ? n : 0;
-        }
-        upto = scan(sum, lane, a.narrow);
-        total = of_lane(upto, 63) * heads;
-    }
-    // the sequence that step x of all lies in (x < total), the steps of one problem of those before it, and of its own
-    __device__ void find(int64_t x, int &seq, int64_t &before, int &steps) const
-    {
-        if (a.d.n_seq == 1) { seq = 0; before = 0; steps = (int)upto; return; }
-        const int first = uniform(__ffsll((unsigned long long)__ballot(upto * heads > x)) - 1);
-        const int64_t at = first > 0 ? of_lane(upto, first - 1) : 0;
-        if (share == 1) {
-            seq = first;
-            before = at;
-            steps = (int)(of_lane(upto, first) - at);
-            return;
-        }
-        const int s = first * share + lane;
-        const int own = lane < share && s < a.d.n_seq ? shared_steps_of<STEP>(a, s) : 0;
-        const int64_t inner = scan((int64_t)own, lane, a.narrow) + at;
-        const int j = uniform(__ffsll((unsigned long long)__ballot(inner * heads > x)) - 1);
-        seq = first * share + j;
-        steps = of_lane(own, j);
-        before = of_lane(inner, j) - steps;
-    }
-    // the same for a given sequence
-    __device__ void of(int seq, int64_t &before, int &steps) const
-    {
-        const int first = uniform(seq / share);
-        before = first > 0 ? of_lane(upto, first - 1) : 0;
-        for (int s = first * share; s < seq; ++s) before += shared_steps_of<STEP>(a, s);
-        steps = shared_steps_of<STEP>(a, seq);
-    }
-};
 // x / n of whole numbers; 64 bits are a hundred instructions, and hardly ever needed
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t n)
 {
     return (uint64_t)(x | n) >> 32 ? x / n : (int64_t)((uint32_t)x / (uint32_t)n);
 }
-// steps of a workgroup's run
-__device__ __forceinline__ int64_t run_of(int64_t total, int workgroups)
-{
-    return max((int64_t)LEAST_STEPS, quotient(total + workgroups - 1, workgroups));
-}
+
+// How the long problems' steps are dealt out: in runs that are cut at the problems' ends, one per workgroup, where the workgroups are
+// enough for them, or would be with runs of up to SPARE steps more; else in equal runs of the steps of all, one problem's behind the other's,
+// so that a workgroup may have pieces of several problems (a piece's chain of loads costs it as much as SPARE steps).  A
+// wavefront's view: each lane has the sums up to its share of the sequences.
+template <int STEP>
+struct Places {
+    const DecodePagedArgs &a;
+    int lane, share, heads;                    // sequences per lane, problems per sequence
+    int steps;                                 // of the lane's sequence, where it has one
+    bool whole;                                // a piece per workgroup
+    int64_t run;                               // steps of a workgroup, at most
+    int64_t upto, total;                       // units (pieces, or steps) of one problem of each sequence up to the lane's last, of all problems
+    __device__ int64_t units_of(int steps) const { return whole ? quotient(steps + run - 1, run) : steps; }
+    __device__ Places(const DecodePagedArgs &args, int l) : a(args), lane(l) {}
+    __device__ void deal()
+    {
+        heads = a.d.n_layers * a.d.Hkv;
+        share = (a.d.n_seq + 63) / 64;
+        int64_t sum = 0;
+        int longs = 0;
+        if (a.d.n_seq == 1) {
+            steps = uniform(shared_steps_of<STEP>(a, 0));
+            longs = steps > 0;
+            upto = sum = steps;
+        } else {
+#pragma unroll 8
+            for (int i = 0; i < share; ++i) {                  // loads without a branch, several at a time
+                const int s = lane * share + i, n = shared_steps_of<STEP>(a, min(s, a.d.n_seq - 1));
+                sum += s < a.d.n_seq ? n : 0;
+                longs += s < a.d.n_seq && n > 0;
+            }
+            steps = (int)sum;
+            upto = scan(sum, lane, a.narrow);
+            longs = of_lane(scan(longs), 63);
+        }
+        total = last() * heads;
+        const int64_t evenly = upto, all = total, problems = (int64_t)longs * heads;
+        run = max((int64_t)LEAST_STEPS, quotient(total + a.workgroups - 1, a.workgroups));
+        if (cut()) return;
+        const int64_t even = run;
+        if (problems < a.workgroups) {                         // a piece more of each problem, and the workgroups are enough
+            run = max(run, quotient(all + a.workgroups - problems - 1, a.workgroups - problems));
+            if (run <= even + SPARE && cut()) return;
+        }
+        whole = false;
+        run = even;
+        upto = evenly;
+        total = all;
+    }
+    __device__ int64_t last() const { return a.d.n_seq > 1 ? of_lane(upto, 63) : upto; }
+    // units are pieces of up to `run` steps, if there are no more than workgroups
+    __device__ bool cut()
+    {
+        whole = true;
+        int64_t own = 0;
+        if (share == 1) own = units_of(steps);
+        else {
+            for (int i = 0; i < share; ++i)
+                if (lane * share + i < a.d.n_seq) own += units_of(shared_steps_of<STEP>(a, lane * share + i));
+        }
+        upto = a.d.n_seq > 1 ? scan(own, lane, a.narrow) : own;
+        total = last() * heads;
+        return total <= a.workgroups;
+    }
+    // the sequence that unit x of all lies in (x < total), the units of one problem of those before it, and the units and steps of its own
+    __device__ void find(int64_t x, int &seq, int64_t &before, int64_t &units, int &n) const
+    {
+        if (a.d.n_seq == 1) { seq = 0; before = 0; units = upto; n = steps; return; }
+        const int first = uniform(__ffsll((unsigned long long)__ballot(upto * heads > x)) - 1);
+        const int64_t at = first > 0 ? of_lane(upto, first - 1) : 0;
+        if (share == 1) {
+            seq = first;
+            before = at;
+            units = of_lane(upto, first) - at;
+            n = of_lane(steps, first);
+            return;
+        }
+        const int s = first * share + lane, own_steps = lane < share && s < a.d.n_seq ? shared_steps_of<STEP>(a, s) : 0;
+        const int64_t own = units_of(own_steps), inner = scan(own, lane, a.narrow) + at;
+        const int j = uniform(__ffsll((unsigned long long)__ballot(inner * heads > x)) - 1);
+        seq = first * share + j;
+        units = of_lane(own, j);
+        n = of_lane(own_steps, j);
+        before = of_lane(inner, j) - units;
+    }
+    // units of one problem of the sequences before the given one
+    __device__ int64_t before(int seq) const
+    {
+        const int first = uniform(seq / share);
+        int64_t sum = first > 0 ? of_lane(upto, first - 1) : 0;
+        for (int s = first * share; s < seq; ++s) sum += units_of(shared_steps_of<STEP>(a, s));
+        return sum;
+    }
+};
 
 __device__ __forceinline__ float over_quarters(float x, bool take_max)        // lanes l, l ^ 16, l ^ 32, l ^ 48
 {
@@ -212,8 +250,9 @@ __device__ __forceinline__ float over_quarters(float x, bool take_max)        //
     return take_max ? fmaxf(x, y) : x + y;
 }
 
-// EP: elements of a row per lane in the second product, D / 16
-template <bool BF16, int EP, int STEP>
+// EP: elements of a row per lane in the second product, D / 16.  SHARED: some problems may be long; else there is nothing but a workgroup per
+// problem (whose registers let a third one reside, heads of 128).
+template <bool BF16, int EP, int STEP, bool SHARED>
 __global__ void __launch_bounds__(NT)
 decode_paged_kernel(DecodePagedArgs a)
 {
@@ -452,27 +491,43 @@ decode_paged_kernel(DecodePagedArgs a)
             }
         }
     };
-    if ((int)blockIdx.x < a.d.P) {
-        const int p = blockIdx.x, s = seq_of_problem(d, p), n = uniform(steps_of<STEP>(a, s));
-        if (n <= a.limit) piece(p, s, 0, n, n);
+    if constexpr (!SHARED) {
+        const int s = seq_of_problem(d, blockIdx.x), n = uniform(steps_of<STEP>(a, s));
+        piece(blockIdx.x, s, 0, n, n);
         return;
     }
-    const int me = blockIdx.x - d.P;
-    const Places<STEP> places(a, lane);
-    const int64_t run = run_of(places.total, a.workgroups), run_to = min((me + 1) * run, places.total);
-    int s = 0, n = 0;
-    int64_t seq_from = 0, seq_to = 0;                          // all steps of sequence s
-    for (int64_t x = me * run; x < run_to;) {
-        if (x >= seq_to) {
-            int64_t before;
-            places.find(x, s, before, n);
-            seq_from = before * places.heads;
-            seq_to = seq_from + (int64_t)n * places.heads;
+    // one call of the above, whatever the workgroup's part is: its code is long, and comes cold from memory
+    const int me = (int)blockIdx.x - d.P;                      // the first ones see to short problems
+    Places<STEP> places(a, lane);
+    int p = blockIdx.x, s = 0, off = 0, count = 0, n = 0;
+    int64_t x = 0, to = 0, seq_from = 0, seq_to = 0, units = 0;                // seq_from, seq_to: all units of sequence s
+    if (me < 0) {
+        s = seq_of_problem(d, p);
+        n = count = uniform(steps_of<STEP>(a, s));
+        if (n > a.limit) return;
+    } else {
+        places.deal();
+        const int64_t share = places.whole ? 1 : places.run;
+        x = me * share;
+        to = min(x + share, places.total);
+        if (x >= to) return;
+    }
+    for (;;) {
+        if (me >= 0) {
+            if (x >= seq_to) {
+                int64_t before;
+                places.find(x, s, before, units, n);
+                seq_from = before * places.heads;
+                seq_to = seq_from + units * places.heads;
+            }
+            const int problem = uniform((int)quotient(x - seq_from, units)), unit = uniform((int)(x - seq_from - problem * units));
+            off = places.whole ? unit * (int)places.run : unit;
+            count = uniform((int)min((int64_t)(n - off), places.whole ? places.run : to - x));
+            p = s * places.heads + problem;
+            x += places.whole ? 1 : count;
         }
-        const int problem = uniform((int)quotient(x - seq_from, n)), off = uniform((int)(x - seq_from - (int64_t)problem * n));
-        const int count = uniform((int)min((int64_t)(n - off), run_to - x));
-        piece(s * places.heads + problem, s, off, count, n);
-        x += count;
+        piece(p, s, off, count, n);
+        if (x >= to) break;
     }
 }
 
@@ -486,16 +541,14 @@ decode_paged_merge_kernel(DecodePagedArgs a)
     __shared__ f32x4 sum[MERGE_T];
     const PageDims &d = a.d;
     const int g = blockIdx.x, p = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
-    const Places<STEP> places(a, lane);
-    const int seq = seq_of_problem(d, p);
-    int n;
-    int64_t before;
-    places.of(seq, before, n);
-    float *out = a.out + ((((int64_t)seq * d.n_layers + layer_of_problem(d, p)) * d.Hq) + head_of_problem(d, p) * d.G + g) * d.D;
+    const int seq = seq_of_problem(d, p), n = shared_steps_of<STEP>(a, seq);
     if (n == 0) return;                                        // a workgroup's alone
-    const int64_t run = run_of(places.total, a.workgroups), at = before * places.heads + (int64_t)(p - seq * places.heads) * n;
-    const int64_t first = quotient(at, run);
-    const int pieces = (int)(quotient(at + n - 1, run) - first) + 1;
+    float *out = a.out + ((((int64_t)seq * d.n_layers + layer_of_problem(d, p)) * d.Hq) + head_of_problem(d, p) * d.G + g) * d.D;
+    Places<STEP> places(a, lane);
+    places.deal();
+    const int64_t units = places.units_of(n), at = places.before(seq) * places.heads + (p - seq * places.heads) * units;
+    const int64_t first = places.whole ? at : quotient(at, places.run);
+    const int pieces = places.whole ? (int)units : (int)(quotient(at + n - 1, places.run) - first) + 1;
     if (pieces == 1) return;                                   // finished where it was computed
     auto slot = [&](int i) { return (2 * (first + i) + (i == 0)) * d.G + g; };
     const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
@@ -544,8 +597,7 @@ decode_paged_merge_kernel(DecodePagedArgs a)
 // 64 sequences of up to 8 192 rows took 218 us in place of 184.
 int resident(const PageDims &d)
 {
-    if (d.dtype == SABLOCK_BF16) return d.D <= 64 ? 3 : 2;
-    return d.D <= 80 ? 3 : d.D <= 160 ? 2 : 1;
+    return d.D <= 64 ? 3 : d.dtype == SABLOCK_BF16 || d.D <= 160 ? 2 : 1;
 }
 int workgroups_of(const PageDims &d) { return std::min(d.cus * resident(d), MAX_PIECES - 1); }
 // Rows of the longest problem that a workgroup takes alone: 256 KB of K and V, or 512 KB where the problems fill the compute units by
@@ -586,15 +638,16 @@ hipError_t launch_decode_paged(const PageDims &d, const void *q, const PageView 
     a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups * d.G * 8));
     using Kern = void (*)(DecodePagedArgs);
     Kern fn = nullptr;
-#define SABLOCK_PAGED_F(EV) if (!bf && d.D == EV * 16) fn = decode_paged_kernel<false, EV, 16>;
-#define SABLOCK_PAGED_B(EV)                                                                                              \
-    if (bf && d.D == EV * 16)                                                                                             \
-        fn = alone ? decode_paged_kernel<true, EV, step_rows(true, EV * 16, true)> : decode_paged_kernel<true, EV, step_rows(true, EV * 16, false)>; \
-    SABLOCK_PAGED_F(EV)
+#define SABLOCK_PAGED(BV, EV)                                                                                             \
+    if (bf == BV && d.D == EV * 16)                                                                                       \
+        fn = alone ? decode_paged_kernel<BV, EV, step_rows(BV, EV * 16, true), false> : decode_paged_kernel<BV, EV, step_rows(BV, EV * 16, false), true>;
+#define SABLOCK_PAGED_F(EV) SABLOCK_PAGED(false, EV)
+#define SABLOCK_PAGED_B(EV) SABLOCK_PAGED(true, EV) SABLOCK_PAGED(false, EV)
     SABLOCK_PAGED_F(1) SABLOCK_PAGED_B(2) SABLOCK_PAGED_F(3) SABLOCK_PAGED_B(4) SABLOCK_PAGED_F(5) SABLOCK_PAGED_B(6) SABLOCK_PAGED_F(7) SABLOCK_PAGED_B(8)
     SABLOCK_PAGED_F(9) SABLOCK_PAGED_B(10) SABLOCK_PAGED_F(11) SABLOCK_PAGED_B(12) SABLOCK_PAGED_F(13) SABLOCK_PAGED_B(14) SABLOCK_PAGED_F(15) SABLOCK_PAGED_B(16)
 #undef SABLOCK_PAGED_B
 #undef SABLOCK_PAGED_F
+#undef SABLOCK_PAGED
     if (!fn) return hipErrorInvalidValue;
     hipLaunchKernelGGL(fn, dim3(a.workgroups + d.P), dim3(NT), 0, st, a);
     if (a.workgroups) hipLaunchKernelGGL(step == 32 ? decode_paged_merge_kernel<32> : decode_paged_merge_kernel<16>, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);

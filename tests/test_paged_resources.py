@@ -19,7 +19,7 @@ def _kernels(text):
 
 def test_no_kernel_spills(assembly):
     kernels = {n: k for text in assembly.values() for n, k in _kernels(text).items()}
-    assert len(kernels) == (2 + 8) + (4 + 6 + 16 + 2) + (2 * 6 * 4 + 4)
+    assert len(kernels) == (2 + 8) + (48 + 2) + (2 * 6 * 4 + 4)
     assert not any(k["private_segment_fixed_size"] for k in kernels.values())
 
 
@@ -27,15 +27,16 @@ def test_as_many_workgroups_reside_as_the_shared_runs_are_cut_for(assembly):
     # 512 registers per lane and SIMD, given out by the eight; a workgroup has a wavefront on each (the same rule as in the source)
     seen = 0
     for name, k in _kernels(assembly["paged_decode.hip"]).items():
-        m = re.search(r"decode_paged_kernelILb([01])ELi(\d+)ELi(\d+)E", name)
+        m = re.search(r"decode_paged_kernelILb([01])ELi(\d+)ELi(\d+)ELb([01])E", name)
         if not m:
             continue
-        bf16, dim, step = m[1] == "1", 16 * int(m[2]), int(m[3])
+        bf16, dim, shared = m[1] == "1", 16 * int(m[2]), m[4] == "1"
+        assert int(m[3]) == (32 if bf16 and dim <= (128 if shared else 64) else 16)
         resident = 512 // -(-k["next_free_vgpr"] // 8 * 8)
-        planned = (3 if dim <= 64 or (step == 16 and dim <= 128) else 2) if bf16 else 3 if dim <= 80 else 2 if dim <= 160 else 1
+        planned = 3 if dim <= 64 or (bf16 and dim <= 128 and not shared) else 2 if bf16 or dim <= 160 else 1
         assert resident >= planned, (name, k["next_free_vgpr"])
         seen += 1
-    assert seen == 26
+    assert seen == 48
 
 
 def _registers(operand):
