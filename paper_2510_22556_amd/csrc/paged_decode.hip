@@ -3,10 +3,10 @@
 //
 //   decode_paged_kernel   Work is counted in steps of 32 or 16 rows.  A short problem (a sequence's KV head in a layer) is one
 //       workgroup's, which finishes it; the first n_seq * n_layers * Hkv workgroups see to those, and write zeros where there is no row.  The
-//       steps of the long ones are counted one behind the other and dealt out in equal runs to as many workgroups as reside at a
-//       time: the lengths, which only the device knows, do not matter.  A run covers pieces of one or several problems; a
-//       problem inside one run is finished there, of another's piece (reference, denominator, numerators) go to the workspace,
-//       at most two per workgroup.
+//       steps of the long ones are dealt out in even runs to as many workgroups as reside at a time (see Places): the lengths,
+//       which only the device knows, do not matter.  A run is a piece of one problem, or pieces of several; a problem inside
+//       one run is finished there, of another's piece (reference, denominator, numerators) go to the workspace, at most two
+//       per workgroup.
 //   decode_paged_merge_kernel   joins the pieces of each problem.  Not launched where no sequence has room to be long.
 //
 // A wavefront does a step alone, on matrix instructions of 16 x 16 whose 16 columns are the query heads of the KV head (G <= 16,
@@ -26,8 +26,9 @@
 //
 // What bounds it: HBM.  4 x 8 heads x 131 072 rows of 128 bf16 elements (2.15 GB, four query heads or eight): 325-340 us, 6.3-6.6 TB/s,
 // what the dense cache's kernel reaches over the same rows (330 us); every byte fetched once; the matrix pipe is busy 8 % of
-// the time, the vector pipe 14 %.  Few rows: the chain of dependent loads (length, table, rows), 7.5 us, and the second kernel,
-// 3.5 us (8 heads x 1 056 rows).  A wavefront holds one step's K and one step's V in flight, the next one's as soon as the products
+// the time, the vector pipe 14 %.  Few rows: the chain of dependent loads (length, table, rows), and that of the second kernel, 10.3 us
+// in all (8 heads x 1 056 rows); what does not depend on the rows is kept short, the code too, which comes cold from memory (with
+// the dealing in 64 bits 10.8).  A wavefront holds one step's K and one step's V in flight, the next one's as soon as the products
 // have taken their operands; a third workgroup per compute unit, spilling, was slower (375 us), ordinary loads in place of non-temporal ones
 // as well (378).
 #include "sablock_internal.h"
@@ -85,7 +86,6 @@ struct DecodePagedArgs {
     float qscale;                // log2(e) / sqrt(D)
     int workgroups;              // that share the long problems' steps
     int limit;                   // steps of the longest problem that a workgroup takes alone
-    bool narrow;                 // 32 bits hold all sequences' steps
     float *out;                  // [n_seq][n_layers][Hq][D]
     float *weights;              // pieces [2 * workgroups][G][2]: reference (log2 domain), denominator
     float *sums;                 // pieces [2 * workgroups][G][D]
@@ -115,11 +115,7 @@ __device__ __forceinline__ int shared_steps_of(const DecodePagedArgs &a, int s)
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // the value of one lane, the same one for all
 __device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-__device__ __forceinline__ int64_t of_lane(int64_t x, int lane)
-{
-    return (int64_t)((uint64_t)(uint32_t)of_lane((int)(x >> 32), lane) << 32 | (uint32_t)of_lane((int)x, lane));
-}
-// inclusive sums over the lanes: in 32 bits by lane shifts inside a row of 16 and the rows' ends into the next ones
+// inclusive sums over the lanes, by shifts inside a row of 16 and the rows' ends into the next ones
 __device__ __forceinline__ int scan(int x)
 {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
@@ -130,63 +126,48 @@ __device__ __forceinline__ int scan(int x)
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
     return x;
 }
-__device__ __forceinline__ int64_t scan(int64_t x, int lane, bool narrow)
-{
-    if (narrow) return scan((int)x);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t u = __shfl_up(x, o);
-        if (lane >= o) x += u;
-    }
-    return x;
-}
-
-// x / n of whole numbers; 64 bits are a hundred instructions, and hardly ever needed
-__device__ __forceinline__ int64_t quotient(int64_t x, int64_t n)
-{
-    return (uint64_t)(x | n) >> 32 ? x / n : (int64_t)((uint32_t)x / (uint32_t)n);
-}
+__device__ __forceinline__ int quotient(int x, int n) { return (int)((uint32_t)x / (uint32_t)n); }            // neither negative
 
 // How the long problems' steps are dealt out: in runs that are cut at the problems' ends, one per workgroup, where the workgroups are
 // enough for them, or would be with runs of up to SPARE steps more; else in equal runs of the steps of all, one problem's behind the other's,
-// so that a workgroup may have pieces of several problems (a piece's chain of loads costs it as much as SPARE steps).  A
-// wavefront's view: each lane has the sums up to its share of the sequences.
+// so that a workgroup may have pieces of several problems (a piece's chain of loads costs it as much as SPARE steps: 8 heads x 700 rows
+// 12.7 us in even runs, 10.7 cut at the ends; x 4 001 14.1 and 12.5).  A
+// wavefront's view: each lane has the sums up to its share of the sequences.  All problems' steps fit 32 bits (the launch sees to it).
 template <int STEP>
 struct Places {
     const DecodePagedArgs &a;
     int lane, share, heads;                    // sequences per lane, problems per sequence
     int steps;                                 // of the lane's sequence, where it has one
     bool whole;                                // a piece per workgroup
-    int64_t run;                               // steps of a workgroup, at most
-    int64_t upto, total;                       // units (pieces, or steps) of one problem of each sequence up to the lane's last, of all problems
-    __device__ int64_t units_of(int steps) const { return whole ? quotient(steps + run - 1, run) : steps; }
+    int run;                                   // steps of a workgroup, at most
+    int upto, total;                           // units (pieces, or steps) of one problem of each sequence up to the lane's last, of all problems
     __device__ Places(const DecodePagedArgs &args, int l) : a(args), lane(l) {}
+    __device__ int units_of(int steps) const { return whole ? quotient(steps + run - 1, run) : steps; }
+    __device__ int last() const { return a.d.n_seq > 1 ? of_lane(upto, 63) : upto; }
     __device__ void deal()
     {
         heads = a.d.n_layers * a.d.Hkv;
         share = (a.d.n_seq + 63) / 64;
-        int64_t sum = 0;
         int longs = 0;
+        steps = 0;
         if (a.d.n_seq == 1) {
-            steps = uniform(shared_steps_of<STEP>(a, 0));
+            upto = steps = uniform(shared_steps_of<STEP>(a, 0));
             longs = steps > 0;
-            upto = sum = steps;
         } else {
-#pragma unroll 8
+#pragma unroll 4
             for (int i = 0; i < share; ++i) {                  // loads without a branch, several at a time
                 const int s = lane * share + i, n = shared_steps_of<STEP>(a, min(s, a.d.n_seq - 1));
-                sum += s < a.d.n_seq ? n : 0;
+                steps += s < a.d.n_seq ? n : 0;
                 longs += s < a.d.n_seq && n > 0;
             }
-            steps = (int)sum;
-            upto = scan(sum, lane, a.narrow);
+            upto = scan(steps);
             longs = of_lane(scan(longs), 63);
         }
         total = last() * heads;
-        const int64_t evenly = upto, all = total, problems = (int64_t)longs * heads;
-        run = max((int64_t)LEAST_STEPS, quotient(total + a.workgroups - 1, a.workgroups));
+        const int evenly = upto, all = total, problems = longs * heads;
+        run = max(LEAST_STEPS, quotient(total + a.workgroups - 1, a.workgroups));
+        const int even = run;
         if (cut()) return;
-        const int64_t even = run;
         if (problems < a.workgroups) {                         // a piece more of each problem, and the workgroups are enough
             run = max(run, quotient(all + a.workgroups - problems - 1, a.workgroups - problems));
             if (run <= even + SPARE && cut()) return;
@@ -196,27 +177,24 @@ struct Places {
         upto = evenly;
         total = all;
     }
-    __device__ int64_t last() const { return a.d.n_seq > 1 ? of_lane(upto, 63) : upto; }
     // units are pieces of up to `run` steps, if there are no more than workgroups
     __device__ bool cut()
     {
         whole = true;
-        int64_t own = 0;
+        int own = 0;
         if (share == 1) own = units_of(steps);
-        else {
+        else
             for (int i = 0; i < share; ++i)
                 if (lane * share + i < a.d.n_seq) own += units_of(shared_steps_of<STEP>(a, lane * share + i));
-        }
-        upto = a.d.n_seq > 1 ? scan(own, lane, a.narrow) : own;
+        upto = a.d.n_seq > 1 ? scan(own) : own;
         total = last() * heads;
         return total <= a.workgroups;
     }
     // the sequence that unit x of all lies in (x < total), the units of one problem of those before it, and the units and steps of its own
-    __device__ void find(int64_t x, int &seq, int64_t &before, int64_t &units, int &n) const
+    __device__ void find(int x, int &seq, int &before, int &units, int &n) const
     {
         if (a.d.n_seq == 1) { seq = 0; before = 0; units = upto; n = steps; return; }
-        const int first = uniform(__ffsll((unsigned long long)__ballot(upto * heads > x)) - 1);
-        const int64_t at = first > 0 ? of_lane(upto, first - 1) : 0;
+        const int first = uniform(__ffsll((unsigned long long)__ballot(upto * heads > x)) - 1), at = first > 0 ? of_lane(upto, first - 1) : 0;
         if (share == 1) {
             seq = first;
             before = at;
@@ -225,18 +203,17 @@ struct Places {
             return;
         }
         const int s = first * share + lane, own_steps = lane < share && s < a.d.n_seq ? shared_steps_of<STEP>(a, s) : 0;
-        const int64_t own = units_of(own_steps), inner = scan(own, lane, a.narrow) + at;
-        const int j = uniform(__ffsll((unsigned long long)__ballot(inner * heads > x)) - 1);
+        const int own = units_of(own_steps), inner = scan(own) + at, j = uniform(__ffsll((unsigned long long)__ballot(inner * heads > x)) - 1);
         seq = first * share + j;
         units = of_lane(own, j);
         n = of_lane(own_steps, j);
         before = of_lane(inner, j) - units;
     }
     // units of one problem of the sequences before the given one
-    __device__ int64_t before(int seq) const
+    __device__ int before(int seq) const
     {
-        const int first = uniform(seq / share);
-        int64_t sum = first > 0 ? of_lane(upto, first - 1) : 0;
+        const int first = uniform(quotient(seq, share));
+        int sum = first > 0 ? of_lane(upto, first - 1) : 0;
         for (int s = first * share; s < seq; ++s) sum += units_of(shared_steps_of<STEP>(a, s));
         return sum;
     }
@@ -500,14 +477,15 @@ decode_paged_kernel(DecodePagedArgs a)
     const int me = (int)blockIdx.x - d.P;                      // the first ones see to short problems
     Places<STEP> places(a, lane);
     int p = blockIdx.x, s = 0, off = 0, count = 0, n = 0;
-    int64_t x = 0, to = 0, seq_from = 0, seq_to = 0, units = 0;                // seq_from, seq_to: all units of sequence s
+    int x = 0, to = 0, seq_from = 0, seq_to = 0, units = 0;    // seq_from, seq_to: all units of sequence s
     if (me < 0) {
         s = seq_of_problem(d, p);
         n = count = uniform(steps_of<STEP>(a, s));
         if (n > a.limit) return;
     } else {
         places.deal();
-        const int64_t share = places.whole ? 1 : places.run;
+        const int share = places.whole ? 1 : places.run;
+        if (me > quotient(places.total, share)) return;        // and so no overflow below
         x = me * share;
         to = min(x + share, places.total);
         if (x >= to) return;
@@ -515,14 +493,14 @@ decode_paged_kernel(DecodePagedArgs a)
     for (;;) {
         if (me >= 0) {
             if (x >= seq_to) {
-                int64_t before;
+                int before;
                 places.find(x, s, before, units, n);
                 seq_from = before * places.heads;
                 seq_to = seq_from + units * places.heads;
             }
-            const int problem = uniform((int)quotient(x - seq_from, units)), unit = uniform((int)(x - seq_from - problem * units));
-            off = places.whole ? unit * (int)places.run : unit;
-            count = uniform((int)min((int64_t)(n - off), places.whole ? places.run : to - x));
+            const int problem = uniform(quotient(x - seq_from, units)), unit = uniform(x - seq_from - problem * units);
+            off = places.whole ? unit * places.run : unit;
+            count = uniform(min(n - off, places.whole ? places.run : to - x));
             p = s * places.heads + problem;
             x += places.whole ? 1 : count;
         }
@@ -546,11 +524,11 @@ decode_paged_merge_kernel(DecodePagedArgs a)
     float *out = a.out + ((((int64_t)seq * d.n_layers + layer_of_problem(d, p)) * d.Hq) + head_of_problem(d, p) * d.G + g) * d.D;
     Places<STEP> places(a, lane);
     places.deal();
-    const int64_t units = places.units_of(n), at = places.before(seq) * places.heads + (p - seq * places.heads) * units;
-    const int64_t first = places.whole ? at : quotient(at, places.run);
-    const int pieces = places.whole ? (int)units : (int)(quotient(at + n - 1, places.run) - first) + 1;
+    const int units = places.units_of(n), at = places.before(seq) * places.heads + (p - seq * places.heads) * units;
+    const int first = places.whole ? at : quotient(at, places.run);
+    const int pieces = places.whole ? units : quotient(at + n - 1, places.run) - first + 1;
     if (pieces == 1) return;                                   // finished where it was computed
-    auto slot = [&](int i) { return (2 * (first + i) + (i == 0)) * d.G + g; };
+    auto slot = [&](int i) { return (int64_t)(2 * (first + i) + (i == 0)) * d.G + g; };
     const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
     // the first of the numerators are on their way while the weights are formed
     auto part = [&](int i) { return *reinterpret_cast<const f32x4 *>(a.sums + slot(min(i, pieces - 1)) * d.D + 4 * c); };
@@ -629,11 +607,11 @@ hipError_t launch_decode_paged(const PageDims &d, const void *q, const PageView 
     a.qscale = (float)(1.4426950408889634 / sqrt((double)d.D));
     a.out = out;
     const int64_t capacity = (int64_t)(list ? std::min(n_listed, d.max_pages) : d.max_pages) * d.page;
-    const bool bf = d.dtype == SABLOCK_BF16, alone = capacity <= rows_alone(d);               // no problem can be longer
+    // no problem can be longer; or tables with room for so many rows that 32 bits do not count all steps, with a workgroup's run to spare
+    const bool bf = d.dtype == SABLOCK_BF16, alone = capacity <= rows_alone(d) || d.P * (capacity / 16 + 1) >= 1 << 30;
     const int workgroups = workgroups_of(d), step = step_rows(bf, d.D, alone);
     a.limit = (rows_alone(d) + step - 1) / step;
     a.workgroups = alone ? 0 : workgroups;
-    a.narrow = d.n_seq * (capacity / step + 1) < INT32_MAX;
     a.weights = static_cast<float *>(ws);
     a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups * d.G * 8));
     using Kern = void (*)(DecodePagedArgs);
