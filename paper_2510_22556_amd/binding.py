@@ -516,7 +516,8 @@ def sablock_select_pages(pages: CPages, q, bounds, page_table, lengths, n_pick: 
 class PagedCache:
     """Pools, page table and lengths of a paged cache, page bounds where asked for, and the workspaces of the calls that read it.
 
-    Which pages a sequence has is the caller's to say: ``page_table`` starts as -1 (no page)."""
+    Which pages a sequence has is the caller's to say: ``page_table`` starts as -1 (no page).  The workspaces serve one call at a time:
+    calls that may overlap, on two streams or in two captured graphs, bring their own."""
 
     def __init__(self, n_seq: int, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, max_pages: int,
                  dtype, device, bounds: bool = True):
