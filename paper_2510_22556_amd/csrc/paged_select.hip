@@ -2,14 +2,16 @@
 // then the best of them per KV head.
 //
 //   page_scores_kernel   max(q lo, q hi) is q+ hi + q- lo with q+ = max(q, 0), q- = min(q, 0): two products per element and head,
-//       formed and summed in fp64.  The products of two bf16 values and their sum over a head are exact there (but for
-//       elements some 2^30 apart), so that which of two pages comes first does not hang on the order of a sum.  A page's row of bounds
-//       is spread over LP lanes, 16 bytes of lo and of hi each, several pages in flight; the sums of up to four heads over the
-//       lanes hand each lane one head, which it rounds to fp32 and turns into a whole number of the same order, and the maximum
-//       over the heads is one of whole numbers, in which what is no number can be the largest.
-//       What bounds it: 8 heads x 8 192 pages of 512 bytes of bounds, four query heads: 12.4 us, of which 5.1 are the bytes at 6.6 TB/s
-//       and 5.7 the vector pipe (two fp64 products per element and head); the rest is the chain length, table, bounds.  With the
-//       next pages' bounds on their way 13.4 in place of 14.7.
+//       formed and summed in fp64, on the matrix pipe.  The products of two bf16 values and their sum over a head are exact there (but for
+//       elements some 2^30 apart), so that which of two pages comes first does not hang on the order of a sum.  A matrix
+//       instruction of four products 4 x 4 x 4 has four pages in its rows, four heads in its columns and, in its four inner places
+//       and in the four products, different 16-byte pieces of a row of bounds, one element of each at a time: a lane's
+//       operand is an element of the piece that it loaded.  The products' sums are joined over the lanes, each lane then
+//       has one page and head, whose score it rounds to fp32 and turns into a whole number of the same order; the maximum over the heads is
+//       one of whole numbers, in which what is no number can be the largest.
+//       What bounds it: loads.  8 heads x 8 192 pages of 512 bytes of bounds, four query heads: 9.7 us, of which 5.1 are the bytes at 6.6 TB/s;
+//       as long without the products, the rest is the launch and the chain length, table, bounds.  Formed on the vector pipe, by fp64
+//       instructions and sums over 16 lanes, 12.3; with 16 query heads, picking and reading with it, 36.3 in place of 46.3.
 //   pick_pages_kernel    a workgroup per problem; the keys stay in registers.  The last key that is taken is found digit by digit, 11 bits
 //       of its distance from the least key at a time (the keys of a problem share their upper bits) until 64 are left, which a wavefront
 //       ranks, and one prefix sum places the pages in order.  8 192 pages: 7.3 us, a chain of a dozen barriers.
@@ -19,7 +21,9 @@ namespace sablock {
 namespace {
 
 constexpr int NT = 256, PICK_NT = 1024;
-constexpr int SCORE_WGS = 2;                   // workgroups of the scores per compute unit: as many as run at a time
+// Workgroups of the scores per compute unit, as many as run at a time (with two 64 x 8 heads x 2 048 pages, scored, picked and read, 209 us in place
+// of 199)
+constexpr int SCORE_WGS = 3;
 constexpr uint32_t NOT_A_NUMBER = 0xfffffffeu; // above every number's key
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -41,34 +45,6 @@ template <int M> __device__ __forceinline__ double xor_lane_d(double x)
     return __builtin_bit_cast(double, (uint64_t)xor_lane_u<M>((uint32_t)(u >> 32)) << 32 | xor_lane_u<M>((uint32_t)u));
 }
 
-// x[0 .. N) summed over LP lanes: lane l gets the entries l % S + S j, S = min(N, LP), in x[j]
-template <int B, int S, int LP, int N>
-__device__ __forceinline__ void sum_lanes(double (&x)[N])
-{
-    if constexpr (B < LP) {
-        if constexpr (B < S) {
-            const bool up = threadIdx.x & B;
-#pragma unroll
-            for (int i = 0; i < N / (2 * B); ++i) {
-                const double own = up ? x[2 * i + 1] : x[2 * i], other = up ? x[2 * i] : x[2 * i + 1];
-                x[i] = own + xor_lane_d<B>(other);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < N / S; ++j) x[j] += xor_lane_d<B>(x[j]);
-        }
-        sum_lanes<2 * B, S, LP, N>(x);
-    }
-}
-template <int B, int S> __device__ __forceinline__ uint32_t most_of_lanes(uint32_t x)
-{
-    if constexpr (B < S) return most_of_lanes<2 * B, S>(max(x, xor_lane_u<B>(x)));
-    else return x;
-}
-
-// Pages in flight per lane: those of the next step besides, or so many more for one loading of the heads' registers
-constexpr int flight_of(bool many) { return many ? 8 : 4; }
-
 struct ScoreArgs {
     PageDims d;
     PageView pv;
@@ -77,116 +53,142 @@ struct ScoreArgs {
     uint32_t *keys;
 };
 
-// grid (parts of a sequence's pages, problems).  HB heads at a time, in registers; more heads (MANY) are more walks over the pages in
-// flight.
-template <bool BF16, int LP, int HB, bool MANY>
-__global__ void __launch_bounds__(NT, 2)
+// How page_scores_kernel spreads its work: a row's pieces over LP lanes, NP per lane, and HS sets of four heads
+template <bool BF16, int LP, int NP, int HS> struct Spread {
+    static constexpr int E = Piece<BF16>::N, PAGES = 64 / LP;  // pages of a wavefront's matrix instruction
+    static constexpr int FLIGHT = NP < 2 ? 2 : 1;              // of those at a time, while as many are on their way (4: 30.2 us for 28.9, 8: 32)
+    static constexpr bool IN_LDS = HS * NP * E > 16;           // the heads' elements do not fit the registers
+    static constexpr int WG_PAGES = NT / 64 * PAGES * FLIGHT;
+};
+
+// grid (problems, parts of a sequence's pages): the heads' bounds of a page lie side by side and are read at one time
+template <bool BF16, int LP, int NP, int HS>
+__global__ void __launch_bounds__(NT, SCORE_WGS)
 page_scores_kernel(ScoreArgs a)
 {
     using Pc = Piece<BF16>;
-    constexpr int E = Pc::N, ELT = 16 / E, PW = 64 / LP, S = HB < LP ? HB : LP, FLIGHT = flight_of(MANY);
+    using Sp = Spread<BF16, LP, NP, HS>;
+    constexpr int E = Pc::N, ELT = 16 / E, FLIGHT = Sp::FLIGHT, BLOCKS = LP / 4;              // BLOCKS: of the four small products, with one page's pieces
     const PageDims &d = a.d;
-    const int p = blockIdx.y, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % LP, place = lane / LP;
+    const int p = blockIdx.x, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // as operand: a page's or a head's number within four, block, place in the inner dimension; a result has the page in the place of the latter
+    const int four = lane & 3, block = lane >> 2 & 3, inner = lane >> 4;
+    const int c = block % BLOCKS + BLOCKS * inner, place = four + 4 * (block / BLOCKS), result_place = inner + 4 * (block / BLOCKS);
     const int n = (rows_of(d, a.pv.lengths, s) + d.page - 1) >> d.shift;
-    const bool mine = c * E < d.D;                             // lanes behind the row's end are padding
     const int64_t row = (int64_t)d.D * ELT;
-    const char *q = a.q + (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G) * row + c * 16;
-    __shared__ __attribute__((aligned(16))) char q_sh[MANY ? 16 * 256 * ELT : 16];         // all heads: read for every walk, beside loads in flight
-    const char *bounds = a.pv.bounds + ((int64_t)layer * d.n_pages * d.Hkv + head) * 2 * row + (mine ? c : 0) * 16;
-    double up[HB][E], down[HB][E];                             // q+ and q-
-    auto load_heads = [&](int g0) {
+    const bool padded = d.D < LP * NP * E;
+    auto mine = [&](int j) { return (c + LP * j) * E < d.D; }; // lanes behind the row's end are padding
+    const char *q = a.q + (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G) * row;
+    const char *bounds = a.pv.bounds + ((int64_t)layer * d.n_pages * d.Hkv + head) * 2 * row;
+    int at[NP];
 #pragma unroll
-        for (int g = 0; g < HB; ++g) {
-            u32x4 x{0, 0, 0, 0};
-            if (mine && g0 + g < d.G) x = *reinterpret_cast<const u32x4 *>(MANY ? q_sh + c * 16 + (g0 + g) * (int)row : q + (g0 + g) * row);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float v = Pc::value(x, e);
-                up[g][e] = (double)(v < 0.f ? 0.f : v);        // what is no number stays one
-                down[g][e] = (double)(v < 0.f ? v : 0.f);
-            }
-        }
-    };
-    struct Flight { int id[FLIGHT]; u32x4 lo[FLIGHT], hi[FLIGHT]; };
+    for (int j = 0; j < NP; ++j) at[j] = mine(j) ? (c + LP * j) * 16 : 0;
+    struct Flight { int id[FLIGHT]; u32x4 lo[FLIGHT][NP], hi[FLIGHT][NP]; };
     // Nothing is loaded behind a branch (what does not exist is replaced by what does, and not used): the compiler could not count
     // the loads in flight there.
     auto load_ids = [&](int i0, int (&id)[FLIGHT]) {
 #pragma unroll
-        for (int u = 0; u < FLIGHT; ++u) id[u] = page_at(d, a.pv.table, s, min(i0 + u * PW + place, n - 1));
+        for (int u = 0; u < FLIGHT; ++u) id[u] = page_at(d, a.pv.table, s, min(i0 + u * Sp::PAGES + place, n - 1));
     };
     auto load_bounds = [&](Flight &f) {
 #pragma unroll
         for (int u = 0; u < FLIGHT; ++u) {
             const char *b = bounds + (int64_t)max(f.id[u], 0) * d.Hkv * 2 * row;
-            f.lo[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(b));
-            f.hi[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(b + row));
+#pragma unroll
+            for (int j = 0; j < NP; ++j) {
+                f.lo[u][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(b + at[j]));
+                f.hi[u][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(b + row + at[j]));
+            }
         }
     };
-    if constexpr (MANY) {
-        for (int i = threadIdx.x * 16; i < d.G * (int)row; i += NT * 16)
-            *reinterpret_cast<u32x4 *>(q_sh + i) = *reinterpret_cast<const u32x4 *>(q - c * 16 + i);
-        __syncthreads();
-    }
-    const int step = gridDim.x * (NT / 64) * PW * FLIGHT, start = (blockIdx.x * (NT / 64) + wave) * PW * FLIGHT;
-    if (start >= n) return;
+    // q+ and q- of the heads; those behind the last are the last again
+    typedef double pair __attribute__((ext_vector_type(2)));
+    auto load_heads = [&](int set, int j, auto &&put) {        // put(e, {q+, q-})
+        u32x4 x{0, 0, 0, 0};
+        if (mine(j)) x = *reinterpret_cast<const u32x4 *>(q + min(4 * set + four, d.G - 1) * row + (c + LP * j) * 16);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float v = Pc::value(x, e);
+            put(e, pair{(double)(v < 0.f ? 0.f : v), (double)(v < 0.f ? v : 0.f)});            // what is no number stays one
+        }
+    };
+    __shared__ pair q_sh[Sp::IN_LDS ? HS * NP * E * 64 : 1];   // [set][piece][element][lane]
+    pair q_own[Sp::IN_LDS ? 1 : HS * NP * E];
+    const int step = gridDim.y * Sp::WG_PAGES, start = (blockIdx.y * (NT / 64) + wave) * Sp::PAGES * FLIGHT;
+    if ((int)(blockIdx.y * Sp::WG_PAGES) >= n) return;
     Flight now, next;
     load_ids(start, now.id);
-    if constexpr (!MANY) load_ids(start + step, next.id);
+    load_ids(start + step, next.id);
     load_bounds(now);
-    if constexpr (!MANY) load_heads(0);
+    if constexpr (Sp::IN_LDS) {
+        for (int i = wave; i < HS * NP; i += NT / 64)
+            load_heads(i / NP, i % NP, [&](int e, pair x) { q_sh[(i * E + e) * 64 + lane] = x; });
+        __syncthreads();
+    } else {
+#pragma unroll
+        for (int i = 0; i < HS * NP; ++i) load_heads(i / NP, i % NP, [&](int e, pair x) { q_own[i * E + e] = x; });
+    }
     for (int i0 = start; i0 < n; i0 += step) {
-        uint32_t key[FLIGHT];
         int later[FLIGHT];
-        if constexpr (!MANY) {
-            load_bounds(next);
-            load_ids(i0 + 2 * step, later);
-        } else load_ids(i0 + step, later);
+        load_bounds(next);
+        load_ids(i0 + 2 * step, later);
+        if (padded) {
+#pragma unroll
+            for (int j = 0; j < NP; ++j)
+                if (!mine(j)) {
+#pragma unroll
+                    for (int u = 0; u < FLIGHT; ++u) now.lo[u][j] = now.hi[u][j] = u32x4{0, 0, 0, 0};
+                }
+        }
+        double x[FLIGHT][HS];
+#pragma unroll
+        for (int u = 0; u < FLIGHT; ++u)
+#pragma unroll
+            for (int g = 0; g < HS; ++g) x[u][g] = 0.0;
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                double l[FLIGHT], h[FLIGHT];
+                if constexpr (Sp::IN_LDS) asm volatile("" ::: "memory");                      // not read sooner: all of them do not fit
+#pragma unroll
+                for (int u = 0; u < FLIGHT; ++u) { l[u] = (double)Pc::value(now.lo[u][j], e); h[u] = (double)Pc::value(now.hi[u][j], e); }
+#pragma unroll
+                for (int g = 0; g < HS; ++g) {
+                    const int i = (g * NP + j) * E + e;
+                    const pair w = Sp::IN_LDS ? q_sh[i * 64 + lane] : q_own[Sp::IN_LDS ? 0 : i];
+#pragma unroll
+                    for (int u = 0; u < FLIGHT; ++u) x[u][g] = __builtin_amdgcn_mfma_f64_4x4x4f64(h[u], w[0], x[u][g], 0, 0, 0);
+#pragma unroll
+                    for (int u = 0; u < FLIGHT; ++u) x[u][g] = __builtin_amdgcn_mfma_f64_4x4x4f64(l[u], w[1], x[u][g], 0, 0, 0);
+                }
+            }
+        // read before any branch, see the products of the decode kernel
+        uint32_t key[FLIGHT];
 #pragma unroll
         for (int u = 0; u < FLIGHT; ++u) {
             key[u] = 0;
-            if (!mine) now.lo[u] = now.hi[u] = u32x4{0, 0, 0, 0};
-        }
-        for (int g0 = 0; g0 < (MANY ? d.G : 1); g0 += HB) {
-            if constexpr (MANY) {
-                load_heads(g0);
 #pragma unroll
-                for (int u = 0; u < FLIGHT; ++u)               // converted anew for every walk: in fp64 they would not fit the registers
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(now.lo[u][i]), "+v"(now.hi[u][i]));
+            for (int g = 0; g < HS; ++g) {
+                double y = x[u][g];
+                if constexpr (BLOCKS >= 2) y += xor_lane_d<4>(y);
+                if constexpr (BLOCKS >= 4) y += xor_lane_d<8>(y);
+                key[u] = max(key[u], y == y ? ordered_key((float)y) : NOT_A_NUMBER);
             }
-#pragma unroll
-            for (int u = 0; u < FLIGHT; ++u) {
-                double x[HB];
-#pragma unroll
-                for (int g = 0; g < HB; ++g) x[g] = 0.0;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const double l = (double)Pc::value(now.lo[u], e), h = (double)Pc::value(now.hi[u], e);
-#pragma unroll
-                    for (int g = 0; g < HB; ++g) x[g] = fma(up[g][e], h, fma(down[g][e], l, x[g]));
-                }
-                sum_lanes<1, S, LP, HB>(x);
-#pragma unroll
-                for (int j = 0; j < HB / S; ++j)
-                    if (g0 + c % S + S * j < d.G) key[u] = max(key[u], x[j] == x[j] ? ordered_key((float)x[j]) : NOT_A_NUMBER);
-            }
+            key[u] = max(key[u], xor_lane_u<1>(key[u]));
+            key[u] = max(key[u], xor_lane_u<2>(key[u]));
+            const uint64_t none = __ballot(now.id[u] < 0) >> (inner + 4 * block);             // the result's page in the lanes of operands
+            if (none & 1) key[u] = ordered_key(-INFINITY);
         }
 #pragma unroll
         for (int u = 0; u < FLIGHT; ++u) {
-            const int i = i0 + u * PW + place;
-            const uint32_t x = most_of_lanes<1, S>(key[u]);
-            if (c == 0 && i < n) a.keys[(int64_t)p * a.stride + i] = now.id[u] >= 0 ? x : ordered_key(-INFINITY);
+            const int i = i0 + u * Sp::PAGES + result_place;
+            if (four == 0 && block % BLOCKS == 0 && i < n) a.keys[(int64_t)p * a.stride + i] = key[u];
         }
-        if constexpr (!MANY) {
-            now = next;
+        now = next;
 #pragma unroll
-            for (int u = 0; u < FLIGHT; ++u) next.id[u] = later[u];
-        } else {
-#pragma unroll
-            for (int u = 0; u < FLIGHT; ++u) now.id[u] = later[u];
-            load_bounds(now);
-        }
+        for (int u = 0; u < FLIGHT; ++u) next.id[u] = later[u];
     }
 }
 
@@ -341,11 +343,23 @@ pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, 
 
 int key_stride(const PageDims &d) { return (d.max_pages + 3) & ~3; }
 
-template <bool BF16, int LP>
-void (*scores_for(int G))(ScoreArgs)
+struct Scores { void (*fn)(ScoreArgs); int pages; };           // pages: of a workgroup at a time
+
+template <bool BF16, int LP, int NP> Scores scores_for(int G)
 {
-    return G == 1 ? page_scores_kernel<BF16, LP, 1, false> : G == 2 ? page_scores_kernel<BF16, LP, 2, false>
-         : G <= 4 ? page_scores_kernel<BF16, LP, 4, false> : page_scores_kernel<BF16, LP, 4, true>;
+    if (G <= 4) return {page_scores_kernel<BF16, LP, NP, 1>, Spread<BF16, LP, NP, 1>::WG_PAGES};
+    if (G <= 8) return {page_scores_kernel<BF16, LP, NP, 2>, Spread<BF16, LP, NP, 2>::WG_PAGES};
+    return {page_scores_kernel<BF16, LP, NP, 4>, Spread<BF16, LP, NP, 4>::WG_PAGES};
+}
+
+template <bool BF16> Scores scores_for(int G, int pieces)
+{
+    if (pieces <= 4) return scores_for<BF16, 4, 1>(G);
+    if (pieces <= 8) return scores_for<BF16, 8, 1>(G);
+    if (pieces <= 16) return scores_for<BF16, 16, 1>(G);
+    if constexpr (!BF16)                                       // no bf16 head has more than 32
+        if (pieces > 32) return scores_for<BF16, 16, 4>(G);
+    return scores_for<BF16, 16, 2>(G);
 }
 
 }  // namespace
@@ -363,18 +377,9 @@ hipError_t launch_select_pages(const PageDims &d, const void *q, const PageView 
     a.keys = static_cast<uint32_t *>(ws);
     if (d.max_pages > n_pick) {                                // otherwise every list is whole
         const int pieces = d.D * elt_bytes(d) / 16;
-        int lp = 1;
-        while (lp < pieces) lp *= 2;
-        const bool bf = d.dtype == SABLOCK_BF16;
-        void (*fn)(ScoreArgs) = nullptr;
-        // bf16 rows of up to 32 pieces, fp32 rows of 2 to 64: twice as many for the same heads
-#define SABLOCK_SCORES(LV) if (bf && lp == LV) fn = scores_for<true, LV>(d.G); if (!bf && lp == 2 * LV) fn = scores_for<false, 2 * LV>(d.G);
-        SABLOCK_SCORES(1) SABLOCK_SCORES(2) SABLOCK_SCORES(4) SABLOCK_SCORES(8) SABLOCK_SCORES(16) SABLOCK_SCORES(32)
-#undef SABLOCK_SCORES
-        if (!fn) return hipErrorInvalidValue;
-        const int pages = NT / lp * flight_of(d.G > 4);                    // of a workgroup at a time
-        const int parts = std::max(1, std::min((d.max_pages + pages - 1) / pages, (SCORE_WGS * d.cus + d.P - 1) / d.P));
-        hipLaunchKernelGGL(fn, dim3(parts, d.P), dim3(NT), 0, st, a);
+        const Scores f = d.dtype == SABLOCK_BF16 ? scores_for<true>(d.G, pieces) : scores_for<false>(d.G, pieces);
+        const int parts = std::max(1, std::min((d.max_pages + f.pages - 1) / f.pages, (SCORE_WGS * d.cus + d.P - 1) / d.P));
+        hipLaunchKernelGGL(f.fn, dim3(d.P, parts), dim3(NT), 0, st, a);
     }
     const int run = (d.max_pages + PICK_NT - 1) / PICK_NT;     // per thread
     const auto pick = run <= 4 ? pick_pages_kernel<4> : run <= 8 ? pick_pages_kernel<8> : run <= 16 ? pick_pages_kernel<16> : pick_pages_kernel<0>;

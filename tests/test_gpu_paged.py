@@ -479,7 +479,8 @@ def _ref_select(c, q, pick, first, last):
 
 
 @pytest.mark.parametrize("G,D,dtype,page", [(1, 32, "bf16", 16), (4, 128, "bf16", 16), (7, 96, "bf16", 32), (8, 256, "bf16", 16), (16, 64, "bf16", 16), (4, 128, "f32", 16),
-                                           (5, 40, "f32", 16), (9, 256, "f32", 16), (3, 8, "bf16", 16), (2, 88, "bf16", 16)])
+                                           (5, 40, "f32", 16), (9, 256, "f32", 16), (3, 8, "bf16", 16), (2, 88, "bf16", 16),
+                                             (16, 16, "f32", 16), (12, 224, "bf16", 64), (6, 128, "bf16", 32), (13, 32, "f32", 16), (7, 200, "f32", 16)])
 @pytest.mark.parametrize("pick,first,last", [(1, 0, 0), (1, 0, 1), (8, 1, 1), (64, 2, 3), (300, 0, 1)])
 def test_select(torch_cuda, G, D, dtype, page, pick, first, last):  # noqa: F811
     torch = torch_cuda

@@ -19,7 +19,7 @@ def _kernels(text):
 
 def test_no_kernel_spills(assembly):
     kernels = {n: k for text in assembly.values() for n, k in _kernels(text).items()}
-    assert len(kernels) == (2 + 8) + (48 + 2) + (2 * 6 * 4 + 4)
+    assert len(kernels) == (2 + 8) + (48 + 2) + (3 * (4 + 5) + 4)
     assert not any(k["private_segment_fixed_size"] for k in kernels.values())
 
 
@@ -43,13 +43,14 @@ def _registers(operand):
     return {int(a) for a in re.findall(r"\bv(\d+)\b", operand)} | {r for a, b in re.findall(r"\bv\[(\d+):(\d+)\]", operand) for r in range(int(a), int(b) + 1)}
 
 
-def test_matrix_results_are_waited_for_on_every_path(assembly):
+@pytest.mark.parametrize("source,kernel,least", [("paged_decode.hip", "decode_paged_kernel", 1000), ("paged_select.hip", "page_scores_kernel", 1000)])
+def test_matrix_results_are_waited_for_on_every_path(assembly, source, kernel, least):
     # An instruction of another kind that touches a product's result has to come as many wait states behind it as the compiler leaves
-    # between them within a block: 8 behind the bf16 products, 10 behind the fp32 ones.  Where a branch came between, it was found to
+    # between them within a block: 8 behind the bf16 products, 10 behind the fp32 ones, 6 behind the small fp64 ones.  Where a branch came between, it was found to
     # leave fewer, down to 1, and old values were read.
-    states_behind = {"v_mfma_f32_16x16x32_bf16": 8, "v_mfma_f32_16x16x16_bf16": 8, "v_mfma_f32_16x16x4_f32": 10}
+    states_behind = {"v_mfma_f32_16x16x32_bf16": 8, "v_mfma_f32_16x16x16_bf16": 8, "v_mfma_f32_16x16x4_f32": 10, "v_mfma_f64_4x4x4_4b_f64": 6}
     products = 0
-    for name, body in re.findall(r"^(\S*decode_paged_kernel\S*):.*?\n(.*?)^\.Lfunc_end", assembly["paged_decode.hip"], re.S | re.M):
+    for name, body in re.findall(rf"^(\S*{kernel}\S*):.*?\n(.*?)^\.Lfunc_end", assembly[source], re.S | re.M):
         code, labels = [], {}
         for line in body.split("\n"):
             label = re.match(r"(\.LBB\w+):", line)
@@ -85,4 +86,4 @@ def test_matrix_results_are_waited_for_on_every_path(assembly):
                 else:
                     assert not (result & _registers(x)), f"{name}: {o} {x} {states} states behind {op} {arg}"
                 ways += [(n, states + (int(x) + 1 if o == "s_nop" else 1)) for n in following(j)]
-    assert products > 1000
+    assert products > least
