@@ -26,9 +26,9 @@
 //
 // What bounds it: HBM.  4 x 8 heads x 131 072 rows of 128 bf16 elements (2.15 GB, four query heads or eight): 325-340 us, 6.3-6.6 TB/s,
 // what the dense cache's kernel reaches over the same rows (330 us); every byte fetched once; the matrix pipe is busy 8 % of
-// the time, the vector pipe 14 %.  Few rows: the chain of dependent loads (length, table, rows), and that of the second kernel, 10.3 us
+// the time, the vector pipe 14 %.  Few rows: the chain of dependent loads (length, table, rows), and that of the second kernel, 9.85 us
 // in all (8 heads x 1 056 rows); what does not depend on the rows is kept short, the code too, which comes cold from memory (with
-// the dealing in 64 bits 10.8).  A wavefront holds one step's K and one step's V in flight, the next one's as soon as the products
+// the dealing in 64 bits 0.5 more).  A wavefront holds one step's K and one step's V in flight, the next one's as soon as the products
 // have taken their operands; a third workgroup per compute unit, spilling, was slower (375 us), ordinary loads in place of non-temporal ones
 // as well (378).
 #include "sablock_internal.h"
@@ -509,16 +509,26 @@ decode_paged_kernel(DecodePagedArgs a)
     }
 }
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <int M> __device__ __forceinline__ float over_lanes(float x, bool take_max)
+{
+    if constexpr (M < 64) {
+        const float y = xor_lane<M>(x);
+        return over_lanes<2 * M>(take_max ? fmaxf(x, y) : x + y, take_max);
+    } else return x;
+}
+
 // grid (G, problems) of the long ones: the pieces' weights first, then their weighted sum, four elements per thread, the pieces dealt out to groups of threads
 constexpr int MERGE_T = 256, MAX_PIECES = 1024, EARLY = 2;
 template <int STEP>
 __global__ void __launch_bounds__(MERGE_T)
 decode_paged_merge_kernel(DecodePagedArgs a)
 {
-    __shared__ float w_sh[MAX_PIECES], red[2 * (MERGE_T / 64)];
+    __shared__ float w_sh[MERGE_T / 64][MAX_PIECES];           // every wavefront forms all weights, no barrier: 8 heads x 1 056 rows 10.3 -> 9.85 us in all
     __shared__ f32x4 sum[MERGE_T];
     const PageDims &d = a.d;
     const int g = blockIdx.x, p = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    float *w = w_sh[tid >> 6];
     const int seq = seq_of_problem(d, p), n = shared_steps_of<STEP>(a, seq);
     if (n == 0) return;                                        // a workgroup's alone
     float *out = a.out + ((((int64_t)seq * d.n_layers + layer_of_problem(d, p)) * d.Hq) + head_of_problem(d, p) * d.G + g) * d.D;
@@ -535,34 +545,27 @@ decode_paged_merge_kernel(DecodePagedArgs a)
     f32x4 early[EARLY];
 #pragma unroll
     for (int j = 0; j < EARLY; ++j) early[j] = part(group + j * groups);
-    float m = -FLT_MAX;
-    for (int i = tid; i < pieces; i += MERGE_T) m = fmaxf(m, a.weights[slot(i) * 2]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (lane == 0) red[tid >> 6] = m;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < MERGE_T / 64; ++i) m = fmaxf(m, red[i]);
+    auto weight = [&](int i) { return *reinterpret_cast<const f32x2 *>(a.weights + slot(min(i, pieces - 1)) * 2); };
+    f32x2 own = weight(lane);                                  // reference, denominator
+    if (lane >= pieces) own = f32x2{-FLT_MAX, 0.f};
+    float m = own[0];
+    for (int i = lane + 64; i < pieces; i += 64) m = fmaxf(m, weight(i)[0]);
+    m = over_lanes<1>(m, true);
     float den = 0.f;
-    for (int i = tid; i < pieces; i += MERGE_T) {
-        const float f = __builtin_amdgcn_exp2f(a.weights[slot(i) * 2] - m);
-        w_sh[i] = f;
-        den += a.weights[slot(i) * 2 + 1] * f;
+    for (int i = lane; i < pieces; i += 64) {
+        if (i > lane) own = weight(i);
+        w[i] = __builtin_amdgcn_exp2f(own[0] - m);
+        den += own[1] * w[i];
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
-    if (lane == 0) red[MERGE_T / 64 + (tid >> 6)] = den;
-    __syncthreads();
-    den = 0.f;
-#pragma unroll
-    for (int i = 0; i < MERGE_T / 64; ++i) den += red[MERGE_T / 64 + i];
+    den = over_lanes<1>(den, false);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // w: other lanes' stores from here on
     f32x4 t{0.f, 0.f, 0.f, 0.f};
     if (group < groups) {
 #pragma unroll
         for (int j = 0; j < EARLY; ++j)
-            if (group + j * groups < pieces) t += early[j] * w_sh[group + j * groups];
+            if (group + j * groups < pieces) t += early[j] * w[group + j * groups];
 #pragma unroll 4
-        for (int i = group + EARLY * groups; i < pieces; i += groups) t += part(i) * w_sh[i];
+        for (int i = group + EARLY * groups; i < pieces; i += groups) t += part(i) * w[i];
     }
     sum[tid] = t;
     __syncthreads();
