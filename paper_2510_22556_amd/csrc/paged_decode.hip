@@ -115,17 +115,6 @@ __device__ __forceinline__ int shared_steps_of(const DecodePagedArgs &a, int s)
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // the value of one lane, the same one for all
 __device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-// inclusive sums over the lanes, by shifts inside a row of 16 and the rows' ends into the next ones
-__device__ __forceinline__ int scan(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
-    return x;
-}
 __device__ __forceinline__ int quotient(int x, int n) { return (int)((uint32_t)x / (uint32_t)n); }            // neither negative
 
 // How the long problems' steps are dealt out: in runs that are cut at the problems' ends, one per workgroup, where the workgroups are
@@ -160,8 +149,8 @@ struct Places {
                 steps += s < a.d.n_seq ? n : 0;
                 longs += s < a.d.n_seq && n > 0;
             }
-            upto = scan(steps);
-            longs = of_lane(scan(longs), 63);
+            upto = sum_upto_lane(steps);
+            longs = of_lane(sum_upto_lane(longs), 63);
         }
         total = last() * heads;
         const int evenly = upto, all = total, problems = longs * heads;
@@ -186,7 +175,7 @@ struct Places {
         else
             for (int i = 0; i < share; ++i)
                 if (lane * share + i < a.d.n_seq) own += units_of(shared_steps_of<STEP>(a, lane * share + i));
-        upto = a.d.n_seq > 1 ? scan(own) : own;
+        upto = a.d.n_seq > 1 ? sum_upto_lane(own) : own;
         total = last() * heads;
         return total <= a.workgroups;
     }
@@ -203,7 +192,7 @@ struct Places {
             return;
         }
         const int s = first * share + lane, own_steps = lane < share && s < a.d.n_seq ? shared_steps_of<STEP>(a, s) : 0;
-        const int own = units_of(own_steps), inner = scan(own) + at, j = uniform(__ffsll((unsigned long long)__ballot(inner * heads > x)) - 1);
+        const int own = units_of(own_steps), inner = sum_upto_lane(own) + at, j = uniform(__ffsll((unsigned long long)__ballot(inner * heads > x)) - 1);
         seq = first * share + j;
         units = of_lane(own, j);
         n = of_lane(own_steps, j);

@@ -14,7 +14,8 @@
 //       instructions and sums over 16 lanes, 12.3; with 16 query heads, picking and reading with it, 36.3 in place of 46.3.
 //   pick_pages_kernel    a workgroup per problem; the keys stay in registers.  The last key that is taken is found digit by digit, 11 bits
 //       of its distance from the least key at a time (the keys of a problem share their upper bits) until 64 are left, which a wavefront
-//       ranks, and one prefix sum places the pages in order.  8 192 pages: 7.3 us, a chain of a dozen barriers.
+//       ranks, and one prefix sum places the pages in order.  8 192 pages: 5.6 us, a chain of seven barriers and the reads between
+//       them (with lane sums through LDS and nine barriers 6.5).
 #include "sablock_internal.h"
 
 namespace sablock {
@@ -192,14 +193,10 @@ page_scores_kernel(ScoreArgs a)
     }
 }
 
-__device__ __forceinline__ int sum_upto(int x, int lane)       // inclusive, over the lanes
+template <int M> __device__ __forceinline__ uint32_t most_of_lanes(uint32_t x)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(x, o);
-        if (lane >= o) x += u;
-    }
-    return x;
+    if constexpr (M < 64) return most_of_lanes<2 * M>(max(x, xor_lane_u<M>(x)));
+    else return x;
 }
 
 constexpr int DIGIT = 11, BINS = 1 << DIGIT;
@@ -252,8 +249,8 @@ pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, 
     };
     uint32_t least = 0xffffffffu, most = 0;
     ranked([&](uint32_t x, int) { least = min(least, x); most = max(most, x); });
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { least = min(least, (uint32_t)__shfl_xor((int)least, o)); most = max(most, (uint32_t)__shfl_xor((int)most, o)); }
+    least = ~most_of_lanes<1>(~least);
+    most = most_of_lanes<1>(most);
     if (lane == 0) { extreme[wave] = least; extreme[NWV + wave] = most; }
     for (int i = tid; i < BINS; i += PICK_NT) hist[i] = 0;
     if (tid == 0) n_few = 0;
@@ -270,7 +267,7 @@ pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, 
         });
         __syncthreads();
         const int b0 = BINS - 1 - 2 * tid, h0 = hist[b0], h1 = hist[b0 - 1];   // two bins per thread, the largest first
-        const int upto = sum_upto(h0 + h1, lane);
+        const int upto = sum_upto_lane(h0 + h1);
         if (lane == 63) red[wave] = upto;
         __syncthreads();
         int before = upto - h0 - h1;
@@ -281,10 +278,9 @@ pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, 
         hist[b0] = hist[b0 - 1] = 0;
         __syncthreads();
         least += (uint32_t)found[0] << shift;
-        left = found[1];
+        left = found[1];                                       // written again only behind a barrier
         inside = found[2];
         bits = shift;
-        __syncthreads();
     }
     // the last that is taken, in the order of keys and of pages: key `cut`, page `cut_at`
     uint32_t cut = least;
@@ -310,7 +306,7 @@ pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, 
         } else {                                               // all inside are equal
             int eq = 0;
             ranked([&](uint32_t x, int) { eq += x == least; });
-            const int upto = sum_upto(eq, lane);
+            const int upto = sum_upto_lane(eq);
             if (lane == 63) red[wave] = upto;
             __syncthreads();
             int before = upto - eq;
@@ -323,12 +319,11 @@ pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, 
         __syncthreads();
         cut = (uint32_t)found[0];
         cut_at = found[1];
-        __syncthreads();
     }
     auto taken = [&](uint32_t x, int i) { return x > cut || (x == cut && i <= cut_at); };
     int count = max(0, min(to, rest0) - from) + max(0, to - max(from, rest1));
     ranked([&](uint32_t x, int i) { count += taken(x, i); });
-    const int upto = sum_upto(count, lane);
+    const int upto = sum_upto_lane(count);
     if (lane == 63) red[wave] = upto;
     __syncthreads();
     int at = upto - count;

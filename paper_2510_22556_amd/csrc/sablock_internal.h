@@ -181,6 +181,18 @@ __device__ __forceinline__ float xor_lane(float x)
     return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
+// inclusive sums over the lanes, by shifts inside a row of 16 and the rows' ends into the next ones
+__device__ __forceinline__ int sum_upto_lane(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ---- kernel launchers (each returns the hipError_t of its launches) ----
