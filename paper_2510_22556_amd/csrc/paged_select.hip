@@ -1,7 +1,7 @@
 // The pages that a decode step over a paged cache reads when it may not read all: a score per page from the bounds of its keys,
 // then the best of them per KV head.
 //
-//   page_scores_kernel   max(q lo, q hi) is q+ hi + q- lo with q+ = max(q, 0), q- = min(q, 0): two products per element and head,
+//   page_scores_kernel   max(q lo, q hi) is q+ hi + q- lo with q+ = max(q, 0), q- = min(q, 0) (finite lo and hi): two products per element and head,
 //       formed and summed in fp64, on the matrix pipe.  The products of two bf16 values and their sum over a head are exact there (but for
 //       elements some 2^30 apart), so that which of two pages comes first does not hang on the order of a sum.  A matrix
 //       instruction of four products 4 x 4 x 4 has four pages in its rows, four heads in its columns and, in its four inner places
@@ -373,7 +373,7 @@ hipError_t launch_select_pages(const PageDims &d, const void *q, const PageView 
     if (d.max_pages > n_pick) {                                // otherwise every list is whole
         const int pieces = d.D * elt_bytes(d) / 16;
         const Scores f = d.dtype == SABLOCK_BF16 ? scores_for<true>(d.G, pieces) : scores_for<false>(d.G, pieces);
-        const int parts = std::max(1, std::min((d.max_pages + f.pages - 1) / f.pages, (SCORE_WGS * d.cus + d.P - 1) / d.P));
+        const int parts = std::min({(d.max_pages + f.pages - 1) / f.pages, (SCORE_WGS * d.cus + d.P - 1) / d.P, (int)GRID_Y_MOST});
         hipLaunchKernelGGL(f.fn, dim3(d.P, parts), dim3(NT), 0, st, a);
     }
     const int run = (d.max_pages + PICK_NT - 1) / PICK_NT;     // per thread

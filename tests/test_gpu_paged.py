@@ -508,6 +508,43 @@ def test_select_of_equal_scores_and_of_what_is_no_number(torch_cuda):  # noqa: F
     assert c.select(q, 1999, 0, 0)[0].tolist() == [i for i in range(2000) if i != 700]
 
 
+@pytest.mark.parametrize("G,D,dtype", [(3, 64, "bf16"), (16, 96, "bf16"), (5, 128, "f32")])
+def test_select_with_infinite_bounds(torch_cuda, G, D, dtype):  # noqa: F811
+    # infinite, or no number, by the side that the query takes; one page's stay with it, and one head's
+    torch = torch_cuda
+    inf = float("inf")
+    c = Cache(torch, D, [16 * 200, 16 * 200], heads=2, group=G, D=D, dtype=dtype).fill()
+    q = c.normal((2, 1, 2 * G, D))
+    plain = _ref_select(c, q, 20, 1, 1)
+    assert c.select(q, 20, 1, 1).tolist() == plain
+    q[..., 5], q[..., 6] = 1.0, -1.0
+    order = c.table[0, :200].long()
+    for page, e, side, value in ((50, 5, 1, inf), (60, 5, 0, -inf), (70, 6, 0, -inf), (80, 6, 1, inf)):      # inf, NaN, inf, NaN
+        c.bounds[0, order[page], 0, side, e] = value
+    c.bounds[0, order[90], 0, 1, 5] = -inf                                                                   # below all
+    c.bounds[0, order[90], 0, 0, 5] = -1.0
+    got = c.select(q, 4, 0, 0)
+    assert got[0].tolist() == [50, 60, 70, 80] and c.select(q, 2, 0, 0)[0].tolist() == [60, 80]
+    assert 90 not in c.select(q, 199, 0, 0)[0].tolist()
+    assert got[1:].tolist() == _ref_select(c, q, 4, 0, 0)[1:]
+
+
+def test_select_planned_for_more_workgroups_than_a_grid_has_places(torch_cuda):  # noqa: F811
+    # the most compute units that a cache may name, and a table with room for 2.2 million pages
+    torch = torch_cuda
+    from paper_2510_22556_amd import binding as B
+
+    c = Cache(torch, 3, [16 * 300], heads=1, group=2, D=128).fill()
+    q = c.normal((1, 1, 2, 128))
+    table = torch.full((1, 2_200_000), -1, dtype=torch.int32, device="cuda")
+    table[:, : c.table.shape[1]] = c.table
+    pages = B.make_pages(c.k_pool, c.v_pool, table, 2, compute_units=65536)
+    ws = torch.empty((B.sablock_select_pages_workspace_bytes(pages),), dtype=torch.uint8, device="cuda")
+    lst = torch.empty((1, 20), dtype=torch.int32, device="cuda")
+    B.sablock_select_pages(pages, q, c.bounds, table, c.lengths, 20, lst, ws)
+    assert lst.tolist() == _ref_select(c, q, 20, 1, 1)
+
+
 @pytest.mark.parametrize("rows", [65536 * 16 + 1, 20000 * 16, 5000 * 16 + 7, 12001 * 16])
 def test_select_among_many_pages(torch_cuda, rows):  # noqa: F811
     torch = torch_cuda
