@@ -376,8 +376,9 @@ SABLOCK_API sablock_status sablock_decode_attention(const sablock_shape *shape, 
  *   them where they are given, sablock_select_pages reads them.  A page's bounds mean something once its row 0 was written
  *   with them.
  * Device data: table entries outside [0, n_pages) name no page: what would be written there is dropped, their rows are
- *   skipped by attention and their scores are -infinity.  Lengths count as 0 .. max_pages * page_size.  Different entries within
- *   the sequences' lengths may name one page (a shared prefix); then no call may write to it.
+ *   skipped by attention and their scores are -infinity.  Rows behind max_pages * page_size have no page either, and negative lengths
+ *   count as 0: what reads the cache takes lengths as 0 .. max_pages * page_size.  Different entries within the sequences' lengths may
+ *   name one page (a shared prefix); then no call may write to it.
  * Limits: n_seq <= 4096, n_seq * n_layers * n_kv_heads <= 65535, page_size a power of two in [16, 256],
  *   max_pages * page_size <= 2^30; UNSUPPORTED beyond.  The pools are 16-byte aligned, strides (in elements) multiples of 8, [3] at least head_dim;
  *   the stride of an axis with one entry is not looked at. */
@@ -432,10 +433,12 @@ typedef struct {
  *   q, q_out    both or neither; q_out [n_seq][n_layers][n_q_heads][n_new][D] dense, of the dtype; it may not overlap q
  *   counts      nullable (every sequence has n_new), or [n_seq] int32, taken as 0 .. n_new and at most lengths[s]; rows of
  *               q_out and of the pools that belong to no token stay as they are
+ *   lengths     not bounded by the table here: the tokens whose rows lie behind max_pages * page_size are dropped, the rows in front of
+ *               them stay as they are, and q of every token is rotated
  *   positions   [n_seq] int32, of each sequence's first new token; may be NULL where R = 0, as may inv_freq
  *   inv_freq    [R/2] fp32, radians per position
  *   bounds      nullable; those of the touched pages are extended by the new rows (begun, where row 0 is among them)
- * Two sequences may not add rows to one page. */
+ * Two sequences may not add rows to one page.  INVALID_ARG if n_new is more than max_pages * page_size. */
 SABLOCK_API sablock_status sablock_append_paged(const sablock_pages *pages, const sablock_new_tokens *tokens,
                                     const void *q /* nullable */, const void *k, const void *v,
                                     const int32_t *counts /* nullable */, const int32_t *positions, const float *inv_freq,

@@ -204,13 +204,15 @@ append_paged_kernel(AppendArgs a)
     __shared__ __attribute__((aligned(16))) float2 turn[ONE ? 128 : ANGLES];               // cosine, sine
     const PageDims &d = a.d;
     const int s = blockIdx.y / d.n_layers, layer = blockIdx.y - s * d.n_layers, tid = threadIdx.x;
-    const int len = rows_of(d, a.pv.lengths, s);
+    // Not rows_of: behind a full table the new tokens are rows that no page holds, not the last ones that have a page.  A length that leaves
+    // them all there is as good as any larger one.
+    const int len = (int)min((uint32_t)max(a.pv.lengths[s], 0), ((uint32_t)d.max_pages << d.shift) + a.t.n_new);
     const int count = min(a.counts ? min(max(a.counts[s], 0), a.t.n_new) : a.t.n_new, len);
     const int first = len - count, page = (first >> d.shift) + (int)blockIdx.x;
     if ((int64_t)page << d.shift >= len) return;
-    const int begin = max(first, page << d.shift), end = min(len, (page + 1) << d.shift);
+    const int page_begin = page << d.shift, begin = max(first, page_begin), end = page_begin + min(len - page_begin, d.page);
     if (begin >= end) return;
-    const int id = page_at(d, a.pv.table, s, page);
+    const int id = page < d.max_pages ? page_at(d, a.pv.table, s, page) : -1;
     // K and V of a page that does not exist go nowhere
     const int slot0 = id < 0 ? max((int)blockIdx.z * a.per, 2 * d.Hkv) : blockIdx.z * a.per, slot_end = min(a.slots, ((int)blockIdx.z + 1) * a.per);
     if (slot0 >= slot_end) return;
@@ -235,7 +237,7 @@ append_paged_kernel(AppendArgs a)
     const int angle_step = half ? NT / half : 1, pair = half ? tid % half : 0, angle_tok = half ? tid / half : angle_step;
     double turns_per = 0.0;
     if (angle_tok < angle_step) turns_per = (double)a.inv_freq[pair] * 0.15915494309189535;
-    for (int t0 = begin; t0 < end; t0 += a.tile) {
+    for (int t0 = begin;; t0 += a.tile) {
         const int n = min(a.tile, end - t0), rows = B * a.groups, batches = (n + rows - 1) / rows;
         u32x4 x[B];
         auto load = [&](int base, int b, u32x4 (&x)[B]) {
@@ -350,6 +352,7 @@ append_paged_kernel(AppendArgs a)
             base = next_base;
             bt = next_bt;
         }
+        if (end - t0 <= a.tile) break;                         // in front of the step, which may pass 2^31
     }
 }
 
