@@ -12,7 +12,8 @@ import ctypes
 import os
 import struct
 from dataclasses import dataclass
-from typing import Optional, Sequence, Tuple
+from functools import lru_cache
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsablock.so")
@@ -141,29 +142,75 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device: Optional[int] = None) -> Optional[int]:
+    """Handle of the stream, or of the current one of the device (None = the current device)."""
     if stream is None:
         # the handle alone: torch.cuda.current_stream() builds an object around it, 2.8 us
-        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device()) or None
+        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device() if device is None else device) or None
     return stream.cuda_stream or None
 
 
 def _pointers(*tensors):
-    """Device pointers (None stays) of tensors that are all on the current device: another one's, or the host's, the kernels could not
+    """The current device, and device pointers (None stays) of tensors that are all on it: another one's, or the host's, the kernels could not
     follow."""
-    at = {t.get_device() for t in tensors if t is not None}
-    if len(at) != 1 or -1 in at:
-        raise ValueError(f"tensors on {[str(t.device) for t in tensors if t is not None]}: the calls take device memory, of one device")
-    if at != {_torch.cuda.current_device()}:
-        raise ValueError(f"tensors on cuda:{at.pop()} while cuda:{_torch.cuda.current_device()} is the current device")
-    return [None if t is None else t.data_ptr() for t in tensors]
+    device, pointers = None, [None]
+    for t in tensors:
+        if t is None:
+            pointers.append(None)
+            continue
+        at = t.get_device()
+        if at != device:
+            if at < 0 or device is not None:
+                raise ValueError(f"tensors on {[str(t.device) for t in tensors if t is not None]}: the calls take device memory, of one device")
+            device = at
+        pointers.append(t.data_ptr())
+    current = _torch._C._cuda_getDevice()      # torch.cuda.current_device() asks first whether the device is initialised; with a tensor there it is
+    if device != current:
+        raise ValueError(f"tensors on cuda:{device} while cuda:{current} is the current device")
+    pointers[0] = device
+    return pointers
 
 
 def _dense(dtype, n: int, *tensors):
     """Dense tensors of at least n elements: what the calls index without strides."""
-    for t in tensors:
+    _all_dense(*[(dtype, n, t) for t in tensors])
+
+
+def _all_dense(*wanted):
+    for dtype, n, t in wanted:
         if t is not None and (t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
             raise ValueError(f"need a dense {dtype} tensor of at least {n} elements, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
+
+class _Extent(NamedTuple):
+    """Where a call looks in a tensor ``[.., .., .., .., D]`` that it indexes by a descriptor."""
+
+    what: str
+    sizes: Tuple[int, ...]
+    steps: Tuple[int, ...]
+    dense: int                                 # elements, if the steps are those of a dense tensor
+
+
+def _extent(what: str, sizes, steps) -> _Extent:
+    dense = 1
+    for n, step in zip(reversed(sizes), reversed(steps)):
+        dense = dense * n if n == 1 or step == dense else 0
+    return _Extent(what, tuple(sizes), tuple(steps), dense)
+
+
+def _strided(dtype, *wanted):
+    """Tensors that hold an extent: of the type and as dense as it (how a dense one is cut into axes is not looked at), or as long on every axis and with
+    the same steps on those of more than one entry.  Of another number of axes: memory that reaches as far."""
+    for t, (what, sizes, steps, dense) in wanted:
+        if t.dtype is dtype and (t.numel() >= dense and t.is_contiguous() if dense else t.shape == sizes and t.stride() == steps):
+            continue
+        if t.dim() == 5:
+            ok = all(m >= n for m, n in zip(t.shape, sizes)) and all(n <= 1 or a == b for n, a, b in zip(sizes, t.stride(), steps))
+        else:
+            last = sum((n - 1) * max(a, 0) for n, a in zip(sizes, steps))
+            ok = last < t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if t.dtype is not dtype or not ok:
+            raise ValueError(f"{what}: the descriptor says {dtype} {sizes} with strides {steps}, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
 def make_shape(q, k, v=None, **tuning) -> CShape:
@@ -416,7 +463,7 @@ def make_pages(k_pool, v_pool, page_table, n_q_heads: int, compute_units: int = 
 
 def make_new_tokens(k, v, q=None, rotary_dim: Optional[int] = None, interleaved: bool = False) -> CNewTokens:
     """Descriptor of the new tokens of an append: ``k, v [n_seq, n_layers, Hkv, n_new, D]``, ``q [n_seq, n_layers, Hq, n_new, D]``, any
-    strides on the four outer axes; ``rotary_dim`` None = the whole head."""
+    strides on the four outer axes; ``rotary_dim`` None = the whole head.  Without ``q`` it describes appends without queries."""
     assert k.dim() == 5 and v.shape == k.shape and k.stride(-1) == 1 and v.stride(-1) == 1 and k.dtype == v.dtype
     assert q is None or (q.dim() == 5 and q.dtype == k.dtype and q.stride(-1) == 1 and (q.shape[:2] + q.shape[3:]) == (k.shape[:2] + k.shape[3:]))
     t = CNewTokens()
@@ -427,48 +474,78 @@ def make_new_tokens(k, v, q=None, rotary_dim: Optional[int] = None, interleaved:
     return t
 
 
-_PAGES_INTS = struct.Struct("9i")              # n_seq .. max_pages: one read, a structure's fields one by one cost as much as the launch
+class _Layout(NamedTuple):
+    """What the kernels make of a cache's descriptor."""
+
+    dtype: object
+    n_seq: int
+    max_pages: int
+    k_pool: _Extent
+    v_pool: _Extent
+    problems: int
+    queries: int                               # elements of one query per head
+    bounds: int                                # elements
 
 
-def _cache_sizes(c: CPages):
-    """Type of a cache's elements, sequences, problems, entries of the page table, elements of the bounds and of one query per head."""
-    n_seq, n_layers, n_q_heads, n_kv_heads, head_dim, dtype, _, n_pages, max_pages = _PAGES_INTS.unpack_from(c)
-    d = n_layers * head_dim
-    return (_torch.float32 if dtype == SABLOCK_F32 else _torch.bfloat16, n_seq, n_seq * n_layers * n_kv_heads, n_seq * max_pages,
-            2 * d * n_pages * n_kv_heads, d * n_seq * n_q_heads)
+def _dtype_of(code: int):
+    return _torch.float32 if code == SABLOCK_F32 else _torch.bfloat16
+
+
+# By the descriptors' contents: their fields read one by one would cost a call as much as the launch
+@lru_cache(256)
+def _cache_layout(pages: bytes) -> _Layout:
+    n_seq, n_layers, n_q_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_pages, _, _, _, *steps = struct.unpack_from("12i8q", pages)
+    sizes = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+    return _Layout(_dtype_of(dtype), n_seq, max_pages, _extent("K pool", sizes, (*steps[:4], 1)), _extent("V pool", sizes, (*steps[4:], 1)),
+                   n_seq * n_layers * n_kv_heads, n_seq * n_layers * n_q_heads * head_dim, 2 * n_layers * n_pages * n_kv_heads * head_dim)
+
+
+@lru_cache(256)
+def _tokens_layout(pages: bytes, tokens: bytes):
+    """The cache's layout, new tokens per sequence, extents of q, k and v, elements of the angles' frequencies."""
+    n_seq, n_layers, n_q_heads, n_kv_heads, head_dim = struct.unpack_from("5i", pages)
+    n_new, rotary_dim, _, _, *steps = struct.unpack_from("4i12q", tokens)
+    sizes = (n_seq, n_layers, n_kv_heads, n_new, head_dim)
+    return (_cache_layout(pages), n_new, _extent("q", (n_seq, n_layers, n_q_heads, n_new, head_dim), (*steps[:4], 1)),
+            _extent("k", sizes, (*steps[4:8], 1)), _extent("v", sizes, (*steps[8:], 1)), rotary_dim // 2)
+
+
+def _table(c: _Layout, page_table):
+    if page_table.dtype is not _torch.int32 or page_table.numel() != c.n_seq * c.max_pages or not page_table.is_contiguous():
+        _dense(_torch.int32, c.n_seq * c.max_pages, page_table)
+        if page_table.dim() == 2 and c.n_seq > 1 and page_table.shape[1] != c.max_pages:
+            raise ValueError(f"a page table of {page_table.shape[1]} entries per sequence, the descriptor says {c.max_pages}")
 
 
 def sablock_compact_paged(shape: CShape, k, v, idx, budget: int, append_window: bool, pages: CPages, page_table, k_pool, v_pool, bounds=None,
                           lengths_out=None, stream=None):
     lib = load()
-    k_at, v_at, idx_at, table, kp, vp, b, lengths = _pointers(k, v, idx, page_table, k_pool, v_pool, bounds, lengths_out)
-    dtype, n_seq, problems, entries, n_bounds, _ = _cache_sizes(pages)
-    i32 = _torch.int32
-    _dense(i32, problems * budget, idx)
-    _dense(i32, entries, page_table)
-    _dense(i32, n_seq, lengths_out)
-    _dense(dtype, n_bounds, bounds)
+    device, k_at, v_at, idx_at, table, kp, vp, b, lengths = _pointers(k, v, idx, page_table, k_pool, v_pool, bounds, lengths_out)
+    c = _cache_layout(bytes(pages))
+    _table(c, page_table)
+    _strided(c.dtype, (k_pool, c.k_pool), (v_pool, c.v_pool))
+    _all_dense((_torch.int32, c.problems * budget, idx), (_torch.int32, c.n_seq, lengths_out), (c.dtype, c.bounds, bounds))
     _check(lib.sablock_compact_paged(ctypes.byref(shape), k_at, v_at, idx_at, budget, 1 if append_window else 0, ctypes.byref(pages), table, kp, vp,
-                                     b, lengths, _stream(stream)))
+                                     b, lengths, _stream(stream, device)))
 
 
 def sablock_append_paged(pages: CPages, tokens: CNewTokens, k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q=None, q_out=None,
                          counts=None, bounds=None, stream=None):
-    """``lengths`` are the rows of every sequence WITH the new tokens."""
+    """``lengths`` are the rows of every sequence WITH the new tokens; q, k and v have the sizes and strides of those that ``tokens`` was made of."""
     lib = load()
-    k_at, v_at, pos, freq, table, rows, kp, vp, q_at, out, c, b = _pointers(k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool, q,
-                                                                            q_out, counts, bounds)
-    dtype, n_seq, _, entries, n_bounds, queries = _cache_sizes(pages)
+    device, k_at, v_at, pos, freq, table, rows, kp, vp, q_at, out, count, b = _pointers(k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool,
+                                                                                        q, q_out, counts, bounds)
+    c, n_new, q_extent, k_extent, v_extent, n_freq = _tokens_layout(bytes(pages), bytes(tokens))
     i32 = _torch.int32
-    _dense(i32, n_seq, positions, lengths, counts)
-    _dense(i32, entries, page_table)
-    _dense(_torch.float32, tokens.rotary_dim // 2, inv_freq)
-    _dense(dtype, queries * tokens.n_new, q_out)
-    _dense(dtype, n_bounds, bounds)
-    if not (k.dtype is v.dtype is k_pool.dtype and (q is None or q.dtype is k.dtype)):
-        raise ValueError("q, k and v are of the cache's dtype")
-    _check(lib.sablock_append_paged(ctypes.byref(pages), ctypes.byref(tokens), q_at, k_at, v_at, c, pos, freq, table, rows, out, kp, vp, b,
-                                    _stream(stream)))
+    _table(c, page_table)
+    if q is not None:
+        _strided(c.dtype, (q, q_extent), (k, k_extent), (v, v_extent), (k_pool, c.k_pool), (v_pool, c.v_pool))
+    else:
+        _strided(c.dtype, (k, k_extent), (v, v_extent), (k_pool, c.k_pool), (v_pool, c.v_pool))
+    _all_dense((i32, c.n_seq, lengths), (i32, c.n_seq, positions), (i32, c.n_seq, counts), (_torch.float32, n_freq, inv_freq),
+               (c.dtype, c.queries * n_new, q_out), (c.dtype, c.bounds, bounds))
+    _check(lib.sablock_append_paged(ctypes.byref(pages), ctypes.byref(tokens), q_at, k_at, v_at, count, pos, freq, table, rows, out, kp, vp, b,
+                                    _stream(stream, device)))
 
 
 def sablock_decode_paged_workspace_bytes(pages: CPages) -> int:
@@ -480,17 +557,14 @@ def sablock_decode_paged_workspace_bytes(pages: CPages) -> int:
 def sablock_decode_paged(pages: CPages, q, k_pool, v_pool, page_table, lengths, out, ws, page_list=None, stream=None):
     """``page_list [P, n]`` int32, dense: the pages to read (``sablock_select_pages``); None = all."""
     lib = load()
-    q_at, kp, vp, table, rows, o, ws_at, listed = _pointers(q, k_pool, v_pool, page_table, lengths, out, ws, page_list)
+    device, q_at, kp, vp, table, rows, o, ws_at, listed = _pointers(q, k_pool, v_pool, page_table, lengths, out, ws, page_list)
     n = 0 if page_list is None else page_list.shape[-1]
-    dtype, n_seq, problems, entries, _, queries = _cache_sizes(pages)
-    i32 = _torch.int32
-    _dense(i32, entries, page_table)
-    _dense(i32, n_seq, lengths)
-    _dense(i32, problems * n, page_list)
-    _dense(dtype, queries, q)
-    _dense(_torch.float32, queries, out)
+    c = _cache_layout(bytes(pages))
+    _table(c, page_table)
+    _strided(c.dtype, (k_pool, c.k_pool), (v_pool, c.v_pool))
+    _all_dense((_torch.int32, c.n_seq, lengths), (_torch.int32, c.problems * n, page_list), (c.dtype, c.queries, q), (_torch.float32, c.queries, out))
     _check(lib.sablock_decode_paged(ctypes.byref(pages), q_at, kp, vp, table, rows, listed, n, o, ws_at, ws.numel() * ws.element_size(),
-                                    _stream(stream)))
+                                    _stream(stream, device)))
 
 
 def sablock_select_pages_workspace_bytes(pages: CPages) -> int:
@@ -501,16 +575,12 @@ def sablock_select_pages_workspace_bytes(pages: CPages) -> int:
 
 def sablock_select_pages(pages: CPages, q, bounds, page_table, lengths, n_pick: int, list_out, ws, n_first: int = 1, n_last: int = 1, stream=None):
     lib = load()
-    q_at, b, table, rows, listed, ws_at = _pointers(q, bounds, page_table, lengths, list_out, ws)
-    dtype, n_seq, problems, entries, n_bounds, queries = _cache_sizes(pages)
-    i32 = _torch.int32
-    _dense(i32, entries, page_table)
-    _dense(i32, n_seq, lengths)
-    _dense(i32, problems * n_pick, list_out)
-    _dense(dtype, queries, q)
-    _dense(dtype, n_bounds, bounds)
+    device, q_at, b, table, rows, listed, ws_at = _pointers(q, bounds, page_table, lengths, list_out, ws)
+    c = _cache_layout(bytes(pages))
+    _table(c, page_table)
+    _all_dense((_torch.int32, c.n_seq, lengths), (_torch.int32, c.problems * n_pick, list_out), (c.dtype, c.queries, q), (c.dtype, c.bounds, bounds))
     _check(lib.sablock_select_pages(ctypes.byref(pages), q_at, b, table, rows, n_pick, n_first, n_last, listed, ws_at,
-                                    ws.numel() * ws.element_size(), _stream(stream)))
+                                    ws.numel() * ws.element_size(), _stream(stream, device)))
 
 
 class PagedCache:
