@@ -451,8 +451,8 @@ SABLOCK_API sablock_status sablock_append_paged(const sablock_pages *pages, cons
  *   page_list   nullable, or [P][n_listed] int32 as written by sablock_select_pages: the pages (places in the sequence's row of the
  *               table) whose rows count, in the first min(n_listed, pages of the sequence) entries; entries outside the sequence's pages
  *               are skipped, one that comes twice counts twice
- *   out         [n_seq][n_layers][n_q_heads][D] fp32, dense.  A sequence without any row gives zeros, as do logits
- *               that are all -infinity.
+ *   out         [n_seq][n_layers][n_q_heads][D] fp32, dense, on any fp32 number's place.  A sequence without any row gives
+ *               zeros, as do logits that are all -infinity.
  *   ws          at least sablock_decode_paged_workspace_bytes(pages) bytes, 16-byte aligned
  * What pages hold behind a sequence's last row, NaN and infinity too, does not matter.
  * Supported: G <= 16; head_dim a multiple of 32 (bf16) or 16 (fp32).  Errors as for the other calls. */

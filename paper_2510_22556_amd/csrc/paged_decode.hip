@@ -499,6 +499,7 @@ decode_paged_kernel(DecodePagedArgs a)
 }
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float out4 __attribute__((ext_vector_type(4), aligned(4)));             // the caller's, on any fp32 number's place
 template <int M> __device__ __forceinline__ float over_lanes(float x, bool take_max)
 {
     if constexpr (M < 64) {
@@ -560,7 +561,7 @@ decode_paged_merge_kernel(DecodePagedArgs a)
     __syncthreads();
     if (group > 0) return;
     for (int i = 1; i < groups; ++i) t += sum[i * per + c];
-    *reinterpret_cast<f32x4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
+    *reinterpret_cast<out4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
 }
 
 // Workgroups per compute unit that the registers leave room for.  The long problems are dealt out to just as many: with two of three

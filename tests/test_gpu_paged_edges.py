@@ -57,3 +57,18 @@ def test_append_behind_a_full_table(torch_cuda, D, R, interleaved, dtype, page, 
     for got, ref in zip((c.k_pool, c.v_pool), want):
         assert torch.equal(got.view(bits), ref.view(bits))
     assert torch.equal(torch.nan_to_num(c.bounds.float(), 7.0), torch.nan_to_num(want[2].float(), 7.0))
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (16, "f32")])
+@pytest.mark.parametrize("place", [1, 2, 3])
+def test_decode_into_any_place_of_an_array(torch_cuda, D, dtype, place):  # noqa: F811
+    # an fp32 number's place is enough for the output; a problem of one workgroup, and one in pieces
+    torch = torch_cuda
+    c = Cache(torch, D, [20, 5000], heads=2, group=3, D=D, dtype=dtype).fill()
+    q = c.normal((2, 1, 6, D))
+    want = c.decode(q)
+    array = torch.full((want.numel() + 8,), 77.0, dtype=torch.float32, device="cuda")
+    out = array[place: place + want.numel()].view(want.shape)
+    ws = torch.empty((c.B.sablock_decode_paged_workspace_bytes(c.pages),), dtype=torch.uint8, device="cuda")
+    c.B.sablock_decode_paged(c.pages, q, c.k_pool, c.v_pool, c.table, c.lengths, out, ws)
+    assert torch.equal(out, want) and bool((array[:place] == 77.0).all()) and bool((array[place + want.numel():] == 77.0).all())
