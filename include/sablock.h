@@ -429,7 +429,8 @@ typedef struct {
  * lengths[s] - c + j: `lengths` are those WITH the new tokens, so that one array serves all layers' calls of a step, and the
  * attention behind them.  K's and q's pairs (a, b) turn by the angle t = position * inv_freq[i]:
  *   (a cos t - b sin t, b cos t + a sin t)
- * (t in fp64, the products in fp32, one rounding to the dtype); V and the elements behind R are copied.
+ * (t in fp64; its cosine and sine to one fp32 rounding in fp32 caches, to 2^-22 in bf16 ones; the products in fp32, one rounding to the
+ * dtype); V and the elements behind R are copied.
  *   q, q_out    both or neither; q_out [n_seq][n_layers][n_q_heads][n_new][D] dense, of the dtype; it may not overlap q
  *   counts      nullable (every sequence has n_new), or [n_seq] int32, taken as 0 .. n_new and at most lengths[s]; rows of
  *               q_out and of the pools that belong to no token stay as they are

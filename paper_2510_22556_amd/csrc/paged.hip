@@ -20,6 +20,8 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
+constexpr double TURN = 0.15915494309189535, TURN_REST = -9.839338337591243e-18;                // 1 / (2 pi), and what fp64 leaves of it
+
 template <bool BF16> struct Elem;
 template <> struct Elem<true> {
     static constexpr int N = 8, BYTES = 2;                     // per 16 bytes, of one
@@ -46,6 +48,14 @@ template <> struct Elem<true> {
         for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), bf16x2));
         return o;
     }
+    // cosine and sine of position * freq.  The fraction of a turn, sine and cosine in fp32: off by 2^-22, which rows of 8 bits do not show
+    static __device__ float2 turn(double position, float freq)
+    {
+        const double turns = position * ((double)freq * TURN);
+        float sn, cs;
+        sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
+        return make_float2(cs, sn);
+    }
 };
 template <> struct Elem<false> {
     static constexpr int N = 4, BYTES = 4;
@@ -57,6 +67,27 @@ template <> struct Elem<false> {
     static __device__ u32x4 pack(const float (&x)[4])
     {
         return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+    }
+    // The angle as the fp64 number that it is, its fraction of a turn to 2^-53 of one however many there are, less the nearest quarter.  What is left, at
+    // most pi / 4, as the sum h + l of two fp32 numbers; sine and cosine by the first terms of their series (the next are below 2^-32 of them), with
+    // what l and the roundings of the large terms leave out put back: off by 0.75 and 0.6 units in the last place at most, on average by as much as fp64
+    // rounded once.  (In fp64 throughout, the registers would leave room for a workgroup less.)
+    static __device__ float2 turn(double position, float freq)
+    {
+        const double angle = position * (double)freq, part = fma(angle, TURN_REST, fma(angle, TURN, -rint(angle * TURN)));
+        const double quarters = rint(4.0 * part), r = (part - 0.25 * quarters) * 6.283185307179586;
+        const float h = (float)r, l = (float)(r - (double)h), z = h * h, zl = fmaf(h, h, -z) + 2.f * h * l;
+        float sn = fmaf(z, -1.f / 39916800, 1.f / 362880), cs = fmaf(z, -1.f / 3628800, 1.f / 40320);
+        sn = fmaf(z, sn, -1.f / 5040);
+        cs = fmaf(z, cs, -1.f / 720);
+        sn = fmaf(z, sn, 1.f / 120);
+        cs = fmaf(z, cs, 1.f / 24);
+        sn = fmaf(z, sn, -1.f / 6);
+        const float most = fmaf(z, -0.5f, 1.f), rest = (1.f - most) - 0.5f * z;
+        const float s = h + fmaf(h * z, sn, l * most), c = most + (fmaf(zl, -0.5f, rest) + z * z * cs);
+        const int q = (int)quarters & 3;                       // the pair turned by a quarter: (c, s) -> (-s, c)
+        const float x = q & 1 ? s : c, y = q & 1 ? c : s;
+        return make_float2(q == 1 || q == 2 ? -x : x, q & 2 ? -y : y);
     }
 };
 
@@ -186,8 +217,8 @@ struct AppendArgs {
 };
 
 // grid (touched pages, sequences x layers, parts of the head rows).  The angle of a (token, pair) is the same for all heads: formed
-// once per workgroup, position * inv_freq in whole turns in fp64 (at position 131 072 an angle in fp32 is off by up to 2^-8), the
-// fraction of a turn in fp32.  A thread has one chunk of every groups-th row of a head, a row's chunks lie in the lanes of one wavefront, where
+// once per workgroup, position * inv_freq in fp64 (at position 131 072 an angle in fp32 is off by up to 2^-8), see turn() of either
+// type.  A thread has one chunk of every groups-th row of a head, a row's chunks lie in the lanes of one wavefront, where
 // the other halves of pairs come from.  The rows of the next step are on their way while one is turned and stored, the first
 // ones while the angles are formed.
 // ONE: a token per sequence, and a workgroup has no more head rows than it does at a time.  SPLIT: the two elements of a pair lie half a rotation
@@ -235,8 +266,8 @@ append_paged_kernel(AppendArgs a)
     };
     // the thread's pair of the angles, which it forms for every angle_step-th token
     const int angle_step = half ? NT / half : 1, pair = half ? tid % half : 0, angle_tok = half ? tid / half : angle_step;
-    double turns_per = 0.0;
-    if (angle_tok < angle_step) turns_per = (double)a.inv_freq[pair] * 0.15915494309189535;
+    float freq = 0.f;
+    if (angle_tok < angle_step) freq = a.inv_freq[pair];
     for (int t0 = begin;; t0 += a.tile) {
         const int n = min(a.tile, end - t0), rows = B * a.groups, batches = (n + rows - 1) / rows;
         u32x4 x[B];
@@ -250,12 +281,8 @@ append_paged_kernel(AppendArgs a)
         if (a.t.R) {
             if (t0 > begin) __syncthreads();
             if (angle_tok < angle_step)
-                for (int tok = angle_tok; tok < n; tok += angle_step) {
-                    const double turns = (double)(position0 + t0 - first + tok) * turns_per;
-                    float sn, cs;
-                    sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
-                    turn[tok * half + pair] = make_float2(cs, sn);
-                }
+                for (int tok = angle_tok; tok < n; tok += angle_step)
+                    turn[tok * half + pair] = E::turn((double)(position0 + t0 - first + tok), freq);
             __syncthreads();
         }
         Bounds<BF16> b;

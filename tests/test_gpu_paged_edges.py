@@ -72,3 +72,27 @@ def test_decode_into_any_place_of_an_array(torch_cuda, D, dtype, place):  # noqa
     ws = torch.empty((c.B.sablock_decode_paged_workspace_bytes(c.pages),), dtype=torch.uint8, device="cuda")
     c.B.sablock_decode_paged(c.pages, q, c.k_pool, c.v_pool, c.table, c.lengths, out, ws)
     assert torch.equal(out, want) and bool((array[:place] == 77.0).all()) and bool((array[place + want.numel():] == 77.0).all())
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("n_new", [1, 70])
+def test_append_angles_in_fp32(torch_cuda, interleaved, n_new):  # noqa: F811
+    # pairs (1, 0) turn into cosine and sine alone.  Their last rounding: 2^-25 of values below 1; those of the terms behind the first, a tenth of them,
+    # a half of that at most
+    torch = torch_cuda
+    D, n = 128, 4
+    c = Cache(torch, 1, [n_new] * n, heads=2, group=1, D=D, dtype="f32")
+    one = torch.zeros((n, 1, 2, n_new, D), device="cuda")
+    one[..., 0::2] = 1.0 if interleaved else 0.0
+    if not interleaved:
+        one[..., : D // 2] = 1.0
+    positions = torch.tensor([0, 1000, 131072, 2 ** 30], dtype=torch.int32, device="cuda")
+    freq = torch.tensor([10000.0 ** (-2 * i / D) for i in range(D // 2)], dtype=torch.float32, device="cuda")
+    q_out = torch.empty_like(one)
+    c.B.sablock_append_paged(c.pages, c.B.make_new_tokens(one, one, one, interleaved=interleaved), one, one, positions, freq, c.table, c.lengths, c.k_pool,
+                             c.v_pool, q=one, q_out=q_out)
+    angle = (positions.double().cpu()[:, None] + torch.arange(n_new)).numpy()[..., None] * freq.double().cpu().numpy()
+    want = np.stack([np.cos(angle), np.sin(angle)], axis=-1 if interleaved else -2).reshape(n, 1, 1, n_new, D)
+    got = q_out.double().cpu().numpy()
+    assert np.abs(got - want).max() <= 2.0 ** -25 + 2.0 ** -26
+    assert torch.equal(c.k_pool[0, c.table[0, 0].long(), :, 0], q_out[0, 0, :, 0])
