@@ -3,7 +3,7 @@
 import numpy as np
 import pytest
 
-from test_gpu_paged import Cache, _ref_append, torch_cuda  # noqa: F401
+from test_gpu_paged import Cache, _ref_append, _ref_decode, _ref_select, torch_cuda  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +96,136 @@ def test_append_angles_in_fp32(torch_cuda, interleaved, n_new):  # noqa: F811
     got = q_out.double().cpu().numpy()
     assert np.abs(got - want).max() <= 2.0 ** -25 + 2.0 ** -26
     assert torch.equal(c.k_pool[0, c.table[0, 0].long(), :, 0], q_out[0, 0, :, 0])
+
+
+# ---- the ways of dealing out a decode step -------------------------------------------------------------------------------
+
+
+def _spread(n, most, least=1):
+    """Lengths all over (0, most], the first the longest."""
+    return [max(least, int(most * (1 - s * 0.6180339887498949 % 1))) for s in range(n)]
+
+
+SHORT = [s % 41 for s in range(4096)]
+WAYS = [                                                       # way, dtype, D, page, heads, group, lengths, compute units (0: the device's), listed pages
+    ("alone", "bf16", 128, 16, 2, 4, [450, 0, 40], 64, None), ("short", "bf16", 128, 16, 2, 4, [510, 0, 40], 64, None),
+    ("cut", "bf16", 128, 16, 2, 4, [3000, 10, 1500, 0, 2000], 64, None), ("longer", "bf16", 128, 16, 2, 3, _spread(5, 3000, 1100), 32, None),
+    ("even", "bf16", 128, 16, 4, 4, _spread(20, 2600), 4, None), ("even", "bf16", 128, 32, 3, 2, _spread(100, 2300), 16, None),
+    ("even", "f32", 64, 64, 3, 7, _spread(33, 5000), 6, None), ("even", "f32", 256, 16, 2, 2, _spread(17, 3000), 8, None), ("even", "bf16", 256, 32, 2, 5, _spread(12, 4000), 8, None),
+    ("even", "bf16", 32, 16, 1, 2, [4500 if s % 70 == 3 else n for s, n in enumerate(SHORT)], 8, None),
+    ("cut", "bf16", 32, 16, 1, 2, [9000 if s % 400 == 3 else n for s, n in enumerate(SHORT)], 256, None),
+    ("even", "bf16", 128, 16, 2, 4, _spread(70, 3000), 4, 80), ("cut", "bf16", 128, 16, 1, 2, _spread(70, 3000), 256, 150), ("even", "f32", 64, 32, 2, 3, _spread(20, 6000), 4, 90),
+    ("even", "bf16", 128, 16, 8, 2, _spread(100, 2300), 0, None)]
+
+
+def _of_way(torch, expected, dtype, D, page, heads, group, lengths, cus, listed):
+    from paged_plan import way
+
+    c = Cache(torch, D + len(lengths), lengths, heads=heads, group=group, D=D, dtype=dtype, page=page, k_axes=(0, 2, 1, 3))
+    c.pages.compute_units = cus
+    real = cus or torch.cuda.get_device_properties(0).multi_processor_count
+    assert cus or real == 256
+    assert way(dtype, D, page, heads, lengths, c.width, real, listed) == expected
+    lst = None if listed is None else torch.randint(-1, c.width, (c.n * heads, listed), generator=c.gen, device="cuda", dtype=torch.int32)
+    return c, lst
+
+
+@pytest.mark.parametrize("args", WAYS, ids=lambda a: f"{a[0]}-{a[1]}-{a[2]}-{len(a[6])}-{a[7]}-{a[8]}")
+def test_decode_in_every_way_of_dealing(torch_cuda, args):  # noqa: F811
+    torch = torch_cuda
+    c, lst = _of_way(torch, *args)
+    c.k_pool.copy_(c.normal(c.k_pool.shape))
+    c.v_pool.copy_(c.normal(c.v_pool.shape))
+    q = c.normal((c.n, 1, c.H * c.G, c.D))
+    got, ref = c.decode(q, lst).double().cpu(), _ref_decode(c, q, None if lst is None else lst.cpu())
+    assert bool(((got - ref).abs() <= 2.0 ** -16 * 6).all())    # as in the test of many sequences
+    assert torch.equal(c.decode(q, lst, ws_fill=0), c.decode(q, lst, ws_fill=0x7F))
+
+
+@pytest.mark.parametrize("args", [a for a in WAYS if a[8] is None], ids=lambda a: f"{a[0]}-{a[1]}-{a[2]}-{len(a[6])}-{a[7]}")
+def test_decode_counts_every_row_once_in_every_way_of_dealing(torch_cuda, args):  # noqa: F811
+    # equal logits: the mean of V, which has a one in column r % D of row r.  2^-20 relative as in the test of one sequence
+    torch = torch_cuda
+    c, _ = _of_way(torch, *args)
+    rows = torch.arange(c.width * c.page, device="cuda")
+    one = torch.nn.functional.one_hot(rows % c.D, c.D).to(c.dt)
+    want = torch.zeros((c.n, c.D), dtype=torch.float64, device="cuda")
+    for s, n in enumerate(c.lengths.tolist()):
+        if n:
+            r = rows[:n]
+            ids = c.table[s, r // c.page].long()
+            c.k_pool[0, ids, :, r % c.page] = 0.0
+            c.v_pool[0, ids, :, r % c.page] = one[:n, None]
+            want[s] = torch.bincount(r % c.D, minlength=c.D).double() / n
+    got = c.decode(c.normal((c.n, 1, c.H * c.G, c.D))).double()
+    assert torch.allclose(got, want[:, None, None].expand_as(got), rtol=2.0 ** -20, atol=0)
+
+
+# ---- precision -----------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_probabilities_are_fp32(torch_cuda, dtype):  # noqa: F811
+    # Three rows whose logits are exact products.  Column 0 has ones: the shares' sum.  The three parts of a probability are within 2^-26 of it (two would
+    # be off by 7e-6 on average), nine products and three terms of the denominator are added, two products and a quotient follow: 14 roundings, 2^-23
+    # each where the matrix pipe cuts, below 2^-19.  Columns 1 to 3 have one row's share each: the logit in the log2 domain, at most 1.5,
+    # rounds twice, its distance from the reference, at most 12, to 2^-21, the power to 2^-23: 2^-20.7 in a share, twice, and the sum's
+    torch = torch_cuda
+    n, G, D = 200, 8, 64
+    c = Cache(torch, 1, [3] * n, heads=1, group=G, D=D, dtype=dtype)
+    at = c.table[:, 0].long()
+    first = (torch.rand((n, 3), generator=c.gen, device="cuda") * 2 - 1).to(torch.bfloat16)
+    c.k_pool[0, at, 0, :3] = 0.0
+    c.k_pool[0, at, 0, :3, 0] = first.to(c.dt)
+    c.v_pool[0, at, 0, :3] = 0.0
+    c.v_pool[0, at, 0, :3, 0] = 1.0
+    for r in range(3):
+        c.v_pool[0, at, 0, r, 1 + r] = 1.0
+    q = torch.zeros((n, 1, G, D), dtype=c.dt, device="cuda")
+    q[..., 0] = torch.arange(1, G + 1, device="cuda").to(c.dt)
+    got = c.decode(q)[:, 0].double().cpu()
+    share = torch.softmax(first.double().cpu()[:, None] * torch.arange(1, G + 1, dtype=torch.float64)[:, None] / 8, dim=-1)
+    assert bool(((got[..., 0] - 1).abs() <= 2.0 ** -19).all()), float((got[..., 0] - 1).abs().max())
+    assert bool(((got[..., 1:4] - share).abs() <= (2.0 ** -19.7 + 2.0 ** -19) * share).all())
+    assert not got[..., 4:].any()
+
+
+@pytest.mark.parametrize("D,R,interleaved", [(128, 128, False), (64, 32, True), (96, 96, False)])
+@pytest.mark.parametrize("n_new", [1, 45])
+def test_append_fp32_rows(torch_cuda, D, R, interleaved, n_new):  # noqa: F811
+    # cosine and sine 0.75, the products and their sum one unit of 2^-24 each: 2.75 of |a| + |b|
+    torch = torch_cuda
+    n = 3
+    c = Cache(torch, 2, [n_new + 20] * n, heads=2, group=2, D=D, dtype="f32", page=32)
+    q, k, v = (c.normal((n, 1, h, n_new, D)) for h in (4, 2, 2))
+    positions = torch.tensor([0, 4000, 131072], dtype=torch.int32, device="cuda")
+    freq = torch.tensor([500000.0 ** (-2 * i / R) for i in range(R // 2)], dtype=torch.float32, device="cuda")
+    q_out = torch.empty_like(q)
+    c.B.sablock_append_paged(c.pages, c.B.make_new_tokens(k, v, q, rotary_dim=R, interleaved=interleaved), k, v, positions, freq, c.table, c.lengths, c.k_pool,
+                             c.v_pool, q=q, q_out=q_out)
+    (rq, sq), (rk, sk) = _ref_append(c, q, k, [n_new] * n, positions.tolist(), freq.tolist(), R, interleaved)
+    assert bool(((q_out.double().cpu() - rq).abs() <= 2.75 * 2.0 ** -24 * sq).all())
+    for s in range(n):
+        assert bool(((c.rows(c.k_pool, s)[:, :, 20:] - rk[s]).abs() <= 2.75 * 2.0 ** -24 * sk[s]).all())
+
+
+# ---- lengths that the table does not hold --------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 224), ("bf16", 3200), ("f32", 3200)])
+def test_reads_end_with_the_table(torch_cuda, dtype, rows):  # noqa: F811
+    # a length beyond the table counts as all of its rows, a negative one as none: in attention, in attention over listed pages, and in the choice of those
+    torch = torch_cuda
+    c = Cache(torch, rows, [0, 64, rows], heads=2, group=2, D=64, dtype=dtype)
+    c.table = c.table[:, : rows // 16].contiguous()
+    c.pages = c.B.make_pages(c.k_pool, c.v_pool, c.table, 4)
+    c.fill()
+    q = c.normal((3, 1, 4, 64))
+    ref, lists = _ref_decode(c, q), _ref_select(c, q, 6, 1, 1)
+    listed = _ref_decode(c, q, torch.tensor(lists))
+    for over in (rows + 1, rows + 16, INT_MAX):
+        c.lengths = torch.tensor([-5, 64, over], dtype=torch.int32, device="cuda")
+        assert bool(((c.decode(q).double().cpu() - ref).abs() <= 2.0 ** -16 * 6).all())
+        got = c.select(q, 6, 1, 1)
+        assert got.tolist() == lists
+        assert bool(((c.decode(q, got).double().cpu() - listed).abs() <= 2.0 ** -16 * 6).all())

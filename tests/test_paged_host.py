@@ -191,3 +191,26 @@ def test_binding_refuses_tensors_that_the_kernels_could_not_follow(lib):  # noqa
                  lambda: B.sablock_select_pages(pages, k, k, k, k, 3, k, k), lambda: B.sablock_compact_paged(_shape(), k, k, k, 3, True, pages, k, k, k)):
         with pytest.raises(ValueError, match="device memory"):  # before the library is asked
             call()
+
+
+def test_decode_launches_as_the_plan_of_the_tests_says(tmp_path):
+    # (dtype, D, problems, compute units): workgroups, rows alone, rows of a step that shares and of one that does not
+    from paged_plan import launch
+
+    cases = [(t, D, P, cus) for t in ("bf16", "f32") for D in (32, 64, 96, 128, 160, 192, 256) for P in (1, 255, 256, 4096) for cus in (4, 256, 400)]
+    rows = _run_host_code(tmp_path, """
+#include "paged_decode.hip"
+#include <cstdio>
+int main()
+{
+    for (const auto &c : std::initializer_list<std::array<int, 4>>{%s}) {
+        sablock::PageDims d{};
+        d.dtype = c[0]; d.D = c[1]; d.P = c[2]; d.cus = c[3];
+        const bool bf = d.dtype == SABLOCK_BF16;
+        std::printf("%%d %%d %%d %%d\\n", sablock::workgroups_of(d), sablock::rows_alone(d), sablock::step_rows(bf, d.D, false), sablock::step_rows(bf, d.D, true));
+    }
+}
+""" % ", ".join("{%d, %d, %d, %d}" % (B.SABLOCK_BF16 if t == "bf16" else B.SABLOCK_F32, D, P, cus) for t, D, P, cus in cases), header="array")
+    for (t, D, P, cus), (workgroups, rows_alone, shared, alone) in zip(cases, rows, strict=True):
+        assert launch(t, D, P, cus, 1 << 17) == (workgroups, rows_alone, shared)
+        assert launch(t, D, P, cus, 16) == (0, rows_alone, alone)
