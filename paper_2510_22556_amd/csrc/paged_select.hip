@@ -22,8 +22,9 @@ namespace sablock {
 namespace {
 
 constexpr int NT = 256, PICK_NT = 1024;
-// Workgroups of the scores per compute unit, as many as run at a time (with two 64 x 8 heads x 2 048 pages, scored, picked and read, 209 us in place
-// of 199)
+// Workgroups of the scores per compute unit that the launch plans for, as many as run at a time (with two 64 x 8 heads x 2 048 pages, scored, picked
+// and read, 209 us in place of 199).  Not so for more than eight query heads and rows of more than 256 bytes in bf16, 512 in fp32: the heads' elements
+// take 64 KB of LDS there, two run at a time, and the third comes behind them.
 constexpr int SCORE_WGS = 3;
 constexpr uint32_t NOT_A_NUMBER = 0xfffffffeu; // above every number's key
 

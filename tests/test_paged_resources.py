@@ -87,3 +87,16 @@ def test_matrix_results_are_waited_for_on_every_path(assembly, source, kernel, l
                     assert not (result & _registers(x)), f"{name}: {o} {x} {states} states behind {op} {arg}"
                 ways += [(n, states + (int(x) + 1 if o == "s_nop" else 1)) for n in following(j)]
     assert products > least
+
+
+def test_as_many_workgroups_of_the_scores_reside_as_the_source_says(assembly):
+    # by registers as above, and by 160 KB of LDS; three, but for more than eight heads of the widest rows
+    seen = {}
+    for name, k in _kernels(assembly["paged_select.hip"]).items():
+        m = re.search(r"page_scores_kernelILb([01])ELi(\d+)ELi(\d+)ELi(\d+)E", name)
+        if m:
+            lds = k["group_segment_fixed_size"]
+            seen[m.groups()] = min(512 // -(-k["next_free_vgpr"] // 8 * 8), 160 * 1024 // lds if lds else 8)
+    two = {("1", "16", "2", "4"), ("0", "16", "4", "4")}
+    assert len(seen) == 27 and two < set(seen)
+    assert all(n == 2 if i in two else n >= 3 for i, n in seen.items()), seen
