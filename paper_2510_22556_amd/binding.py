@@ -605,11 +605,12 @@ class PagedCache:
 class Buffers:
     """Device buffers for one call geometry: outputs of every step plus the workspace.
 
-    Allocation happens here, once; the five ``sablock_*`` calls then only enqueue kernels.
+    Allocation happens here, once; the five ``sablock_*`` calls then only enqueue kernels.  ``dense=False``: without ``k_out`` and
+    ``v_out``, for a cache in pages.
     """
 
     def __init__(self, shape: CShape, seg: Segments, budget: int, device, append_window: bool = True,
-                 dtype=None):
+                 dtype=None, dense: bool = True):
         import torch
 
         P, L, W, D = n_problems(shape), shape.seq_len, shape.window, shape.head_dim
@@ -627,8 +628,7 @@ class Buffers:
         self.n_sel = torch.empty((P,), dtype=torch.int32, device=device)
         self.topb = torch.empty((P, 2), dtype=torch.int32, device=device)
         rows = budget + (W if append_window else 0)
-        self.k_out = torch.empty((P, max(rows, 1), D), dtype=dt, device=device)
-        self.v_out = torch.empty((P, max(rows, 1), D), dtype=dt, device=device)
+        self.k_out, self.v_out = (torch.empty((P, max(rows, 1), D), dtype=dt, device=device) if dense else None for _ in range(2))
         self.ws = torch.empty((sablock_workspace_bytes(shape, seg.max_segments, budget),), dtype=torch.uint8,
                               device=device)
 
@@ -638,6 +638,8 @@ def compress(shape: CShape, q, k, v, seg: Segments, cand: Sequence[int], budget:
     """The whole hot path: score, refine, search_blocks + select (one call for both, or the two separate calls with
     ``fused=False``: same results), compact: into ``buf.k_out`` / ``buf.v_out``, or into the pages of ``cache`` where one is given (its
     ``lengths`` are written, and its bounds)."""
+    if cache is None and buf.k_out is None:
+        raise ValueError("buffers without k_out and v_out are for a cache in pages")
     # the calls above with their arguments marshalled once: small calls are bound by what the host does between launches
     lib, st, sp = load(), _stream(stream), ctypes.byref(shape)
     s, ent, s_tilde, topb, idx, n_sel = (_ptr(t) for t in (buf.s, buf.ent, buf.s_tilde, buf.topb, buf.idx, buf.n_sel))

@@ -229,3 +229,26 @@ def test_reads_end_with_the_table(torch_cuda, dtype, rows):  # noqa: F811
         got = c.select(q, 6, 1, 1)
         assert got.tolist() == lists
         assert bool(((c.decode(q, got).double().cpu() - listed).abs() <= 2.0 ** -16 * 6).all())
+
+
+def test_compress_into_pages_without_dense_buffers(torch_cuda):  # noqa: F811
+    torch = torch_cuda
+    from paper_2510_22556_amd import binding as B
+    from paper_2510_22556_amd import synth
+
+    n, nl, H, D, L, W, budget = 2, 1, 2, 64, 700, 16, 90
+    q, k, v = (synth.normal_torch(60 + i, i, (n, nl, h, m, D), "cuda", torch.bfloat16) for i, h, m in ((1, 2 * H, W), (2, H, L), (3, H, L)))
+    seg = B.make_segments(np.concatenate([np.arange(0, L - W, 36), [L - W]] * n), np.arange(n + 1) * (-(-(L - W) // 36) + 1), "cuda")
+    shape = B.make_shape(q, k, v)
+    caches = []
+    for dense in (True, False):
+        buf = B.Buffers(shape, seg, budget, "cuda", dense=dense)
+        cache = B.PagedCache(n, nl, 2 * H, H, D, 16, 20, 8, torch.bfloat16, "cuda")
+        cache.page_table.copy_(torch.arange(16, device="cuda").view(n, 8))
+        B.compress(shape, q, k, v, seg, [1, 2, 4], budget, buf, cache=cache)
+        caches.append(cache)
+    assert buf.k_out is None and buf.v_out is None
+    for name in ("k_pool", "v_pool", "bounds", "lengths"):
+        assert torch.equal(*(getattr(c, name) for c in caches)), name
+    with pytest.raises(ValueError, match="cache in pages"):
+        B.compress(shape, q, k, v, seg, [1, 2, 4], budget, buf)
