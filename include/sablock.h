@@ -467,7 +467,8 @@ SABLOCK_API sablock_status sablock_decode_paged(const sablock_pages *pages, cons
  * sequence and, of the others, those with the best scores, n_pick in all.  A page's score is a bound of its rows' logits,
  *   max over the G query heads of  sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d >= sqrt(D) * (any logit of the page),
  * with lo, hi the page bounds; summed in fp64 and rounded to fp32 once.  Equal scores: the lower page first; a score that
- * is not a number counts as the largest, and an infinite bound makes it infinite or that (0 times infinity).
+ * is not a number counts as the largest, and an infinite bound makes it infinite or that (0 times infinity): a page with an infinite element of K
+ * comes in front of all without one, whatever the query's sign there.
  *   q           [n_seq][n_layers][n_q_heads][D], dense, dtype of the cache
  *   list_out    [P][n_pick] int32: pages in ascending order, all of them where the sequence has no more than n_pick; -1 behind
  *               the last

@@ -6,8 +6,8 @@
 // What bounds them: the copy.  A large device copy reaches 5.0-5.3 TB/s here, read and written.  Compaction of 32 layers x 8 heads,
 // 1 024 rows of 256 bytes each out of 32 768 (272 MB in and out): 61 us, 4.6 TB/s; several rows per thread in flight gain
 // nothing over one and eight workgroups per compute unit (61.1, 60.2 us).  Appended prompts, 11 300 tokens x 48 heads (278 MB): 69 us,
-// 4.0 TB/s, the rotation's vector instructions a third of that time beside it; without a rotation 68.  One token: 3.8 us, as good as one
-// launch and three dependent loads; 256 sequences, a token each, 5.3 us.
+// 4.0 TB/s, the rotation's vector instructions a third of that time beside it; without a rotation 68; fp32 130 us.  One token: 4.4 us in a graph, as
+// good as one launch and three dependent loads; 256 sequences, a token each, 5.9 us.
 #include "sablock_internal.h"
 
 namespace sablock {

@@ -9,13 +9,13 @@
 //       operand is an element of the piece that it loaded.  The products' sums are joined over the lanes, each lane then
 //       has one page and head, whose score it rounds to fp32 and turns into a whole number of the same order; the maximum over the heads is
 //       one of whole numbers, in which what is no number can be the largest.
-//       What bounds it: loads.  8 heads x 8 192 pages of 512 bytes of bounds, four query heads: 9.7 us, of which 5.1 are the bytes at 6.6 TB/s;
+//       What bounds it: loads.  8 heads x 8 192 pages of 512 bytes of bounds, four query heads: 10.2 us (at best 9.6), of which 5.1 are the bytes at 6.6 TB/s;
 //       as long without the products, the rest is the launch and the chain length, table, bounds.  Formed on the vector pipe, by fp64
-//       instructions and sums over 16 lanes, 12.3; with 16 query heads, picking and reading with it, 36.3 in place of 46.3.
+//       instructions and sums over 16 lanes, 12.3 at best; with 16 query heads, picking and reading with it, 36.3 in place of 46.3.
 //   pick_pages_kernel    a workgroup per problem; the keys stay in registers.  The last key that is taken is found digit by digit, 11 bits
 //       of its distance from the least key at a time (the keys of a problem share their upper bits) until 64 are left, which a wavefront
-//       ranks, and one prefix sum places the pages in order.  8 192 pages: 5.6 us, a chain of seven barriers and the reads between
-//       them (with lane sums through LDS and nine barriers 6.5).
+//       ranks, and one prefix sum places the pages in order.  8 192 pages: 7.2 us, at best 5.6, a chain of seven barriers and the reads between
+//       them (with lane sums through LDS and nine barriers 6.5 at best).
 #include "sablock_internal.h"
 
 namespace sablock {
