@@ -446,6 +446,25 @@ SABLOCK_API sablock_status sablock_append_paged(const sablock_pages *pages, cons
                                     const int32_t *page_table, const int32_t *lengths, void *q_out /* nullable */,
                                     void *k_pool, void *v_pool, void *bounds /* nullable */, void *stream);
 
+/* The norm of a head: x_d -> x_d w_d / sqrt(mean over the head's D elements of x^2 + eps). */
+typedef struct {
+    float   eps;              /* positive, finite */
+    int32_t per_head;         /* weights: 0 = [n_layers][D], one for all heads of a layer; 1 = [n_layers][heads][D] */
+    int32_t reserved[2];      /* must be 0 */
+} sablock_head_norms;
+
+/* sablock_append_paged with a norm of every head of q and of k in front of the rotation, for models that have one: the same arguments,
+ * rows, positions, counts and bounds; V is copied as it is.  The norm covers the whole head whatever R is.
+ *   q_weight, k_weight  fp32, dense, 16-byte aligned, laid out as norms->per_head says; q_weight may be NULL where q is
+ * Squares, their sum, the norm and the rotation in fp32, one rounding to the dtype.  A head whose squares' sum passes fp32 becomes zeros; one
+ * with an element that is no number, or infinite, is no number there or throughout. */
+SABLOCK_API sablock_status sablock_append_normed_paged(const sablock_pages *pages, const sablock_new_tokens *tokens,
+                                    const sablock_head_norms *norms, const void *q /* nullable */, const void *k, const void *v,
+                                    const float *q_weight, const float *k_weight, const int32_t *counts /* nullable */,
+                                    const int32_t *positions, const float *inv_freq, const int32_t *page_table,
+                                    const int32_t *lengths, void *q_out /* nullable */, void *k_pool, void *v_pool,
+                                    void *bounds /* nullable */, void *stream);
+
 /* Decode-time attention of ONE new token per sequence over its pages (Sec. 2.1, Eq. 1 with a single query position):
  *   out[h] = softmax_r(<q[h], K[r]> / sqrt(D)) . V[r]  over the rows r < lengths[s], or those of the listed pages.
  *   q           [n_seq][n_layers][n_q_heads][D], dense, dtype of the cache

@@ -31,7 +31,7 @@ EXPORTS = ("sablock_version", "sablock_last_error", "sablock_workspace_bytes", "
            "sablock_window_attention", "sablock_score_static", "sablock_stream_probe", "sablock_validate_segments",
            "sablock_segment_slices", "sablock_segment_slice_count", "sablock_segment_slice_offsets",
            "sablock_compact_paged", "sablock_append_paged", "sablock_decode_paged_workspace_bytes", "sablock_decode_paged",
-           "sablock_select_pages_workspace_bytes", "sablock_select_pages")
+           "sablock_select_pages_workspace_bytes", "sablock_select_pages", "sablock_append_normed_paged")
 
 
 class SablockError(RuntimeError):
@@ -73,6 +73,12 @@ class CNewTokens(ctypes.Structure):
 
     _fields_ = [("n_new", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("q_stride", ctypes.c_int64 * 4), ("k_stride", ctypes.c_int64 * 4), ("v_stride", ctypes.c_int64 * 4)]
+
+
+class CHeadNorms(ctypes.Structure):
+    """The norms of an append (``sablock_head_norms``)."""
+
+    _fields_ = [("eps", ctypes.c_float), ("per_head", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
 
 
 def load():
@@ -123,6 +129,7 @@ def load():
         pp = ctypes.POINTER(CPages)
         lib.sablock_compact_paged.argtypes = [sp, vp, vp, vp, i32, i32, pp, vp, vp, vp, vp, vp, vp]
         lib.sablock_append_paged.argtypes = [pp, ctypes.POINTER(CNewTokens)] + [vp] * 13
+        lib.sablock_append_normed_paged.argtypes = [pp, ctypes.POINTER(CNewTokens), ctypes.POINTER(CHeadNorms)] + [vp] * 15
         lib.sablock_decode_paged_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
         lib.sablock_decode_paged.argtypes = [pp, vp, vp, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
         lib.sablock_select_pages_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
@@ -474,6 +481,11 @@ def make_new_tokens(k, v, q=None, rotary_dim: Optional[int] = None, interleaved:
     return t
 
 
+def make_head_norms(eps: float = 1e-6, per_head: bool = False) -> CHeadNorms:
+    """Descriptor of the norms of q's and k's heads: weights ``[n_layers, D]``, or with ``per_head`` ``[n_layers, heads, D]``."""
+    return CHeadNorms(float(eps), 1 if per_head else 0)
+
+
 class _Layout(NamedTuple):
     """What the kernels make of a cache's descriptor."""
 
@@ -546,6 +558,28 @@ def sablock_append_paged(pages: CPages, tokens: CNewTokens, k, v, positions, inv
                (c.dtype, c.queries * n_new, q_out), (c.dtype, c.bounds, bounds))
     _check(lib.sablock_append_paged(ctypes.byref(pages), ctypes.byref(tokens), q_at, k_at, v_at, count, pos, freq, table, rows, out, kp, vp, b,
                                     _stream(stream, device)))
+
+
+def sablock_append_normed_paged(pages: CPages, tokens: CNewTokens, norms: CHeadNorms, k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool,
+                                q=None, q_out=None, q_weight=None, k_weight=None, counts=None, bounds=None, stream=None):
+    """``sablock_append_paged`` with q's and k's heads over their root mean square in front of the rotation; ``q_weight`` and ``k_weight`` fp32,
+    ``[n_layers, D]`` or ``[n_layers, heads, D]``."""
+    lib = load()
+    device, k_at, v_at, pos, freq, table, rows, kp, vp, q_at, out, qw, kw, count, b = _pointers(k, v, positions, inv_freq, page_table, lengths, k_pool, v_pool,
+                                                                                                q, q_out, q_weight, k_weight, counts, bounds)
+    c, n_new, q_extent, k_extent, v_extent, n_freq = _tokens_layout(bytes(pages), bytes(tokens))
+    i32, f32 = _torch.int32, _torch.float32
+    _table(c, page_table)
+    if q is not None:
+        _strided(c.dtype, (q, q_extent))
+    _strided(c.dtype, (k, k_extent), (v, v_extent), (k_pool, c.k_pool), (v_pool, c.v_pool))
+    n_layers, q_heads, head_dim = q_extent.sizes[1], q_extent.sizes[2], q_extent.sizes[4]
+    per = n_layers * head_dim
+    _all_dense((i32, c.n_seq, lengths), (i32, c.n_seq, positions), (i32, c.n_seq, counts), (f32, n_freq, inv_freq), (c.dtype, c.queries * n_new, q_out),
+               (c.dtype, c.bounds, bounds), (f32, per * q_heads if norms.per_head else per, q_weight),
+               (f32, per * k_extent.sizes[2] if norms.per_head else per, k_weight))
+    _check(lib.sablock_append_normed_paged(ctypes.byref(pages), ctypes.byref(tokens), ctypes.byref(norms), q_at, k_at, v_at, qw, kw, count, pos, freq, table,
+                                           rows, out, kp, vp, b, _stream(stream, device)))
 
 
 def sablock_decode_paged_workspace_bytes(pages: CPages) -> int:

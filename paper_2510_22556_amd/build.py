@@ -14,7 +14,8 @@ LIB = os.path.join(HERE, "libsablock.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["api.hip", "score_generic.hip", "score_mfma.hip", "refine.hip", "search_select.hip", "compact.hip", "segment.hip", "decode.hip", "window_attn.hip",
-           "paged.hip", "paged_decode.hip", "paged_select.hip"]
+           "paged.hip", "paged_decode.hip", "paged_select.hip", "paged_norm.hip"]
+HEADERS = ["paged_rows.h", "paged_append.h"]    # of the paged cache's kernels
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function",
          # keep packed fp32 instructions out of the generated code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -26,6 +27,7 @@ def _compile(src: str, force: bool) -> str:
     s = os.path.join(CSRC, src)
     o = os.path.join(OBJ, src.replace(".hip", ".o"))
     deps = [s, os.path.join(CSRC, "sablock_internal.h"), os.path.join(HERE, "..", "include", "sablock.h")]
+    deps += [os.path.join(CSRC, h) for h in HEADERS if src.startswith("paged")]
     if force or not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(d) for d in deps):
         subprocess.run([HIPCC, *FLAGS, "-c", s, "-o", o], check=True)
     return o

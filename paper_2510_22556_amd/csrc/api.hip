@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -722,14 +723,14 @@ sablock_status sablock_compact_paged(const sablock_shape *shape, const void *k, 
     return dev(launch_compact_paged(d, k, v, idx, budget, (int32_t)rows, pd, pv, lengths_out, static_cast<hipStream_t>(stream)), who);
 }
 
-sablock_status sablock_append_paged(const sablock_pages *pages, const sablock_new_tokens *tokens, const void *q, const void *k, const void *v,
-                                    const int32_t *counts, const int32_t *positions, const float *inv_freq, const int32_t *page_table,
-                                    const int32_t *lengths, void *q_out, void *k_pool, void *v_pool, void *bounds, void *stream)
+// What both calls that append make of their arguments
+static sablock_status make_append(const char *who, const sablock_pages *pages, const sablock_new_tokens *tokens, const void *q, const void *k, const void *v,
+                                  const int32_t *positions, const float *inv_freq, const int32_t *page_table, const int32_t *lengths, const void *q_out,
+                                  const void *k_pool, const void *v_pool, const void *bounds, PageDims *pd_out, TokenDims *td_out, PageView *pv)
 {
-    const char *who = "sablock_append_paged";
-    PageDims pd;
-    sablock_status st = make_pages(who, pages, &pd);
+    sablock_status st = make_pages(who, pages, pd_out);
     if (st != SABLOCK_OK) return st;
+    const PageDims &pd = *pd_out;
     if (!tokens || !k || !v || !lengths) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
     if ((q == nullptr) != (q_out == nullptr)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: q and q_out must both be given or both be NULL", who);
     if (q && q == q_out) return fail(SABLOCK_ERR_INVALID_ARG, "%s: q_out may not overlap q", who);
@@ -749,17 +750,49 @@ sablock_status sablock_append_paged(const sablock_pages *pages, const sablock_ne
         return fail(SABLOCK_ERR_INVALID_ARG, "%s: token stride smaller than head_dim", who);
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out))
         return fail(SABLOCK_ERR_INVALID_ARG, "%s: q, k, v and q_out must be 16-byte aligned", who);
-    PageView pv;
-    st = make_page_view(who, page_table, lengths, k_pool, v_pool, bounds, &pv);
+    st = make_page_view(who, page_table, lengths, k_pool, v_pool, bounds, pv);
     if (st != SABLOCK_OK) return st;
-    TokenDims td;
+    TokenDims &td = *td_out;
     td.n_new = tokens->n_new; td.R = tokens->rotary_dim; td.interleaved = tokens->interleaved;
     for (int a = 0; a < 4; ++a) {
         td.qs[a] = nq[a] > 1 ? tokens->q_stride[a] : 0;
         td.ks[a] = nk[a] > 1 ? tokens->k_stride[a] : 0;
         td.vs[a] = nk[a] > 1 ? tokens->v_stride[a] : 0;
     }
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_append_paged(const sablock_pages *pages, const sablock_new_tokens *tokens, const void *q, const void *k, const void *v,
+                                    const int32_t *counts, const int32_t *positions, const float *inv_freq, const int32_t *page_table,
+                                    const int32_t *lengths, void *q_out, void *k_pool, void *v_pool, void *bounds, void *stream)
+{
+    const char *who = "sablock_append_paged";
+    PageDims pd;
+    TokenDims td;
+    PageView pv;
+    sablock_status st = make_append(who, pages, tokens, q, k, v, positions, inv_freq, page_table, lengths, q_out, k_pool, v_pool, bounds, &pd, &td, &pv);
+    if (st != SABLOCK_OK) return st;
     return dev(launch_append_paged(pd, td, q, k, v, counts, positions, inv_freq, pv, q_out, static_cast<hipStream_t>(stream)), who);
+}
+
+sablock_status sablock_append_normed_paged(const sablock_pages *pages, const sablock_new_tokens *tokens, const sablock_head_norms *norms, const void *q,
+                                           const void *k, const void *v, const float *q_weight, const float *k_weight, const int32_t *counts,
+                                           const int32_t *positions, const float *inv_freq, const int32_t *page_table, const int32_t *lengths,
+                                           void *q_out, void *k_pool, void *v_pool, void *bounds, void *stream)
+{
+    const char *who = "sablock_append_normed_paged";
+    PageDims pd;
+    TokenDims td;
+    PageView pv;
+    sablock_status st = make_append(who, pages, tokens, q, k, v, positions, inv_freq, page_table, lengths, q_out, k_pool, v_pool, bounds, &pd, &td, &pv);
+    if (st != SABLOCK_OK) return st;
+    if (!norms || !k_weight || (q && !q_weight)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (!(norms->eps > 0.f) || norms->eps > FLT_MAX) return fail(SABLOCK_ERR_INVALID_ARG, "%s: eps must be positive and finite", who);
+    if (norms->per_head != 0 && norms->per_head != 1) return fail(SABLOCK_ERR_INVALID_ARG, "%s: per_head must be 0 or 1", who);
+    if (norms->reserved[0] || norms->reserved[1]) return fail(SABLOCK_ERR_INVALID_ARG, "%s: reserved must be 0", who);
+    if (!aligned16(q_weight) || !aligned16(k_weight)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: the weights must be 16-byte aligned", who);
+    const NormDims nd{q ? q_weight : k_weight, k_weight, norms->eps, norms->per_head};
+    return dev(launch_append_normed_paged(pd, td, nd, q, k, v, counts, positions, inv_freq, pv, q_out, static_cast<hipStream_t>(stream)), who);
 }
 
 static sablock_status make_decode_pages(const char *who, const sablock_pages *pages, PageDims *pd)

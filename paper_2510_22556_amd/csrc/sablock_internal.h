@@ -307,6 +307,7 @@ struct PageView {                                             // the cache's dev
     char *k, *v, *bounds;                                     // bounds: nullable
 };
 struct TokenDims { int32_t n_new, R, interleaved; int64_t qs[4], ks[4], vs[4]; };
+struct NormDims { const float *q_weight, *k_weight; float eps; int32_t per_head; };            // weights [layer][head, if per_head][D]
 
 __host__ __device__ inline int32_t seq_of_problem(const PageDims &d, int32_t p) { return quotient(p, d.inv_seq); }
 __host__ __device__ inline int32_t head_of_problem(const PageDims &d, int32_t p) { return p - quotient(p, d.inv_heads) * d.Hkv; }
@@ -329,6 +330,8 @@ hipError_t launch_compact_paged(const Dims &d, const void *k, const void *v, con
                                 const PageDims &pd, const PageView &pv, int32_t *lengths_out, hipStream_t st);
 hipError_t launch_append_paged(const PageDims &pd, const TokenDims &td, const void *q, const void *k, const void *v, const int32_t *counts,
                                const int32_t *positions, const float *inv_freq, const PageView &pv, void *q_out, hipStream_t st);
+hipError_t launch_append_normed_paged(const PageDims &pd, const TokenDims &td, const NormDims &nd, const void *q, const void *k, const void *v,
+                                      const int32_t *counts, const int32_t *positions, const float *inv_freq, const PageView &pv, void *q_out, hipStream_t st);
 bool decode_paged_supported(const PageDims &pd);
 size_t decode_paged_ws_bytes(const PageDims &pd);
 hipError_t launch_decode_paged(const PageDims &pd, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out,
