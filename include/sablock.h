@@ -498,6 +498,27 @@ SABLOCK_API sablock_status sablock_select_pages(const sablock_pages *pages, cons
                                     const int32_t *page_table, const int32_t *lengths, int32_t n_pick, int32_t n_first,
                                     int32_t n_last, int32_t *list_out, void *ws, size_t ws_bytes, void *stream);
 
+/* Eviction: every sequence of more than n_keep rows is cut to n_keep of them, per problem the first n_first, the last n_last
+ * and, of the others, those of the largest weights (equal weights: the lower row first; a weight that is no number counts as the
+ * largest).  The rows that stay go, in their order and bit for bit, K, V and weight, to the rows 0 .. of the pages that page_table_out names; a
+ * sequence of no more than n_keep rows goes there whole.  Nothing else is written: the pages that the rows came from stay as they are, so that they
+ * may be other sequences' too (a shared prefix), and are the caller's to use again once all layers' rows have moved.
+ *   weights        [n_layers][n_pages][n_kv_heads][page_size] fp32, dense, 16-byte aligned: of every row, what sablock_decode_weighed_paged
+ *                  gathers in them or any other number
+ *   page_table_out [n_seq][max_pages]: of its pages, those in front of ceil(rows that stay / page_size) are named once, and none of them
+ *                  lies within a sequence's old rows
+ *   lengths_out    [n_seq]: min(rows, n_keep).  An array of its own, as the new table is: the calls of all layers take the old ones
+ *   rows_out       [P][n_keep] int32: the old rows that stay, ascending, -1 behind the last
+ *   bounds         nullable; written for every page that gets a row
+ *   ws             at least sablock_evict_paged_workspace_bytes(pages) bytes, 16-byte aligned
+ * A row whose page does not exist has less weight than any number; where it stays all the same, it becomes a row of zeros of weight 0.
+ * n_keep >= 1, n_first, n_last >= 0, n_first + n_last <= n_keep (INVALID_ARG otherwise). */
+SABLOCK_API sablock_status sablock_evict_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out);
+SABLOCK_API sablock_status sablock_evict_paged(const sablock_pages *pages, const int32_t *page_table, const int32_t *lengths,
+                                    int32_t n_keep, int32_t n_first, int32_t n_last, const int32_t *page_table_out,
+                                    int32_t *lengths_out, int32_t *rows_out, float *weights, void *k_pool, void *v_pool,
+                                    void *bounds /* nullable */, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

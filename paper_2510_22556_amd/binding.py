@@ -31,7 +31,8 @@ EXPORTS = ("sablock_version", "sablock_last_error", "sablock_workspace_bytes", "
            "sablock_window_attention", "sablock_score_static", "sablock_stream_probe", "sablock_validate_segments",
            "sablock_segment_slices", "sablock_segment_slice_count", "sablock_segment_slice_offsets",
            "sablock_compact_paged", "sablock_append_paged", "sablock_decode_paged_workspace_bytes", "sablock_decode_paged",
-           "sablock_select_pages_workspace_bytes", "sablock_select_pages", "sablock_append_normed_paged")
+           "sablock_select_pages_workspace_bytes", "sablock_select_pages", "sablock_append_normed_paged",
+           "sablock_evict_paged_workspace_bytes", "sablock_evict_paged")
 
 
 class SablockError(RuntimeError):
@@ -134,6 +135,8 @@ def load():
         lib.sablock_decode_paged.argtypes = [pp, vp, vp, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
         lib.sablock_select_pages_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
         lib.sablock_select_pages.argtypes = [pp, vp, vp, vp, vp, i32, i32, i32, vp, vp, ctypes.c_size_t, vp]
+        lib.sablock_evict_paged_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
+        lib.sablock_evict_paged.argtypes = [pp, vp, vp, i32, i32, i32] + [vp] * 8 + [ctypes.c_size_t, vp]
         for n in EXPORTS[2:]:
             getattr(lib, n).restype = ctypes.c_int
         _lib = lib
@@ -497,6 +500,7 @@ class _Layout(NamedTuple):
     problems: int
     queries: int                               # elements of one query per head
     bounds: int                                # elements
+    weights: int                               # rows of all pages, in every layer and head
 
 
 def _dtype_of(code: int):
@@ -509,7 +513,8 @@ def _cache_layout(pages: bytes) -> _Layout:
     n_seq, n_layers, n_q_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_pages, _, _, _, *steps = struct.unpack_from("12i8q", pages)
     sizes = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
     return _Layout(_dtype_of(dtype), n_seq, max_pages, _extent("K pool", sizes, (*steps[:4], 1)), _extent("V pool", sizes, (*steps[4:], 1)),
-                   n_seq * n_layers * n_kv_heads, n_seq * n_layers * n_q_heads * head_dim, 2 * n_layers * n_pages * n_kv_heads * head_dim)
+                   n_seq * n_layers * n_kv_heads, n_seq * n_layers * n_q_heads * head_dim, 2 * n_layers * n_pages * n_kv_heads * head_dim,
+                   n_layers * n_pages * n_kv_heads * page_size)
 
 
 @lru_cache(256)
@@ -615,6 +620,29 @@ def sablock_select_pages(pages: CPages, q, bounds, page_table, lengths, n_pick: 
     _all_dense((_torch.int32, c.n_seq, lengths), (_torch.int32, c.problems * n_pick, list_out), (c.dtype, c.queries, q), (c.dtype, c.bounds, bounds))
     _check(lib.sablock_select_pages(ctypes.byref(pages), q_at, b, table, rows, n_pick, n_first, n_last, listed, ws_at,
                                     ws.numel() * ws.element_size(), _stream(stream, device)))
+
+
+def sablock_evict_paged_workspace_bytes(pages: CPages) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().sablock_evict_paged_workspace_bytes(ctypes.byref(pages), ctypes.byref(out)))
+    return int(out.value)
+
+
+def sablock_evict_paged(pages: CPages, page_table, lengths, weights, k_pool, v_pool, n_keep: int, page_table_out, lengths_out, rows_out, ws,
+                        n_first: int = 0, n_last: int = 1, bounds=None, stream=None):
+    """``page_table`` and ``lengths`` are the old ones; ``page_table_out`` names the pages that the rows go to."""
+    lib = load()
+    device, table, rows, w, kp, vp, table_out, len_out, kept, ws_at, b = _pointers(page_table, lengths, weights, k_pool, v_pool, page_table_out, lengths_out,
+                                                                                   rows_out, ws, bounds)
+    c = _cache_layout(bytes(pages))
+    _table(c, page_table)
+    _table(c, page_table_out)
+    _strided(c.dtype, (k_pool, c.k_pool), (v_pool, c.v_pool))
+    i32 = _torch.int32
+    _all_dense((i32, c.n_seq, lengths), (i32, c.n_seq, lengths_out), (i32, c.problems * n_keep, rows_out), (_torch.float32, c.weights, weights),
+               (c.dtype, c.bounds, bounds))
+    _check(lib.sablock_evict_paged(ctypes.byref(pages), table, rows, n_keep, n_first, n_last, table_out, len_out, kept, w, kp, vp, b, ws_at,
+                                   ws.numel() * ws.element_size(), _stream(stream, device)))
 
 
 class PagedCache:

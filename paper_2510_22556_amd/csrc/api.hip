@@ -864,4 +864,37 @@ sablock_status sablock_select_pages(const sablock_pages *pages, const void *q, c
     return dev(launch_select_pages(pd, q, pv, n_pick, n_first, n_last, list_out, ws, static_cast<hipStream_t>(stream)), who);
 }
 
+sablock_status sablock_evict_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out)
+{
+    if (!bytes_out) return fail(SABLOCK_ERR_INVALID_ARG, "bytes_out is NULL");
+    PageDims pd;
+    sablock_status st = make_pages("sablock_evict_paged_workspace_bytes", pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    *bytes_out = evict_ws_bytes(pd);
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_evict_paged(const sablock_pages *pages, const int32_t *page_table, const int32_t *lengths, int32_t n_keep, int32_t n_first,
+                                   int32_t n_last, const int32_t *page_table_out, int32_t *lengths_out, int32_t *rows_out, float *weights,
+                                   void *k_pool, void *v_pool, void *bounds, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "sablock_evict_paged";
+    PageDims pd;
+    sablock_status st = make_pages(who, pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    if (!lengths || !page_table_out || !lengths_out || !rows_out || !weights) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (page_table_out == page_table || lengths_out == lengths)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: the table and the lengths of the rows that stay are arrays of their own", who);
+    if (n_keep < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > n_keep)
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: need n_keep >= 1 and n_first + n_last <= n_keep, none negative", who);
+    if (!aligned16(weights) || !aligned16(ws)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: the weights and the workspace must be 16-byte aligned", who);
+    PageView pv;
+    st = make_page_view(who, page_table, lengths, k_pool, v_pool, bounds, &pv);
+    if (st != SABLOCK_OK) return st;
+    const size_t need = evict_ws_bytes(pd);
+    if (!ws || ws_bytes < need) return fail(SABLOCK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+    const EvictDims ed{page_table_out, weights, lengths_out, rows_out, n_keep, n_first, n_last};
+    return dev(launch_evict(pd, pv, ed, ws, static_cast<hipStream_t>(stream)), who);
+}
+
 }  // extern "C"

@@ -1,0 +1,106 @@
+// Eviction from the paged cache: of every problem the rows that have gathered the most weight, with the first and the last ones, into the pages of
+// another table, in their order.
+//
+//   row_keys_kernel    the weights of a problem's rows, out of its pages, as whole numbers of the same order, side by side.
+//   pick_pages_kernel  (paged_select.hip) takes rows here: the first, the last, and the largest of the others, ascending.
+//   evict_kernel       a workgroup fills one page of one problem: K, V and weights of its rows, and the page's bounds.  The rows' places are found
+//       once, by a thread each, and wait in LDS: list, table and row are loads that depend on each other.
+#include "paged_rows.h"
+
+namespace sablock {
+namespace {
+
+constexpr int KEY_ROWS = 4;                    // of a thread, in one page
+constexpr int KEY_WGS = 8;                     // workgroups of the keys per compute unit, at most
+
+// grid (parts, problems)
+__global__ void __launch_bounds__(NT)
+row_keys_kernel(PageDims d, PageView pv, const float *weights, uint32_t *keys, int64_t stride)
+{
+    const int p = blockIdx.y, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p);
+    const int n = rows_of(d, pv.lengths, s);
+    const int64_t step = (int64_t)gridDim.x * NT * KEY_ROWS;
+    for (int64_t r = ((int64_t)blockIdx.x * NT + threadIdx.x) * KEY_ROWS; r < n; r += step) {
+        const int id = page_at(d, pv.table, s, (int)(r >> d.shift));
+        f32x4 w{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (id >= 0) w = *reinterpret_cast<const f32x4 *>(weights + weight_at(d, layer, id, head) + (r & (d.page - 1)));
+        u32x4 key;
+#pragma unroll
+        for (int i = 0; i < KEY_ROWS; ++i) key[i] = w[i] == w[i] ? ordered_key(w[i]) : NOT_A_NUMBER;
+        *reinterpret_cast<u32x4 *>(keys + (int64_t)p * stride + r) = key;
+    }
+}
+
+// grid (pages of the rows that stay, problems)
+template <bool BF16>
+__global__ void __launch_bounds__(NT)
+evict_kernel(PageDims d, PageView pv, EvictDims ed, int chunks)
+{
+    using E = Elem<BF16>;
+    __shared__ __attribute__((aligned(16))) uint32_t sh[NT * 8];
+    __shared__ int2 from[NT];                                  // page, row in it
+    const int p = blockIdx.y, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p), tid = threadIdx.x;
+    const int len = rows_of(d, pv.lengths, s), kept = min(len, ed.n_keep);
+    if (blockIdx.x == 0 && layer == 0 && head == 0 && tid == 0) ed.lengths_out[s] = kept;
+    const int r0 = blockIdx.x << d.shift, n = min(d.page, kept - r0);
+    if (n <= 0) return;
+    const int id = page_at(d, ed.table_out, s, blockIdx.x);
+    if (id < 0) return;
+    if (tid < n) {
+        const int t = ed.rows_out[(int64_t)p * ed.n_keep + r0 + tid], at = t & (d.page - 1);
+        const int source = page_at(d, pv.table, s, t >> d.shift);
+        from[tid] = make_int2(source, at);
+        ed.weights[weight_at(d, layer, id, head) + tid] = source < 0 ? 0.f : ed.weights[weight_at(d, layer, source, head) + at];
+    }
+    __syncthreads();
+    const int groups = NT / chunks, group = tid / chunks, c = tid - group * chunks;
+    const bool active = group < groups;
+    const char *ksrc = pv.k + (layer * d.ks[0] + head * d.ks[2]) * E::BYTES + (int64_t)c * 16, *vsrc = pv.v + (layer * d.vs[0] + head * d.vs[2]) * E::BYTES + (int64_t)c * 16;
+    char *kdst = pv.k + (layer * d.ks[0] + id * d.ks[1] + head * d.ks[2]) * E::BYTES + (int64_t)c * 16;
+    char *vdst = pv.v + (layer * d.vs[0] + id * d.vs[1] + head * d.vs[2]) * E::BYTES + (int64_t)c * 16;
+    Bounds<BF16> b;
+    b.clear();
+    if (active)
+        for (int r = group; r < n; r += groups) {
+            const int2 f = from[r];
+            u32x4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
+            if (f.x >= 0) {
+                x = *reinterpret_cast<const u32x4 *>(ksrc + (f.x * d.ks[1] + f.y * d.ks[3]) * E::BYTES);
+                y = *reinterpret_cast<const u32x4 *>(vsrc + (f.x * d.vs[1] + f.y * d.vs[3]) * E::BYTES);
+            }
+            *reinterpret_cast<u32x4 *>(kdst + r * d.ks[3] * E::BYTES) = x;
+            *reinterpret_cast<u32x4 *>(vdst + r * d.vs[3] * E::BYTES) = y;
+            b.add(x);
+        }
+    if (!pv.bounds) return;
+    char *at = bounds_at(d, pv, layer, id, head);
+    store_joined<BF16>(b, sh, groups, chunks, group, c, active, d.D * E::BYTES, false, [&](int place) { return at + place * 16; });
+}
+
+int64_t row_stride(const PageDims &d) { return (int64_t)d.max_pages << d.shift; }
+
+}  // namespace
+
+size_t evict_ws_bytes(const PageDims &d) { return align256((size_t)d.P * row_stride(d) * 4); }
+
+hipError_t launch_evict(const PageDims &d, const PageView &pv, const EvictDims &ed, void *ws, hipStream_t st)
+{
+    uint32_t *keys = static_cast<uint32_t *>(ws);
+    const int64_t rows = row_stride(d), most = (rows + NT * KEY_ROWS - 1) / (NT * KEY_ROWS);
+    if (rows > ed.n_keep) {                                    // otherwise every row stays
+        const int64_t parts = std::min<int64_t>(most, (KEY_WGS * d.cus + d.P - 1) / d.P);
+        hipLaunchKernelGGL(row_keys_kernel, dim3((unsigned)parts, d.P), dim3(NT), 0, st, d, pv, ed.weights, keys, rows);
+    }
+    PageDims as_rows = d;                                      // pages of one row
+    as_rows.page = 1;
+    as_rows.shift = 0;
+    as_rows.max_pages = (int32_t)rows;
+    const hipError_t picked = launch_pick(as_rows, pv, ed.n_keep, ed.n_first, ed.n_last, keys, (int32_t)rows, ed.rows_out, st);
+    if (picked != hipSuccess) return picked;
+    const int64_t pages = (std::min<int64_t>(rows, ed.n_keep) + d.page - 1) >> d.shift;
+    hipLaunchKernelGGL(d.dtype == SABLOCK_BF16 ? evict_kernel<true> : evict_kernel<false>, dim3((unsigned)pages, d.P), dim3(NT), 0, st, d, pv, ed,
+                       d.D * elt_bytes(d) / 16);
+    return hipGetLastError();
+}
+
+}  // namespace sablock

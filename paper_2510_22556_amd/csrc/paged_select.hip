@@ -26,7 +26,6 @@ constexpr int NT = 256, PICK_NT = 1024;
 // and read, 209 us in place of 199).  Not so for more than eight query heads and rows of more than 256 bytes in bf16, 512 in fp32: the heads' elements
 // take 64 KB of LDS there, two run at a time, and the third comes behind them.
 constexpr int SCORE_WGS = 3;
-constexpr uint32_t NOT_A_NUMBER = 0xfffffffeu; // above every number's key
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -377,9 +376,15 @@ hipError_t launch_select_pages(const PageDims &d, const void *q, const PageView 
         const int parts = std::min({(d.max_pages + f.pages - 1) / f.pages, (SCORE_WGS * d.cus + d.P - 1) / d.P, (int)GRID_Y_MOST});
         hipLaunchKernelGGL(f.fn, dim3(d.P, parts), dim3(NT), 0, st, a);
     }
+    return launch_pick(d, pv, n_pick, n_first, n_last, a.keys, a.stride, list, st);
+}
+
+hipError_t launch_pick(const PageDims &d, const PageView &pv, int32_t n_pick, int32_t n_first, int32_t n_last, const uint32_t *keys, int32_t stride,
+                       int32_t *list, hipStream_t st)
+{
     const int run = (d.max_pages + PICK_NT - 1) / PICK_NT;     // per thread
     const auto pick = run <= 4 ? pick_pages_kernel<4> : run <= 8 ? pick_pages_kernel<8> : run <= 16 ? pick_pages_kernel<16> : pick_pages_kernel<0>;
-    hipLaunchKernelGGL(pick, dim3(d.P), dim3(PICK_NT), 0, st, d, pv, n_pick, n_first, n_last, a.keys, a.stride, list);
+    hipLaunchKernelGGL(pick, dim3(d.P), dim3(PICK_NT), 0, st, d, pv, n_pick, n_first, n_last, keys, stride, list);
     return hipGetLastError();
 }
 

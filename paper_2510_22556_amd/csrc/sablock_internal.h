@@ -66,6 +66,8 @@ __host__ __device__ inline int32_t layer_of_problem(const Dims &d, int32_t p)
     return quotient(p, d.inv_heads) - seq_of_problem(d, p) * d.n_layers;
 }
 
+constexpr uint32_t NOT_A_NUMBER = 0xfffffffeu; // the key of what is no number where that counts as the largest: above every number's
+
 // Grids over (parts, problems).  Workgroups go round the 8 XCDs, each of which has an L2
 // cache of 4 MiB; where what the steps hand on to each other (12 bytes per key) fits these caches, the problems come first, so that
 // with 8 problems, a layer of most models, every step finds what the one before it wrote in its own XCD's cache.  With more data
@@ -326,6 +328,12 @@ __host__ __device__ inline int32_t page_at(const PageDims &d, const int32_t *tab
     return (uint32_t)id < (uint32_t)d.n_pages ? id : -1;
 }
 
+// of row 0 of a page, in an array [n_layers][n_pages][Hkv][page]
+__host__ __device__ inline int64_t weight_at(const PageDims &d, int32_t layer, int32_t id, int32_t head)
+{
+    return (((int64_t)layer * d.n_pages + id) * d.Hkv + head) << d.shift;
+}
+
 hipError_t launch_compact_paged(const Dims &d, const void *k, const void *v, const int32_t *idx, int32_t budget, int32_t rows,
                                 const PageDims &pd, const PageView &pv, int32_t *lengths_out, hipStream_t st);
 hipError_t launch_append_paged(const PageDims &pd, const TokenDims &td, const void *q, const void *k, const void *v, const int32_t *counts,
@@ -339,5 +347,18 @@ hipError_t launch_decode_paged(const PageDims &pd, const void *q, const PageView
 size_t select_pages_ws_bytes(const PageDims &pd);
 hipError_t launch_select_pages(const PageDims &pd, const void *q, const PageView &pv, int32_t n_pick, int32_t n_first, int32_t n_last,
                                int32_t *list, void *ws, hipStream_t st);
+
+// n_pick of the first ceil(rows / page) keys [P][stride] of each problem: the first n_first and the last n_last, and the largest of the others
+hipError_t launch_pick(const PageDims &pd, const PageView &pv, int32_t n_pick, int32_t n_first, int32_t n_last, const uint32_t *keys, int32_t stride,
+                       int32_t *list, hipStream_t st);
+
+struct EvictDims {
+    const int32_t *table_out;
+    float *weights;                                           // [n_layers][n_pages][Hkv][page]
+    int32_t *lengths_out, *rows_out;                          // rows_out [P][n_keep]
+    int32_t n_keep, n_first, n_last;
+};
+size_t evict_ws_bytes(const PageDims &pd);
+hipError_t launch_evict(const PageDims &pd, const PageView &pv, const EvictDims &ed, void *ws, hipStream_t st);
 
 }  // namespace sablock
