@@ -498,6 +498,24 @@ SABLOCK_API sablock_status sablock_select_pages(const sablock_pages *pages, cons
                                     const int32_t *page_table, const int32_t *lengths, int32_t n_pick, int32_t n_first,
                                     int32_t n_last, int32_t *list_out, void *ws, size_t ws_bytes, void *stream);
 
+/* sablock_decode_paged (all pages) that also adds every row's share of the attention to what the row has gathered so far:
+ *   out[h] = softmax_r(<q[h], K[r]> / sqrt(D)) . V[r],   weights[r] <- decay * weights[r] + sum over the G query heads of softmax_r
+ *   weights     [n_layers][n_pages][n_kv_heads][page_size] fp32, dense, 16-byte aligned, beside the pools: row r % page_size of its page.  What
+ *               sablock_evict_paged takes.  Rows behind a sequence's last stay as they are.
+ *   n_new       the last rows of every sequence, which have gathered nothing: their weights are begun, whatever lies there
+ *   counts      nullable (every sequence has n_new), or [n_seq] int32, taken as 0 .. n_new: both as in the append in front of this step
+ *   decay       finite, >= 0: 1 keeps what was gathered, 0 forgets it
+ *   ws          at least sablock_decode_weighed_paged_workspace_bytes(pages) bytes, 16-byte aligned: the logits of all rows that the table has
+ *               room for are among them, 4 bytes per row and query head
+ * Different entries within the sequences' lengths may not name one page: this call writes to it.  A row of a page that does not exist has
+ * no share; a head without a finite logit adds nothing, one whose softmax is no number makes all its KV head's weights so.
+ * q, out and what is supported as in sablock_decode_paged. */
+SABLOCK_API sablock_status sablock_decode_weighed_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out);
+SABLOCK_API sablock_status sablock_decode_weighed_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool,
+                                    const int32_t *page_table, const int32_t *lengths, int32_t n_new,
+                                    const int32_t *counts /* nullable */, float decay, float *weights, float *out,
+                                    void *ws, size_t ws_bytes, void *stream);
+
 /* Eviction: every sequence of more than n_keep rows is cut to n_keep of them, per problem the first n_first, the last n_last
  * and, of the others, those of the largest weights (equal weights: the lower row first; a weight that is no number counts as the
  * largest).  The rows that stay go, in their order and bit for bit, K, V and weight, to the rows 0 .. of the pages that page_table_out names; a

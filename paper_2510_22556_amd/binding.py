@@ -32,7 +32,8 @@ EXPORTS = ("sablock_version", "sablock_last_error", "sablock_workspace_bytes", "
            "sablock_segment_slices", "sablock_segment_slice_count", "sablock_segment_slice_offsets",
            "sablock_compact_paged", "sablock_append_paged", "sablock_decode_paged_workspace_bytes", "sablock_decode_paged",
            "sablock_select_pages_workspace_bytes", "sablock_select_pages", "sablock_append_normed_paged",
-           "sablock_evict_paged_workspace_bytes", "sablock_evict_paged")
+           "sablock_evict_paged_workspace_bytes", "sablock_evict_paged", "sablock_decode_weighed_paged_workspace_bytes",
+           "sablock_decode_weighed_paged")
 
 
 class SablockError(RuntimeError):
@@ -135,6 +136,8 @@ def load():
         lib.sablock_decode_paged.argtypes = [pp, vp, vp, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
         lib.sablock_select_pages_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
         lib.sablock_select_pages.argtypes = [pp, vp, vp, vp, vp, i32, i32, i32, vp, vp, ctypes.c_size_t, vp]
+        lib.sablock_decode_weighed_paged_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
+        lib.sablock_decode_weighed_paged.argtypes = [pp, vp, vp, vp, vp, vp, i32, vp, f32, vp, vp, vp, ctypes.c_size_t, vp]
         lib.sablock_evict_paged_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
         lib.sablock_evict_paged.argtypes = [pp, vp, vp, i32, i32, i32] + [vp] * 8 + [ctypes.c_size_t, vp]
         for n in EXPORTS[2:]:
@@ -620,6 +623,27 @@ def sablock_select_pages(pages: CPages, q, bounds, page_table, lengths, n_pick: 
     _all_dense((_torch.int32, c.n_seq, lengths), (_torch.int32, c.problems * n_pick, list_out), (c.dtype, c.queries, q), (c.dtype, c.bounds, bounds))
     _check(lib.sablock_select_pages(ctypes.byref(pages), q_at, b, table, rows, n_pick, n_first, n_last, listed, ws_at,
                                     ws.numel() * ws.element_size(), _stream(stream, device)))
+
+
+def sablock_decode_weighed_paged_workspace_bytes(pages: CPages) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().sablock_decode_weighed_paged_workspace_bytes(ctypes.byref(pages), ctypes.byref(out)))
+    return int(out.value)
+
+
+def sablock_decode_weighed_paged(pages: CPages, q, k_pool, v_pool, page_table, lengths, weights, out, ws, n_new: int = 1, counts=None, decay: float = 1.0,
+                                 stream=None):
+    """``sablock_decode_paged`` that adds every row's share to ``weights [n_layers, n_pages, Hkv, page_size]``; the last ``n_new`` rows of a sequence (or
+    those of ``counts``, if fewer) have gathered nothing yet."""
+    lib = load()
+    device, q_at, kp, vp, table, rows, w, o, ws_at, count = _pointers(q, k_pool, v_pool, page_table, lengths, weights, out, ws, counts)
+    c = _cache_layout(bytes(pages))
+    _table(c, page_table)
+    _strided(c.dtype, (k_pool, c.k_pool), (v_pool, c.v_pool))
+    i32, f32 = _torch.int32, _torch.float32
+    _all_dense((i32, c.n_seq, lengths), (i32, c.n_seq, counts), (f32, c.weights, weights), (c.dtype, c.queries, q), (f32, c.queries, out))
+    _check(lib.sablock_decode_weighed_paged(ctypes.byref(pages), q_at, kp, vp, table, rows, n_new, count, decay, w, o, ws_at, ws.numel() * ws.element_size(),
+                                            _stream(stream, device)))
 
 
 def sablock_evict_paged_workspace_bytes(pages: CPages) -> int:

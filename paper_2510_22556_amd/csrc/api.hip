@@ -864,6 +864,37 @@ sablock_status sablock_select_pages(const sablock_pages *pages, const void *q, c
     return dev(launch_select_pages(pd, q, pv, n_pick, n_first, n_last, list_out, ws, static_cast<hipStream_t>(stream)), who);
 }
 
+sablock_status sablock_decode_weighed_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out)
+{
+    if (!bytes_out) return fail(SABLOCK_ERR_INVALID_ARG, "bytes_out is NULL");
+    PageDims pd;
+    sablock_status st = make_decode_pages("sablock_decode_weighed_paged_workspace_bytes", pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    *bytes_out = decode_weighed_ws_bytes(pd);
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_decode_weighed_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table,
+                                            const int32_t *lengths, int32_t n_new, const int32_t *counts, float decay, float *weights, float *out,
+                                            void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "sablock_decode_weighed_paged";
+    PageDims pd;
+    sablock_status st = make_decode_pages(who, pages, &pd);
+    if (st != SABLOCK_OK) return st;
+    if (!q || !lengths || !weights || !out) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (!aligned16(q) || !aligned16(weights) || !aligned16(ws))
+        return fail(SABLOCK_ERR_INVALID_ARG, "%s: q, the weights and the workspace must be 16-byte aligned", who);
+    if (n_new < 0) return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_new < 0", who);
+    if (!(decay >= 0.f) || decay > FLT_MAX) return fail(SABLOCK_ERR_INVALID_ARG, "%s: decay must be finite and not negative", who);
+    PageView pv;
+    st = make_page_view(who, page_table, lengths, k_pool, v_pool, nullptr, &pv);
+    if (st != SABLOCK_OK) return st;
+    const size_t need = decode_weighed_ws_bytes(pd);
+    if (!ws || ws_bytes < need) return fail(SABLOCK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+    return dev(launch_decode_weighed(pd, q, pv, counts, n_new, decay, weights, out, ws, static_cast<hipStream_t>(stream)), who);
+}
+
 sablock_status sablock_evict_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out)
 {
     if (!bytes_out) return fail(SABLOCK_ERR_INVALID_ARG, "bytes_out is NULL");
