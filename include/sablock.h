@@ -516,6 +516,22 @@ SABLOCK_API sablock_status sablock_decode_weighed_paged(const sablock_pages *pag
                                     const int32_t *counts /* nullable */, float decay, float *weights, float *out,
                                     void *ws, size_t ws_bytes, void *stream);
 
+/* sablock_decode_paged (all pages) for a batch in which sequences have their first pages in common: those are read once for all of
+ * them, and the sequences' own rows behind them as ever.  The same arguments and results (sums in another order), and
+ *   prefix_begin  [n_prefixes + 1] device int32, ascending: prefix i is that of the sequences prefix_begin[i] .. prefix_begin[i+1] - 1; other
+ *                 sequences have none
+ *   prefix_pages  [n_prefixes] device int32: so many entries at the front of these sequences' rows of the table are the same; they are read from one
+ *                 of them, for those sequences that have all the rows of these pages.  One that ends before is read by itself, as are the
+ *                 sequences of a prefix that only one has.
+ *   ws            at least sablock_decode_prefix_paged_workspace_bytes(pages, n_prefixes) bytes, 16-byte aligned
+ * Appends go behind the prefix as ever, into pages that only their sequence has: a prefix is whole pages.
+ * 1 <= n_prefixes <= 4096.  Values out of range in prefix_begin and prefix_pages are taken as the nearest in range. */
+SABLOCK_API sablock_status sablock_decode_prefix_paged_workspace_bytes(const sablock_pages *pages, int32_t n_prefixes, size_t *bytes_out);
+SABLOCK_API sablock_status sablock_decode_prefix_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool,
+                                    const int32_t *page_table, const int32_t *lengths, const int32_t *prefix_begin,
+                                    const int32_t *prefix_pages, int32_t n_prefixes, float *out, void *ws, size_t ws_bytes,
+                                    void *stream);
+
 /* Eviction: every sequence of more than n_keep rows is cut to n_keep of them, per problem the first n_first, the last n_last
  * and, of the others, those of the largest weights (equal weights: the lower row first; a weight that is no number counts as the
  * largest).  The rows that stay go, in their order and bit for bit, K, V and weight, to the rows 0 .. of the pages that page_table_out names; a

@@ -33,7 +33,7 @@ EXPORTS = ("sablock_version", "sablock_last_error", "sablock_workspace_bytes", "
            "sablock_compact_paged", "sablock_append_paged", "sablock_decode_paged_workspace_bytes", "sablock_decode_paged",
            "sablock_select_pages_workspace_bytes", "sablock_select_pages", "sablock_append_normed_paged",
            "sablock_evict_paged_workspace_bytes", "sablock_evict_paged", "sablock_decode_weighed_paged_workspace_bytes",
-           "sablock_decode_weighed_paged")
+           "sablock_decode_weighed_paged", "sablock_decode_prefix_paged_workspace_bytes", "sablock_decode_prefix_paged")
 
 
 class SablockError(RuntimeError):
@@ -138,6 +138,8 @@ def load():
         lib.sablock_select_pages.argtypes = [pp, vp, vp, vp, vp, i32, i32, i32, vp, vp, ctypes.c_size_t, vp]
         lib.sablock_decode_weighed_paged_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
         lib.sablock_decode_weighed_paged.argtypes = [pp, vp, vp, vp, vp, vp, i32, vp, f32, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.sablock_decode_prefix_paged_workspace_bytes.argtypes = [pp, i32, ctypes.POINTER(ctypes.c_size_t)]
+        lib.sablock_decode_prefix_paged.argtypes = [pp] + [vp] * 7 + [i32, vp, vp, ctypes.c_size_t, vp]
         lib.sablock_evict_paged_workspace_bytes.argtypes = [pp, ctypes.POINTER(ctypes.c_size_t)]
         lib.sablock_evict_paged.argtypes = [pp, vp, vp, i32, i32, i32] + [vp] * 8 + [ctypes.c_size_t, vp]
         for n in EXPORTS[2:]:
@@ -644,6 +646,26 @@ def sablock_decode_weighed_paged(pages: CPages, q, k_pool, v_pool, page_table, l
     _all_dense((i32, c.n_seq, lengths), (i32, c.n_seq, counts), (f32, c.weights, weights), (c.dtype, c.queries, q), (f32, c.queries, out))
     _check(lib.sablock_decode_weighed_paged(ctypes.byref(pages), q_at, kp, vp, table, rows, n_new, count, decay, w, o, ws_at, ws.numel() * ws.element_size(),
                                             _stream(stream, device)))
+
+
+def sablock_decode_prefix_paged_workspace_bytes(pages: CPages, n_prefixes: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().sablock_decode_prefix_paged_workspace_bytes(ctypes.byref(pages), n_prefixes, ctypes.byref(out)))
+    return int(out.value)
+
+
+def sablock_decode_prefix_paged(pages: CPages, q, k_pool, v_pool, page_table, lengths, prefix_begin, prefix_pages, out, ws, stream=None):
+    """``sablock_decode_paged`` where the sequences ``prefix_begin[i] .. prefix_begin[i + 1] - 1`` have their first ``prefix_pages[i]`` pages in common;
+    both int32, on the device."""
+    lib = load()
+    device, q_at, kp, vp, table, rows, begin, n_pages, o, ws_at = _pointers(q, k_pool, v_pool, page_table, lengths, prefix_begin, prefix_pages, out, ws)
+    c, n = _cache_layout(bytes(pages)), prefix_pages.numel()
+    _table(c, page_table)
+    _strided(c.dtype, (k_pool, c.k_pool), (v_pool, c.v_pool))
+    i32 = _torch.int32
+    _all_dense((i32, c.n_seq, lengths), (i32, n + 1, prefix_begin), (i32, n, prefix_pages), (c.dtype, c.queries, q), (_torch.float32, c.queries, out))
+    _check(lib.sablock_decode_prefix_paged(ctypes.byref(pages), q_at, kp, vp, table, rows, begin, n_pages, n, o, ws_at, ws.numel() * ws.element_size(),
+                                           _stream(stream, device)))
 
 
 def sablock_evict_paged_workspace_bytes(pages: CPages) -> int:

@@ -895,6 +895,43 @@ sablock_status sablock_decode_weighed_paged(const sablock_pages *pages, const vo
     return dev(launch_decode_weighed(pd, q, pv, counts, n_new, decay, weights, out, ws, static_cast<hipStream_t>(stream)), who);
 }
 
+static sablock_status make_prefix_pages(const char *who, const sablock_pages *pages, int32_t n_prefixes, PageDims *pd)
+{
+    sablock_status st = make_decode_pages(who, pages, pd);
+    if (st != SABLOCK_OK) return st;
+    if (n_prefixes < 1) return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_prefixes must be >= 1", who);
+    if (n_prefixes > MAX_PAGED_SEQ) return fail(SABLOCK_ERR_UNSUPPORTED, "%s: n_prefixes %d: at most %d per call", who, n_prefixes, MAX_PAGED_SEQ);
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_decode_prefix_paged_workspace_bytes(const sablock_pages *pages, int32_t n_prefixes, size_t *bytes_out)
+{
+    if (!bytes_out) return fail(SABLOCK_ERR_INVALID_ARG, "bytes_out is NULL");
+    PageDims pd;
+    sablock_status st = make_prefix_pages("sablock_decode_prefix_paged_workspace_bytes", pages, n_prefixes, &pd);
+    if (st != SABLOCK_OK) return st;
+    *bytes_out = decode_prefix_ws_bytes(pd, n_prefixes);
+    return SABLOCK_OK;
+}
+
+sablock_status sablock_decode_prefix_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table,
+                                           const int32_t *lengths, const int32_t *prefix_begin, const int32_t *prefix_pages, int32_t n_prefixes,
+                                           float *out, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "sablock_decode_prefix_paged";
+    PageDims pd;
+    sablock_status st = make_prefix_pages(who, pages, n_prefixes, &pd);
+    if (st != SABLOCK_OK) return st;
+    if (!q || !lengths || !prefix_begin || !prefix_pages || !out) return fail(SABLOCK_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (!aligned16(q) || !aligned16(ws)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: q and the workspace must be 16-byte aligned", who);
+    PageView pv;
+    st = make_page_view(who, page_table, lengths, k_pool, v_pool, nullptr, &pv);
+    if (st != SABLOCK_OK) return st;
+    const size_t need = decode_prefix_ws_bytes(pd, n_prefixes);
+    if (!ws || ws_bytes < need) return fail(SABLOCK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+    return dev(launch_decode_prefix(pd, q, pv, prefix_begin, prefix_pages, n_prefixes, out, ws, static_cast<hipStream_t>(stream)), who);
+}
+
 sablock_status sablock_evict_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out)
 {
     if (!bytes_out) return fail(SABLOCK_ERR_INVALID_ARG, "bytes_out is NULL");

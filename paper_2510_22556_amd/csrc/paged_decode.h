@@ -94,13 +94,31 @@ struct DecodePagedArgs {
     float *sums;                 // pieces [2 * workgroups][G][D]
     static constexpr bool STATS = false;         // a problem's reference and denominator go out too
     static constexpr bool LOGITS = false;        // and its logits
+    static constexpr bool SKIP = false;          // the first pages of some sequences are another kernel's: a.skipped(s, rows) of them
 };
+
+// rows of a sequence that are this kernel's
+template <typename Args>
+__device__ __forceinline__ int rows_here(const Args &a, int s)
+{
+    const int rows = rows_of(a.d, a.pv.lengths, s);
+    if constexpr (Args::SKIP) return rows - (a.skipped(s, rows) << a.d.shift);
+    else return rows;
+}
+
+// and the page of place i of those
+template <typename Args>
+__device__ __forceinline__ int page_here(const Args &a, int s, int i)
+{
+    if constexpr (Args::SKIP) i += a.skipped(s, rows_of(a.d, a.pv.lengths, s));
+    return page_at(a.d, a.pv.table, s, i);
+}
 
 // steps of a problem of sequence s
 template <int STEP, typename Args>
 __device__ __forceinline__ int steps_of(const Args &a, int s)
 {
-    const int len = rows_of(a.d, a.pv.lengths, s);
+    const int len = rows_here(a, s);
     int rows = len;
     if (a.list) {
         const int pages = (len + a.d.page - 1) >> a.d.shift;
@@ -244,7 +262,7 @@ decode_paged_kernel(Args a)
     auto piece = [&](int p, int s, int off, int count, int n) __attribute__((always_inline)) {
         const int layer = layer_of_problem(d, p), head = head_of_problem(d, p);
         // not made uniform: with the length in a scalar register the compiler's order of the loop is 2 % slower
-        const int len = rows_of(d, a.pv.lengths, s), pages = (len + d.page - 1) >> d.shift;
+        const int len = rows_here(a, s), pages = (len + d.page - 1) >> d.shift;
         const int entries = a.list ? min(a.n_listed, pages) : pages;
         const int64_t qrow = (((int64_t)s * d.n_layers + layer) * d.Hq + head * d.G) * D;
 
@@ -272,7 +290,7 @@ decode_paged_kernel(Args a)
                 if (a.list && e < entries) at = a.list[(int64_t)p * a.n_listed + e];
                 ids = held = 0;
                 if (e < entries && (uint32_t)at < (uint32_t)pages) {
-                    const int id = page_at(d, a.pv.table, s, at);
+                    const int id = page_here(a, s, at);
                     if (id >= 0) {
                         ids = id;
                         held = min(d.page, len - (at << d.shift));

@@ -1,0 +1,477 @@
+// Decode attention of a batch whose sequences have their first pages in common: those are read once for all of them.
+//
+//   decode_paged_kernel (paged_decode.h)   every sequence's own rows, with the reference and denominator of each head.
+//   prefix_kernel    The columns of a prefix are the queries of all its sequences and of the KV head's query heads, side by side without a gap;
+//       its rows are cut into pieces.  A workgroup takes a block of columns over a piece of the rows and leaves references, denominators
+//       and numerators in the workspace.  Pieces are dealt out by every workgroup for itself: the prefixes, which only the device knows, are few.
+//   join_kernel      joins the pieces of a sequence's prefix with its own rows.
+//
+// A sequence takes part in its prefix if all the prefix's rows are its own; one that ends before reads its rows by itself, so that no row of
+// the prefix has to be masked for one column and not for another.
+#include "paged_decode.h"
+
+namespace sablock {
+namespace {
+
+struct PrefixView { const int32_t *begin, *pages; int n; };    // device: [n + 1], [n]
+
+// Sequences of prefix i, and its pages: none where a single sequence has it
+struct Prefix { int first, count, pages; };
+__device__ __forceinline__ Prefix prefix_at(const PageDims &d, const PrefixView &v, int i)
+{
+    const int from = min(max(v.begin[i], 0), d.n_seq), to = min(max(v.begin[i + 1], 0), d.n_seq);
+    return Prefix{from, max(to - from, 0), to - from > 1 ? min(max(v.pages[i], 0), d.max_pages) : 0};
+}
+// the prefix of sequence s: the last one that begins at it or before, -1 for none
+__device__ __forceinline__ int prefix_of(const PrefixView &v, int s)
+{
+    int lo = -1, hi = v.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (v.begin[mid] <= s) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+struct PrefixArgs : DecodePagedArgs {
+    PrefixView prefixes;
+    float *stats;                // [P][G][2] of the sequences' own rows: reference (log2 domain), 1 / denominator
+    uint32_t inv_group;          // ceil(2^32 / G)
+    int slots;                   // pieces that the workspace has room for
+    float *piece_weights;        // [slots][columns][2]: reference, denominator
+    float *piece_sums;           // [slots][columns][D]
+    static constexpr bool STATS = true, SKIP = true;
+    // pages in front of the own rows of sequence s
+    __device__ __forceinline__ int skipped(int s, int rows) const
+    {
+        const int i = prefix_of(prefixes, s);
+        if (i < 0) return 0;
+        const Prefix x = prefix_at(d, prefixes, i);
+        return s < x.first + x.count && rows >> d.shift >= x.pages ? x.pages : 0;
+    }
+};
+
+constexpr int TILE = 16;                       // columns of a matrix product
+
+__device__ __forceinline__ int64_t over_wave(int64_t x)
+{
+    for (int m = 1; m < 64; m *= 2) x += (int64_t)__shfl_xor((long long)x, m);
+    return x;
+}
+
+// How the prefixes' rows are cut: pieces of `run` steps at most, as many as there are workgroups if those are enough.  A wavefront's view, a
+// prefix per lane, 64 of them at a time.
+template <int STEP, int COLUMNS>
+struct Cut {
+    const PrefixArgs &a;
+    int lane, run, heads;
+    struct Part { int first, count, pages, blocks, pieces; };  // blocks of columns of one problem; pieces of a block
+    __device__ Cut(const PrefixArgs &args, int l) : a(args), lane(l), heads(args.d.n_layers * args.d.Hkv)
+    {
+        int64_t steps = 0, blocks = 0;
+        for (int base = 0; base < a.prefixes.n; base += 64) {
+            const Prefix x = at(base + lane);
+            const int64_t b = x.pages ? (int64_t)heads * blocks_of(x) : 0;
+            steps += b * steps_of_pages(x.pages);
+            blocks += b;
+        }
+        steps = over_wave(steps);
+        blocks = over_wave(blocks);
+        const int64_t free = a.workgroups - blocks, shares = free > 0 ? free : a.workgroups;
+        run = (int)min(max((int64_t)LEAST_STEPS, (steps + shares - 1) / shares), (int64_t)1 << 27);      // no table has room for more
+    }
+    __device__ Prefix at(int i) const { return i < a.prefixes.n ? prefix_at(a.d, a.prefixes, i) : Prefix{0, 0, 0}; }
+    __device__ int blocks_of(const Prefix &x) const { return (x.count * a.d.G + COLUMNS - 1) / COLUMNS; }
+    __device__ int steps_of_pages(int pages) const { return ((pages << a.d.shift) + STEP - 1) / STEP; }
+    __device__ int pieces_of(const Prefix &x) const { return x.pages ? (steps_of_pages(x.pages) + run - 1) / run : 0; }
+    // the prefix that piece x of all lies in, and the pieces in front of it; -1 behind the last piece
+    __device__ int find(int x, int &before) const
+    {
+        before = 0;
+        for (int base = 0; base < a.prefixes.n; base += 64) {
+            const Prefix own = at(base + lane);
+            const int n = own.pages ? heads * blocks_of(own) * pieces_of(own) : 0, upto = sum_upto_lane(n) + before;
+            const unsigned long long behind = __ballot(upto > x);
+            if (behind) {
+                const int l = uniform(__ffsll(behind) - 1);
+                before = of_lane(upto, l) - of_lane(n, l);
+                return base + l;
+            }
+            before = of_lane(upto, 63);
+        }
+        return -1;
+    }
+    // pieces of the prefixes in front of prefix i
+    __device__ int before(int i) const
+    {
+        int sum = 0;
+        for (int base = 0; base < i; base += 64) {
+            const Prefix own = at(base + lane);
+            const int n = base + lane < i && own.pages ? heads * blocks_of(own) * pieces_of(own) : 0;
+            sum += of_lane(sum_upto_lane(n), 63);
+        }
+        return sum;
+    }
+};
+
+// CT: tiles of 16 columns of a workgroup, which every wavefront has; the steps of a piece are shared among the wavefronts.  A step is that of
+// decode_paged_kernel, with the operands of K and V used for all tiles.
+template <bool BF16, int EP, int STEP, int CT>
+__global__ void __launch_bounds__(NT)
+prefix_kernel(PrefixArgs a)
+{
+    constexpr int D = EP * 16, ELT = BF16 ? 2 : 4, R = STEP / 4, KT = STEP / 16, KC = D * ELT / 64, VW = EP * ELT / 4, KEEP = D / 4 + 2;
+    constexpr int COLUMNS = CT * TILE;
+    __shared__ float sh[(NW - 1) * KEEP * 64];
+    const PageDims &d = a.d;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = lane & 15, c = lane >> 4;
+    const int krow = KT == 2 ? (m >> 2) * 8 + (m & 3) : m, row = R * c;
+    const int64_t kstep = d.ks[3] * ELT, vstep = d.vs[3] * ELT;
+    // the first of a prefix's sequences that takes part in it: the others' rows of the table may not have its pages
+    auto first_member = [&](const Prefix &x) {
+        int at = 0;
+        for (; at < x.count; at += 64) {
+            const bool member = at + lane < x.count && rows_of(d, a.pv.lengths, min(x.first + at + lane, d.n_seq - 1)) >> d.shift >= x.pages;
+            const unsigned long long members = __ballot(member);
+            if (members) return uniform(at + __ffsll(members) - 1);
+        }
+        return x.count;
+    };
+    const Cut<STEP, COLUMNS> cut(a, lane);
+    for (int x = blockIdx.x; x < a.slots; x += a.workgroups) {
+        int before;
+        const int i = cut.find(x, before);
+        if (i < 0) return;
+        const Prefix prefix = prefix_at(d, a.prefixes, i);
+        const int blocks = cut.blocks_of(prefix), pieces = cut.pieces_of(prefix), n = cut.steps_of_pages(prefix.pages);
+        const int block = uniform(quotient(x - before, pieces)), j = uniform(x - before - block * pieces);
+        const int problem = uniform(quotient(block, blocks)), column0 = (block - problem * blocks) * COLUMNS;
+        const int layer = uniform(quotient(problem, d.Hkv)), head = problem - layer * d.Hkv;
+        const int columns = prefix.count * d.G, s = prefix.first + first_member(prefix);       // the table's row that is read
+        if (s >= prefix.first + prefix.count) continue;
+        const int off = j * cut.run, count = min(cut.run, n - off);
+
+        u32x4 q[CT][KC];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const int col = column0 + t * TILE + m, at = sablock::quotient(min(col, columns - 1), a.inv_group), g = min(col, columns - 1) - at * d.G;
+            const int64_t qrow = (((int64_t)(prefix.first + at) * d.n_layers + layer) * d.Hq + head * d.G + g) * D;
+#pragma unroll
+            for (int e = 0; e < KC; ++e) q[t][e] = *reinterpret_cast<const u32x4 *>(a.q + qrow * ELT + e * 64 + c * 16);
+        }
+        float ref[CT], den[CT];
+        f32x4 acc[CT][EP];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            ref[t] = -FLT_MAX;
+            den[t] = 0.f;
+#pragma unroll
+            for (int e = 0; e < EP; ++e) acc[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        const int from = off + (int)((int64_t)count * wave / NW), to = off + (int)((int64_t)count * (wave + 1) / NW);
+        int ids = -1, base = -1 << 30;                         // pages of 64 places at a time, one per lane
+        const char *kat = nullptr, *vat = nullptr;
+        bool whole = false, there = false;                     // all rows of the step exist; this lane's results' rows do
+        auto locate = [&](int st) {
+            const int r0 = st * STEP, e0 = r0 >> d.shift;
+            if (e0 - base >= 64) {
+                base = e0;
+                ids = e0 + lane < prefix.pages ? page_at(d, a.pv.table, s, e0 + lane) : -1;
+            }
+            const int at = e0 - base, in_page = r0 & (d.page - 1);
+            int idk = __builtin_amdgcn_readlane(ids, at), idv = idk;
+            int rk = in_page + krow, rv = in_page + row;
+            whole = there = idk >= 0;
+            if (KT == 2 && d.shift == 4) {                     // two pages; a lane's rows lie in one of them
+                const int id1 = at < 63 ? __builtin_amdgcn_readlane(ids, at + 1) : -1;
+                whole = idk >= 0 && id1 >= 0;
+                idk = krow < 16 ? idk : id1;
+                idv = row < 16 ? idv : id1;
+                there = idv >= 0;
+                rk &= 15;
+                rv &= 15;
+            }
+            kat = a.pv.k + (layer * d.ks[0] + max(idk, 0) * d.ks[1] + head * d.ks[2]) * ELT + rk * kstep + c * 16;
+            vat = a.pv.v + (layer * d.vs[0] + max(idv, 0) * d.vs[1] + head * d.vs[2]) * ELT + rv * vstep + m * EP * ELT;
+        };
+        u32x4 k[KT][KC];
+        uint32_t v[R][VW];
+        auto load_k = [&]() {
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int e = 0; e < KC; ++e) k[t][e] = *reinterpret_cast<const u32x4 *>(kat + t * 4 * kstep + e * 64);
+        };
+        auto load_v = [&]() {
+#pragma unroll
+            for (int r = 0; r < R; ++r) load_words<VW>(v[r], vat + r * vstep);
+        };
+        if (from < to) {
+            locate(from);
+            load_k();
+            load_v();
+        }
+        auto step = [&](int st, auto more) __attribute__((always_inline)) {
+            float z[CT][R];
+#pragma unroll
+            for (int u = 0; u < CT; ++u) {
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    f32x4 r{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < KC; ++e) {
+                        if constexpr (BF16) {
+                            r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][e]), __builtin_bit_cast(bf16x8, q[u][e]), r, 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int w = 0; w < 4; ++w)
+                                r = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][e][w]), __uint_as_float(q[u][e][w]), r, 0, 0, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) z[u][4 * t + w] = r[w] * a.qscale;
+                }
+                // read before any branch, see decode_paged_kernel
+#pragma unroll
+                for (int r = 0; r < R; ++r) asm volatile("" : "+v"(z[u][r]));
+            }
+            const bool now_whole = whole, now_there = there;
+            if constexpr (more.value) {
+                locate(st + 1);
+                load_k();
+            }
+            if (!now_whole) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (!now_there) {
+#pragma unroll
+                        for (int u = 0; u < CT; ++u) z[u][r] = -INFINITY;
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) v[r][w] = 0;
+                    }
+            }
+            bool moves = false;
+            float most[CT];
+#pragma unroll
+            for (int u = 0; u < CT; ++u) {
+                most[u] = z[u][0];
+#pragma unroll
+                for (int r = 1; r < R; ++r) most[u] = fmaxf(most[u], z[u][r]);
+                moves |= most[u] > ref[u];
+            }
+            if (__ballot(moves) != 0ull) {
+#pragma unroll
+                for (int u = 0; u < CT; ++u) {
+                    const float top = over_quarters(most[u], true), to_ref = top > ref[u] ? top + AHEAD : ref[u];
+                    const float f = __builtin_amdgcn_exp2f(ref[u] - to_ref);
+                    ref[u] = to_ref;
+                    den[u] *= f;
+#pragma unroll
+                    for (int e = 0; e < EP; ++e) acc[u][e] *= f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < CT; ++u)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    z[u][r] = __builtin_amdgcn_exp2f(z[u][r] - ref[u]);
+                    den[u] += z[u][r];
+                }
+            if constexpr (BF16) {
+                typedef uint32_t Operand __attribute__((ext_vector_type(R / 2)));
+                Operand part[CT][3];
+#pragma unroll
+                for (int u = 0; u < CT; ++u)
+#pragma unroll
+                    for (int r = 0; r < R / 2; ++r) {
+                        float lo = z[u][2 * r], hi = z[u][2 * r + 1];
+#pragma unroll
+                        for (int t = 0; t < 3; ++t) {
+                            part[u][t][r] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+                            lo = fmaf(z[u][2 * r], PART_LEAST, lo - __uint_as_float(__float_as_uint(lo) & 0xffff0000u));
+                            hi = fmaf(z[u][2 * r + 1], PART_LEAST, hi - __uint_as_float(__float_as_uint(hi) & 0xffff0000u));
+                        }
+                    }
+#pragma unroll
+                for (int e = 0; e < EP; ++e) {
+                    Operand o;
+#pragma unroll
+                    for (int r = 0; r < R / 2; ++r)
+                        o[r] = __builtin_amdgcn_perm(v[2 * r + 1][e / 2], v[2 * r][e / 2], e % 2 ? 0x07060302 : 0x05040100);
+#pragma unroll
+                    for (int u = 0; u < CT; ++u)
+#pragma unroll
+                        for (int t = 2; t >= 0; --t) {
+                            if constexpr (R == 8)
+                                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part[u][t]), acc[u][e], 0, 0, 0);
+                            else
+                                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, o), __builtin_bit_cast(s16x4, part[u][t]), acc[u][e], 0, 0, 0);
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int e = 0; e < EP; ++e)
+#pragma unroll
+                        for (int u = 0; u < CT; ++u)
+                            acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][e]), z[u][r], acc[u][e], 0, 0, 0);
+            }
+            if constexpr (more.value) load_v();
+        };
+        if (from < to) {
+            for (int st = from; st + 1 < to; ++st) step(st, std::true_type{});
+            step(to - 1, std::false_type{});
+        }
+        // the wavefronts' shares, lane by lane and tile by tile; the first one joins them
+#pragma unroll
+        for (int u = 0; u < CT; ++u) {
+            den[u] = over_quarters(den[u], false);
+            __syncthreads();                                   // of the tile before
+            if (wave > 0) {
+                float *o = sh + (wave - 1) * KEEP * 64 + lane;
+                o[0] = ref[u];
+                o[64] = den[u];
+#pragma unroll
+                for (int e = 0; e < EP; ++e)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) o[(2 + 4 * e + w) * 64] = acc[u][e][w];
+            }
+            __syncthreads();
+            const int col = u * TILE + m;
+            if (wave == 0 && column0 + col < columns) {        // elements EP (4 c + w) + e of the column
+                float w[NW], top = ref[u];
+#pragma unroll
+                for (int t = 1; t < NW; ++t) { w[t] = sh[(t - 1) * KEEP * 64 + lane]; top = fmaxf(top, w[t]); }
+                w[0] = __builtin_amdgcn_exp2f(ref[u] - top);
+                float sum = den[u] * w[0];
+#pragma unroll
+                for (int t = 1; t < NW; ++t) {
+                    w[t] = __builtin_amdgcn_exp2f(w[t] - top);
+                    sum += sh[((t - 1) * KEEP + 1) * 64 + lane] * w[t];
+                }
+                const int64_t slot = (int64_t)x * COLUMNS + col;
+                float *o = a.piece_sums + slot * D;
+                if (c == 0) *reinterpret_cast<f32x2 *>(a.piece_weights + slot * 2) = f32x2{top, sum};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                    for (int e = 0; e < EP; ++e) {
+                        float t = acc[u][e][r] * w[0];
+#pragma unroll
+                        for (int y = 1; y < NW; ++y) t = fmaf(sh[((y - 1) * KEEP + 2 + 4 * e + r) * 64 + lane], w[y], t);
+                        o[EP * (4 * c + r) + e] = t;
+                    }
+                    asm volatile("" ::: "memory");             // a quarter at a time: all of the others' sums do not fit the registers
+                }
+            }
+        }
+    }
+}
+
+// grid (G, problems): the pieces of a sequence's prefix and what its own rows gave
+template <int STEP, int COLUMNS>
+__global__ void __launch_bounds__(MERGE_T)
+join_kernel(PrefixArgs a)
+{
+    __shared__ f32x4 sum[MERGE_T];
+    const PageDims &d = a.d;
+    const int g = blockIdx.x, p = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int s = seq_of_problem(d, p), skip = a.skipped(s, rows_of(d, a.pv.lengths, s));
+    if (skip == 0) return;                                     // its own rows are all
+    const int i = uniform(prefix_of(a.prefixes, s));
+    const Prefix prefix = prefix_at(d, a.prefixes, i);
+    const Cut<STEP, COLUMNS> cut(a, lane);
+    const int pieces = cut.pieces_of(prefix), blocks = cut.blocks_of(prefix), column = (s - prefix.first) * d.G + g, block = column / COLUMNS;
+    const int64_t first = cut.before(i) + (int64_t)((p - s * cut.heads) * blocks + block) * pieces;
+    if (first + pieces > a.slots) return;                      // prefixes that do not follow each other
+    auto slot = [&](int j) { return (first + j) * COLUMNS + column - block * COLUMNS; };
+    auto weight = [&](int j) { return *reinterpret_cast<const f32x2 *>(a.piece_weights + slot(j) * 2); };
+    const f32x2 own = *reinterpret_cast<const f32x2 *>(a.stats + ((int64_t)p * d.G + g) * 2);
+    float m = own[0];
+    for (int j = lane; j < pieces; j += 64) m = fmaxf(m, weight(j)[0]);
+    m = over_lanes<1>(m, true);
+    float den = 0.f;
+    for (int j = lane; j < pieces; j += 64) {
+        const f32x2 w = weight(j);
+        den += w[1] * __builtin_amdgcn_exp2f(w[0] - m);
+    }
+    den = over_lanes<1>(den, false);
+    const float own_den = own[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(own[0] - m) / own[1];
+    den += own_den;
+    const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
+    f32x4 t{0.f, 0.f, 0.f, 0.f};
+    if (group < groups)
+        for (int j = group; j < pieces; j += groups)
+            t += *reinterpret_cast<const f32x4 *>(a.piece_sums + slot(j) * d.D + 4 * c) * __builtin_amdgcn_exp2f(weight(j)[0] - m);
+    sum[tid] = t;
+    __syncthreads();
+    if (group > 0) return;
+    for (int j = 1; j < groups; ++j) t += sum[j * per + c];
+    out4 *out = reinterpret_cast<out4 *>(a.out + (((int64_t)s * d.n_layers + layer_of_problem(d, p)) * d.Hq + head_of_problem(d, p) * d.G + g) * d.D + 4 * c);
+    const f32x4 mine = *out;
+    if (own_den != 0.f) t += mine * own_den;
+    *out = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
+}
+
+constexpr int prefix_step(bool bf16, int D) { return bf16 && D <= 128 ? 32 : 16; }
+constexpr int prefix_tiles(bool bf16, int D) { return D <= (bf16 ? 128 : 64) ? 2 : 1; }
+int prefix_columns(const PageDims &d) { return prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
+int prefix_workgroups(const PageDims &d) { return d.cus * 2; }
+// pieces at most: one more than its share for every workgroup, and one for every block of columns, of which the last ones of prefixes of two sequences
+// or more may be short
+int prefix_slots(const PageDims &d, int n_prefixes)
+{
+    const int64_t blocks = ((int64_t)d.n_seq * d.G) / prefix_columns(d) + std::min(n_prefixes, d.n_seq / 2);
+    return (int)(prefix_workgroups(d) + (int64_t)d.n_layers * d.Hkv * blocks);
+}
+size_t stats_bytes(const PageDims &d) { return align256((size_t)d.P * d.G * 8); }
+size_t weights_bytes(const PageDims &d, int slots) { return align256((size_t)slots * prefix_columns(d) * 8); }
+size_t sums_bytes(const PageDims &d, int slots) { return align256((size_t)slots * prefix_columns(d) * d.D * 4); }
+
+}  // namespace
+
+size_t decode_prefix_ws_bytes(const PageDims &d, int32_t n_prefixes)
+{
+    const int slots = prefix_slots(d, n_prefixes);
+    return decode_ws_bytes_of(d) + stats_bytes(d) + weights_bytes(d, slots) + sums_bytes(d, slots);
+}
+
+hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView &pv, const int32_t *begin, const int32_t *pages, int32_t n_prefixes,
+                                float *out, void *ws, hipStream_t st)
+{
+    PrefixArgs a;
+    a.prefixes = PrefixView{begin, pages, n_prefixes};
+    a.inv_group = inverse_of((uint32_t)d.G);
+    a.slots = prefix_slots(d, n_prefixes);
+    char *at = static_cast<char *>(ws) + decode_ws_bytes_of(d);
+    a.stats = reinterpret_cast<float *>(at);
+    at += stats_bytes(d);
+    a.piece_weights = reinterpret_cast<float *>(at);
+    a.piece_sums = reinterpret_cast<float *>(at + weights_bytes(d, a.slots));
+    const hipError_t own = launch_decode_of(a, d, q, pv, nullptr, 0, out, ws, st);
+    if (own != hipSuccess) return own;
+    a.workgroups = prefix_workgroups(d);
+    const bool bf = d.dtype == SABLOCK_BF16;
+    using Kern = void (*)(PrefixArgs);
+    Kern fn = nullptr;
+#define SABLOCK_PREFIX(BV, EV)                                                                                            \
+    if (bf == BV && d.D == EV * 16) fn = prefix_kernel<BV, EV, prefix_step(BV, EV * 16), prefix_tiles(BV, EV * 16)>;
+#define SABLOCK_PREFIX_F(EV) SABLOCK_PREFIX(false, EV)
+#define SABLOCK_PREFIX_B(EV) SABLOCK_PREFIX(true, EV) SABLOCK_PREFIX(false, EV)
+    SABLOCK_PREFIX_F(1) SABLOCK_PREFIX_B(2) SABLOCK_PREFIX_F(3) SABLOCK_PREFIX_B(4) SABLOCK_PREFIX_F(5) SABLOCK_PREFIX_B(6) SABLOCK_PREFIX_F(7) SABLOCK_PREFIX_B(8)
+    SABLOCK_PREFIX_F(9) SABLOCK_PREFIX_B(10) SABLOCK_PREFIX_F(11) SABLOCK_PREFIX_B(12) SABLOCK_PREFIX_F(13) SABLOCK_PREFIX_B(14) SABLOCK_PREFIX_F(15) SABLOCK_PREFIX_B(16)
+#undef SABLOCK_PREFIX_B
+#undef SABLOCK_PREFIX_F
+#undef SABLOCK_PREFIX
+    if (!fn) return hipErrorInvalidValue;
+    const int step = prefix_step(bf, d.D);
+    const Kern join = prefix_columns(d) == 2 * TILE ? (step == 32 ? join_kernel<32, 2 * TILE> : join_kernel<16, 2 * TILE>) : join_kernel<16, TILE>;
+    hipLaunchKernelGGL(fn, dim3(std::min(a.workgroups, a.slots)), dim3(NT), 0, st, a);
+    hipLaunchKernelGGL(join, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace sablock
