@@ -80,6 +80,22 @@ __device__ __forceinline__ void load_words(uint32_t *w, const char *p)
 // 256 rows 23.7 -> 20.6 us, 64 of 512 rows 12.3 -> 11.0; heads of 64, 64 problems of 512 rows: 7.3 -> 8.3; shared, 4 x 131 072 rows: 345 -> 349).
 constexpr int step_rows(bool bf16, int D, bool alone) { return bf16 && D <= 128 && !(alone && D > 64) ? 32 : 16; }
 
+// where the logits of head g and rows r .. r + 3 of a problem lie (r a multiple of 4): step by step, of a step of 32 rows the lanes' first four rows of
+// all heads in front of their second four
+__device__ __forceinline__ int64_t logit_place(int step, int G, int64_t r, int g)
+{
+    const int in = (int)r & (step - 1);
+    return (r - in) * G + (step == 32 ? (in >> 2 & 1) * G * 16 + g * 16 + (in >> 3) * 4 : g * 16 + in);
+}
+
+// Workgroups per compute unit that the registers leave room for, by kernel
+constexpr int planned(bool bf16, int D, bool shared) { return D <= 64 || (bf16 && D <= 128 && !shared) ? 3 : bf16 || D <= 160 ? 2 : 1; }
+// logits that a wavefront keeps in LDS: what those workgroups and the joining of their wavefronts leave room for; 16 heads' of a step fit
+constexpr int kept_logits(bool bf16, int D, bool shared)
+{
+    return ((160 * 1024 / std::max(planned(bf16, D, shared), 2) - 1024) / 4 - (NW - 1) * (D / 4 + 2) * 64) / NW & ~15;
+}
+
 struct DecodePagedArgs {
     PageDims d;
     PageView pv;
@@ -250,7 +266,10 @@ decode_paged_kernel(Args a)
     constexpr int KC = D * ELT / 64;                           // 16-byte pieces of a row per lane in the first product
     constexpr int VW = EP * ELT / 4;                           // dwords of a row per lane in the second
     constexpr int KEEP = D / 4 + 2;                            // registers of a lane that wavefronts join
+    constexpr int KEPT = Args::LOGITS ? kept_logits(BF16, D, SHARED) : 1;      // of a wavefront
     __shared__ float sh[(NW - 1) * KEEP * 64];
+    __shared__ __attribute__((aligned(16))) float logits_sh[NW * KEPT];
+    __shared__ f32x2 stats_sh[Args::LOGITS ? 16 : 1];
     const PageDims &d = a.d;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, c = lane >> 4;
@@ -276,6 +295,8 @@ decode_paged_kernel(Args a)
         for (int e = 0; e < EP; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
         const int from = off + (int)((int64_t)count * wave / NW), to = off + (int)((int64_t)count * (wave + 1) / NW);
+        float *kept = logits_sh + (Args::LOGITS ? wave * KEPT : 0);
+        int kept_from = from;                                  // first step of those whose logits LDS has
         // the page and the rows of it that count, of 64 entries at a time, one per lane
         int ids = 0, held = 0, base = -1 << 30;
         const char *kat = nullptr, *vat = nullptr;
@@ -356,6 +377,21 @@ decode_paged_kernel(Args a)
             // first read of its result, but where a branch came in between it was found to leave some out, and old values were read.
 #pragma unroll
             for (int i = 0; i < R; ++i) asm volatile("" : "+v"(z[i]));
+            if constexpr (Args::LOGITS) {
+                // Rows that do not count as well.  They stay in LDS as long as they fit, and a problem that is this workgroup's alone is weighed from there
+                float *to = kept + (st - kept_from) * STEP * d.G;
+                if (m < d.G) {
+#pragma unroll
+                    for (int i = 0; i < R; i += 4) *reinterpret_cast<f32x4 *>(to + i * d.G * 4 + m * 16 + c * 4) = f32x4{z[i], z[i + 1], z[i + 2], z[i + 3]};
+                }
+                const int n_kept = st + 1 - kept_from;
+                if (more.value ? (n_kept + 1) * STEP * d.G > KEPT : count != n) {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // other lanes' stores
+                    f32x4 *out = reinterpret_cast<f32x4 *>(a.logits + ((int64_t)p * a.stride + (int64_t)kept_from * STEP) * d.G);
+                    for (int i = lane; i < n_kept * STEP * d.G / 4; i += 64) out[i] = reinterpret_cast<const f32x4 *>(kept)[i];
+                    kept_from = st + 1;
+                }
+            }
             const bool now_whole = whole;
             const int now_limit = limit;
             if constexpr (more.value) {
@@ -370,13 +406,6 @@ decode_paged_kernel(Args a)
 #pragma unroll
                         for (int w = 0; w < VW; ++w) v[i][w] = 0;             // zero times what lies there may be no number
                     }
-            }
-            if constexpr (Args::LOGITS) {
-                if (m < d.G) {
-                    float *to = a.logits + ((int64_t)p * d.G + m) * a.stride + (int64_t)st * STEP + row;
-#pragma unroll
-                    for (int i = 0; i < R; i += 4) *reinterpret_cast<f32x4 *>(to + i) = f32x4{z[i], z[i + 1], z[i + 2], z[i + 3]};
-                }
             }
             float most = z[0];
 #pragma unroll
@@ -467,6 +496,9 @@ decode_paged_kernel(Args a)
                 if constexpr (Args::STATS) {
                     if (c == 0) *reinterpret_cast<f32x2 *>(a.stats + ((int64_t)p * d.G + m) * 2) = f32x2{top, f};
                 }
+                if constexpr (Args::LOGITS) {
+                    if (c == 0) stats_sh[m] = f32x2{top, f};
+                }
             } else {
                 const int64_t slot = 2 * (int64_t)(blockIdx.x - d.P) + (off == 0);
                 o = a.sums + (slot * d.G + m) * D;
@@ -487,6 +519,17 @@ decode_paged_kernel(Args a)
                     o[EP * (4 * c + i) + e] = t;
                 }
                 asm volatile("" ::: "memory");                 // a quarter at a time: all of the others' sums do not fit the registers
+            }
+        }
+        if constexpr (Args::LOGITS) {
+            if (count == n) {                                  // each wavefront weighs its own steps' rows
+                __syncthreads();
+                const float *early = a.logits + (int64_t)p * a.stride * d.G;
+                for (int r = from * STEP + 4 * lane; r < min(to * STEP, len); r += 256)
+                    a.weigh(s, layer, head, r, len, stats_sh, [&](int g) __attribute__((always_inline)) {
+                        const int64_t at = logit_place(STEP, d.G, r, g), first = (int64_t)kept_from * STEP * d.G;
+                        return *reinterpret_cast<const f32x4 *>(at >= first ? kept + (at - first) : early + at);
+                    });
             }
         }
     };
@@ -560,6 +603,28 @@ decode_paged_merge_kernel(Args a)
     const int first = places.whole ? at : quotient(at, places.run);
     const int pieces = places.whole ? units : quotient(at + n - 1, places.run) - first + 1;
     if (pieces == 1) return;                                   // finished where it was computed
+    if constexpr (Args::LOGITS) {
+        if (g >= d.G) {                                        // weighs rows, all heads
+            __shared__ f32x2 stats_sh[16];
+            for (int h = tid >> 6; h < d.G; h += MERGE_T / 64) {
+                auto weight = [&](int i) { return *reinterpret_cast<const f32x2 *>(a.weights + ((int64_t)(2 * (first + i) + (i == 0)) * d.G + h) * 2); };
+                float m = -FLT_MAX, den = 0.f;
+                for (int i = lane; i < pieces; i += 64) m = fmaxf(m, weight(i)[0]);
+                m = over_lanes<1>(m, true);
+                for (int i = lane; i < pieces; i += 64) den += weight(i)[1] * __builtin_amdgcn_exp2f(weight(i)[0] - m);
+                den = over_lanes<1>(den, false);
+                if (lane == 0) stats_sh[h] = f32x2{m, den == 0.f ? 0.f : 1.f / den};
+            }
+            __syncthreads();
+            const float *logits = a.logits + (int64_t)p * a.stride * d.G;
+            const int len = rows_of(d, a.pv.lengths, seq), step = (gridDim.x - d.G) * MERGE_T * 4;
+            for (int64_t r = ((int64_t)(g - d.G) * MERGE_T + tid) * 4; r < len; r += step)
+                a.weigh(seq, layer_of_problem(d, p), head_of_problem(d, p), (int)r, len, stats_sh, [&](int h) __attribute__((always_inline)) {
+                    return *reinterpret_cast<const f32x4 *>(logits + logit_place(STEP, d.G, r, h));
+                });
+            return;
+        }
+    }
     auto slot = [&](int i) { return (int64_t)(2 * (first + i) + (i == 0)) * d.G + g; };
     const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
     // the first of the numerators are on their way while the weights are formed
@@ -622,7 +687,7 @@ size_t decode_ws_bytes_of(const PageDims &d)
 // The arguments that all such calls share, and the launch
 template <typename Args>
 hipError_t launch_decode_of(Args &a, const PageDims &d, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out, void *ws,
-                         hipStream_t st)
+                            hipStream_t st, int more_merging = 0)
 {
     a.d = d;
     a.pv = pv;
@@ -654,7 +719,7 @@ hipError_t launch_decode_of(Args &a, const PageDims &d, const void *q, const Pag
     if (!fn) return hipErrorInvalidValue;
     const Kern merge = step == 32 ? decode_paged_merge_kernel<32, Args> : decode_paged_merge_kernel<16, Args>;
     hipLaunchKernelGGL(fn, dim3(a.workgroups + d.P), dim3(NT), 0, st, a);
-    if (a.workgroups) hipLaunchKernelGGL(merge, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
+    if (a.workgroups) hipLaunchKernelGGL(merge, dim3(d.G + more_merging, d.P), dim3(MERGE_T), 0, st, a);
     return hipGetLastError();
 }
 

@@ -52,6 +52,7 @@ struct PrefixArgs : DecodePagedArgs {
     }
 };
 
+constexpr int XCDS = 8;
 constexpr int TILE = 16;                       // columns of a matrix product
 
 __device__ __forceinline__ int64_t over_wave(int64_t x)
@@ -140,14 +141,16 @@ prefix_kernel(PrefixArgs a)
         return x.count;
     };
     const Cut<STEP, COLUMNS> cut(a, lane);
-    for (int x = blockIdx.x; x < a.slots; x += a.workgroups) {
+    // The blocks of columns over the same rows follow each other, and workgroups that follow each other are an XCD's: workgroups go round the eight
+    const int mine = blockIdx.x % XCDS * (a.workgroups / XCDS) + blockIdx.x / XCDS;
+    for (int x = mine; x < a.slots; x += a.workgroups) {
         int before;
         const int i = cut.find(x, before);
         if (i < 0) return;
         const Prefix prefix = prefix_at(d, a.prefixes, i);
         const int blocks = cut.blocks_of(prefix), pieces = cut.pieces_of(prefix), n = cut.steps_of_pages(prefix.pages);
-        const int block = uniform(quotient(x - before, pieces)), j = uniform(x - before - block * pieces);
-        const int problem = uniform(quotient(block, blocks)), column0 = (block - problem * blocks) * COLUMNS;
+        const int part = uniform(quotient(x - before, blocks)), column0 = uniform(x - before - part * blocks) * COLUMNS;
+        const int problem = uniform(quotient(part, pieces)), j = part - problem * pieces;
         const int layer = uniform(quotient(problem, d.Hkv)), head = problem - layer * d.Hkv;
         const int columns = prefix.count * d.G, s = prefix.first + first_member(prefix);       // the table's row that is read
         if (s >= prefix.first + prefix.count) continue;
@@ -385,9 +388,9 @@ join_kernel(PrefixArgs a)
     const Prefix prefix = prefix_at(d, a.prefixes, i);
     const Cut<STEP, COLUMNS> cut(a, lane);
     const int pieces = cut.pieces_of(prefix), blocks = cut.blocks_of(prefix), column = (s - prefix.first) * d.G + g, block = column / COLUMNS;
-    const int64_t first = cut.before(i) + (int64_t)((p - s * cut.heads) * blocks + block) * pieces;
-    if (first + pieces > a.slots) return;                      // prefixes that do not follow each other
-    auto slot = [&](int j) { return (first + j) * COLUMNS + column - block * COLUMNS; };
+    const int64_t first = cut.before(i) + (int64_t)(p - s * cut.heads) * pieces * blocks + block;
+    if (first + (int64_t)(pieces - 1) * blocks >= a.slots) return;             // prefixes that do not follow each other
+    auto slot = [&](int j) { return (first + (int64_t)j * blocks) * COLUMNS + column - block * COLUMNS; };
     auto weight = [&](int j) { return *reinterpret_cast<const f32x2 *>(a.piece_weights + slot(j) * 2); };
     const f32x2 own = *reinterpret_cast<const f32x2 *>(a.stats + ((int64_t)p * d.G + g) * 2);
     float m = own[0];
@@ -419,7 +422,7 @@ join_kernel(PrefixArgs a)
 constexpr int prefix_step(bool bf16, int D) { return bf16 && D <= 128 ? 32 : 16; }
 constexpr int prefix_tiles(bool bf16, int D) { return D <= (bf16 ? 128 : 64) ? 2 : 1; }
 int prefix_columns(const PageDims &d) { return prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
-int prefix_workgroups(const PageDims &d) { return d.cus * 2; }
+int prefix_workgroups(const PageDims &d) { return (d.cus * 2 + XCDS - 1) / XCDS * XCDS; }
 // pieces at most: one more than its share for every workgroup, and one for every block of columns, of which the last ones of prefixes of two sequences
 // or more may be short
 int prefix_slots(const PageDims &d, int n_prefixes)
@@ -469,7 +472,7 @@ hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView
     if (!fn) return hipErrorInvalidValue;
     const int step = prefix_step(bf, d.D);
     const Kern join = prefix_columns(d) == 2 * TILE ? (step == 32 ? join_kernel<32, 2 * TILE> : join_kernel<16, 2 * TILE>) : join_kernel<16, TILE>;
-    hipLaunchKernelGGL(fn, dim3(std::min(a.workgroups, a.slots)), dim3(NT), 0, st, a);
+    hipLaunchKernelGGL(fn, dim3(a.workgroups), dim3(NT), 0, st, a);
     hipLaunchKernelGGL(join, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
     return hipGetLastError();
 }
