@@ -116,6 +116,123 @@ struct Cut {
     }
 };
 
+// the first of a prefix's sequences that takes part in it: the others' rows of the table may not have its pages
+__device__ __forceinline__ int first_member(const PrefixArgs &a, const Prefix &x, int lane)
+{
+    for (int at = 0; at < x.count; at += 64) {
+        const bool member = at + lane < x.count && rows_of(a.d, a.pv.lengths, min(x.first + at + lane, a.d.n_seq - 1)) >> a.d.shift >= x.pages;
+        const unsigned long long members = __ballot(member);
+        if (members) return uniform(at + __ffsll(members) - 1);
+    }
+    return x.count;
+}
+
+// What a step of either kernel makes of its logits: a tile's references, denominators and probabilities in parts
+template <int CT, int EP, int R>
+struct Columns {
+    float ref[CT], den[CT];
+    f32x4 acc[CT][EP];
+    __device__ void clear()
+    {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            ref[t] = -FLT_MAX;
+            den[t] = 0.f;
+#pragma unroll
+            for (int e = 0; e < EP; ++e) acc[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    static __device__ __forceinline__ void largest(const float (&z)[CT][R], float (&most)[CT])
+    {
+#pragma unroll
+        for (int u = 0; u < CT; ++u) {
+            most[u] = z[u][0];
+#pragma unroll
+            for (int r = 1; r < R; ++r) most[u] = fmaxf(most[u], z[u][r]);
+        }
+    }
+    // logits z, the largest of a lane given, become probabilities; references move where a logit passes them.  SCALE: they are still to be multiplied by `scale`
+    template <bool SCALE> __device__ __forceinline__ void take(float (&z)[CT][R], float (&most)[CT], float scale)
+    {
+        bool moves = false;
+#pragma unroll
+        for (int u = 0; u < CT; ++u) {
+            if constexpr (SCALE) most[u] *= scale;
+            moves |= most[u] > ref[u];
+        }
+        if (__ballot(moves) != 0ull) {
+#pragma unroll
+            for (int u = 0; u < CT; ++u) {
+                const float top = over_quarters(most[u], true), to_ref = top > ref[u] ? top + AHEAD : ref[u];
+                const float f = __builtin_amdgcn_exp2f(ref[u] - to_ref);
+                ref[u] = to_ref;
+                den[u] *= f;
+#pragma unroll
+                for (int e = 0; e < EP; ++e) acc[u][e] *= f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < CT; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                z[u][r] = __builtin_amdgcn_exp2f(SCALE ? fmaf(z[u][r], scale, -ref[u]) : z[u][r] - ref[u]);
+                den[u] += z[u][r];
+            }
+    }
+    // out^T += V^T P^T, V's rows as dwords of two elements.  SPREAD: products into one accumulator far from each other, as the next one waits for the last
+    // one's result; it takes the registers of all operands at a time
+    template <bool SPREAD> __device__ __forceinline__ void add_bf16(const float (&z)[CT][R], const uint32_t (&v)[R][EP / 2])
+    {
+        typedef uint32_t Operand __attribute__((ext_vector_type(R / 2)));
+        Operand part[CT][3];
+#pragma unroll
+        for (int u = 0; u < CT; ++u)
+#pragma unroll
+            for (int r = 0; r < R / 2; ++r) {
+                float lo = z[u][2 * r], hi = z[u][2 * r + 1];
+#pragma unroll
+                for (int t = 0; t < 3; ++t) {
+                    part[u][t][r] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+                    lo = fmaf(z[u][2 * r], PART_LEAST, lo - __uint_as_float(__float_as_uint(lo) & 0xffff0000u));
+                    hi = fmaf(z[u][2 * r + 1], PART_LEAST, hi - __uint_as_float(__float_as_uint(hi) & 0xffff0000u));
+                }
+            }
+        auto operand = [&](int e) {
+            Operand o;
+#pragma unroll
+            for (int r = 0; r < R / 2; ++r)
+                o[r] = __builtin_amdgcn_perm(v[2 * r + 1][e / 2], v[2 * r][e / 2], e % 2 ? 0x07060302 : 0x05040100);
+            return o;
+        };
+        auto product = [&](const Operand &o, int e, int u, int t) {
+            if constexpr (R == 8)
+                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part[u][t]), acc[u][e], 0, 0, 0);
+            else
+                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, o), __builtin_bit_cast(s16x4, part[u][t]), acc[u][e], 0, 0, 0);
+        };
+        if constexpr (SPREAD) {
+            Operand o[EP];
+#pragma unroll
+            for (int e = 0; e < EP; ++e) o[e] = operand(e);
+#pragma unroll
+            for (int t = 2; t >= 0; --t)
+#pragma unroll
+                for (int e = 0; e < EP; ++e)
+#pragma unroll
+                    for (int u = 0; u < CT; ++u) product(o[e], e, u, t);
+        } else {
+#pragma unroll
+            for (int e = 0; e < EP; ++e) {
+                const Operand o = operand(e);
+#pragma unroll
+                for (int u = 0; u < CT; ++u)
+#pragma unroll
+                    for (int t = 2; t >= 0; --t) product(o, e, u, t);
+            }
+        }
+    }
+};
+
 // CT: tiles of 16 columns of a workgroup, which every wavefront has; the steps of a piece are shared among the wavefronts.  A step is that of
 // decode_paged_kernel, with the operands of K and V used for all tiles.
 template <bool BF16, int EP, int STEP, int CT>
@@ -130,16 +247,6 @@ prefix_kernel(PrefixArgs a)
     const int m = lane & 15, c = lane >> 4;
     const int krow = KT == 2 ? (m >> 2) * 8 + (m & 3) : m, row = R * c;
     const int64_t kstep = d.ks[3] * ELT, vstep = d.vs[3] * ELT;
-    // the first of a prefix's sequences that takes part in it: the others' rows of the table may not have its pages
-    auto first_member = [&](const Prefix &x) {
-        int at = 0;
-        for (; at < x.count; at += 64) {
-            const bool member = at + lane < x.count && rows_of(d, a.pv.lengths, min(x.first + at + lane, d.n_seq - 1)) >> d.shift >= x.pages;
-            const unsigned long long members = __ballot(member);
-            if (members) return uniform(at + __ffsll(members) - 1);
-        }
-        return x.count;
-    };
     const Cut<STEP, COLUMNS> cut(a, lane);
     // The blocks of columns over the same rows follow each other, and workgroups that follow each other are an XCD's: workgroups go round the eight
     const int mine = blockIdx.x % XCDS * (a.workgroups / XCDS) + blockIdx.x / XCDS;
@@ -152,7 +259,7 @@ prefix_kernel(PrefixArgs a)
         const int part = uniform(quotient(x - before, blocks)), column0 = uniform(x - before - part * blocks) * COLUMNS;
         const int problem = uniform(quotient(part, pieces)), j = part - problem * pieces;
         const int layer = uniform(quotient(problem, d.Hkv)), head = problem - layer * d.Hkv;
-        const int columns = prefix.count * d.G, s = prefix.first + first_member(prefix);       // the table's row that is read
+        const int columns = prefix.count * d.G, s = prefix.first + first_member(a, prefix, lane);     // the table's row that is read
         if (s >= prefix.first + prefix.count) continue;
         const int off = j * cut.run, count = min(cut.run, n - off);
 
@@ -164,15 +271,8 @@ prefix_kernel(PrefixArgs a)
 #pragma unroll
             for (int e = 0; e < KC; ++e) q[t][e] = *reinterpret_cast<const u32x4 *>(a.q + qrow * ELT + e * 64 + c * 16);
         }
-        float ref[CT], den[CT];
-        f32x4 acc[CT][EP];
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            ref[t] = -FLT_MAX;
-            den[t] = 0.f;
-#pragma unroll
-            for (int e = 0; e < EP; ++e) acc[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
+        Columns<CT, EP, R> own;
+        own.clear();
         const int from = off + (int)((int64_t)count * wave / NW), to = off + (int)((int64_t)count * (wave + 1) / NW);
         int ids = -1, base = -1 << 30;                         // pages of 64 places at a time, one per lane
         const char *kat = nullptr, *vat = nullptr;
@@ -255,64 +355,11 @@ prefix_kernel(PrefixArgs a)
                         for (int w = 0; w < VW; ++w) v[r][w] = 0;
                     }
             }
-            bool moves = false;
             float most[CT];
-#pragma unroll
-            for (int u = 0; u < CT; ++u) {
-                most[u] = z[u][0];
-#pragma unroll
-                for (int r = 1; r < R; ++r) most[u] = fmaxf(most[u], z[u][r]);
-                moves |= most[u] > ref[u];
-            }
-            if (__ballot(moves) != 0ull) {
-#pragma unroll
-                for (int u = 0; u < CT; ++u) {
-                    const float top = over_quarters(most[u], true), to_ref = top > ref[u] ? top + AHEAD : ref[u];
-                    const float f = __builtin_amdgcn_exp2f(ref[u] - to_ref);
-                    ref[u] = to_ref;
-                    den[u] *= f;
-#pragma unroll
-                    for (int e = 0; e < EP; ++e) acc[u][e] *= f;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < CT; ++u)
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    z[u][r] = __builtin_amdgcn_exp2f(z[u][r] - ref[u]);
-                    den[u] += z[u][r];
-                }
+            own.largest(z, most);
+            own.template take<false>(z, most, 1.f);
             if constexpr (BF16) {
-                typedef uint32_t Operand __attribute__((ext_vector_type(R / 2)));
-                Operand part[CT][3];
-#pragma unroll
-                for (int u = 0; u < CT; ++u)
-#pragma unroll
-                    for (int r = 0; r < R / 2; ++r) {
-                        float lo = z[u][2 * r], hi = z[u][2 * r + 1];
-#pragma unroll
-                        for (int t = 0; t < 3; ++t) {
-                            part[u][t][r] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
-                            lo = fmaf(z[u][2 * r], PART_LEAST, lo - __uint_as_float(__float_as_uint(lo) & 0xffff0000u));
-                            hi = fmaf(z[u][2 * r + 1], PART_LEAST, hi - __uint_as_float(__float_as_uint(hi) & 0xffff0000u));
-                        }
-                    }
-#pragma unroll
-                for (int e = 0; e < EP; ++e) {
-                    Operand o;
-#pragma unroll
-                    for (int r = 0; r < R / 2; ++r)
-                        o[r] = __builtin_amdgcn_perm(v[2 * r + 1][e / 2], v[2 * r][e / 2], e % 2 ? 0x07060302 : 0x05040100);
-#pragma unroll
-                    for (int u = 0; u < CT; ++u)
-#pragma unroll
-                        for (int t = 2; t >= 0; --t) {
-                            if constexpr (R == 8)
-                                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part[u][t]), acc[u][e], 0, 0, 0);
-                            else
-                                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, o), __builtin_bit_cast(s16x4, part[u][t]), acc[u][e], 0, 0, 0);
-                        }
-                }
+                own.template add_bf16<false>(z, v);
             } else {
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -320,7 +367,7 @@ prefix_kernel(PrefixArgs a)
                     for (int e = 0; e < EP; ++e)
 #pragma unroll
                         for (int u = 0; u < CT; ++u)
-                            acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][e]), z[u][r], acc[u][e], 0, 0, 0);
+                            own.acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][e]), z[u][r], own.acc[u][e], 0, 0, 0);
             }
             if constexpr (more.value) load_v();
         };
@@ -331,25 +378,25 @@ prefix_kernel(PrefixArgs a)
         // the wavefronts' shares, lane by lane and tile by tile; the first one joins them
 #pragma unroll
         for (int u = 0; u < CT; ++u) {
-            den[u] = over_quarters(den[u], false);
+            own.den[u] = over_quarters(own.den[u], false);
             __syncthreads();                                   // of the tile before
             if (wave > 0) {
                 float *o = sh + (wave - 1) * KEEP * 64 + lane;
-                o[0] = ref[u];
-                o[64] = den[u];
+                o[0] = own.ref[u];
+                o[64] = own.den[u];
 #pragma unroll
                 for (int e = 0; e < EP; ++e)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) o[(2 + 4 * e + w) * 64] = acc[u][e][w];
+                    for (int w = 0; w < 4; ++w) o[(2 + 4 * e + w) * 64] = own.acc[u][e][w];
             }
             __syncthreads();
             const int col = u * TILE + m;
             if (wave == 0 && column0 + col < columns) {        // elements EP (4 c + w) + e of the column
-                float w[NW], top = ref[u];
+                float w[NW], top = own.ref[u];
 #pragma unroll
                 for (int t = 1; t < NW; ++t) { w[t] = sh[(t - 1) * KEEP * 64 + lane]; top = fmaxf(top, w[t]); }
-                w[0] = __builtin_amdgcn_exp2f(ref[u] - top);
-                float sum = den[u] * w[0];
+                w[0] = __builtin_amdgcn_exp2f(own.ref[u] - top);
+                float sum = own.den[u] * w[0];
 #pragma unroll
                 for (int t = 1; t < NW; ++t) {
                     w[t] = __builtin_amdgcn_exp2f(w[t] - top);
@@ -362,7 +409,7 @@ prefix_kernel(PrefixArgs a)
                 for (int r = 0; r < 4; ++r) {
 #pragma unroll
                     for (int e = 0; e < EP; ++e) {
-                        float t = acc[u][e][r] * w[0];
+                        float t = own.acc[u][e][r] * w[0];
 #pragma unroll
                         for (int y = 1; y < NW; ++y) t = fmaf(sh[((y - 1) * KEEP + 2 + 4 * e + r) * 64 + lane], w[y], t);
                         o[EP * (4 * c + r) + e] = t;
@@ -370,6 +417,192 @@ prefix_kernel(PrefixArgs a)
                     asm volatile("" ::: "memory");             // a quarter at a time: all of the others' sums do not fit the registers
                 }
             }
+        }
+    }
+}
+
+typedef __attribute__((address_space(3))) const void *lds_ptr;
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
+// 16 bytes per lane from base + offset to consecutive places of LDS; waited for by wait_for_pieces
+__device__ __forceinline__ void piece_to_lds(uint32_t offset, const char *base, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory", "m0");
+}
+template <int BEHIND> __device__ __forceinline__ void wait_for_pieces() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(BEHIND) : "memory"); }
+template <int N> __device__ __forceinline__ void row_of_lds(uint32_t (&w)[N], const char *p)  // on a multiple of its size, or of 4 bytes
+{
+    if constexpr (N == 4 || N == 2) {
+        typedef uint32_t T __attribute__((ext_vector_type(N)));
+        const T x = *reinterpret_cast<const T *>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+    }
+}
+// all LDS traffic of this wavefront done, then the workgroup barrier (loads to LDS stay in flight)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The same for prefixes with many columns, bf16 heads of up to 128 elements: a wavefront has columns of its own, 32 of the workgroup's 128, and all
+// wavefronts do every step, from K and V in LDS.  Steps come there four at a time, each wavefront seeing to a quarter of the pieces of 1 KiB; a
+// piece's rows lie in one page.  One barrier per step: everybody's pieces of this step have landed, and the last step's place is free.
+// A row of K in LDS has its 16-byte chunks in the order of place(): the 16 rows of an operand, (m >> 2) * 8 + (m & 3) apart from 4, come from different banks.
+constexpr int WIDE_TILES = 2, WIDE = NW * WIDE_TILES * TILE, STAGES = 4;
+template <int EP> __device__ __forceinline__ int place(int chunk, int row)
+{
+    return chunk ^ (EP == 8 ? (row >> 3) * 4 + (row & 3) : EP == 4 ? (row >> 3) * 2 + (row >> 1 & 1) : row >> 3);
+}
+
+template <int EP>
+__global__ void __launch_bounds__(NT, 2)
+prefix_wide_kernel(PrefixArgs a)
+{
+    constexpr int D = EP * 16, STEP = 32, R = 8, KT = 2, CT = WIDE_TILES, KC = D / 32, VW = EP / 2;
+    constexpr int ROW = D * 2, CHUNKS = D / 8, PIECES = D / 16, OWN = (PIECES + NW - 1) / NW, KV = STEP * ROW;
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * KV];
+    const PageDims &d = a.d;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = lane & 15, c = lane >> 4;
+    const int64_t kstep = d.ks[3] * 2, vstep = d.vs[3] * 2;
+    // this lane's part of its wavefront's pieces
+    uint32_t k_offset[OWN], v_offset[OWN];
+    int piece[OWN];
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+        piece[o] = min(wave * OWN + o, PIECES - 1);
+        const int at = piece[o] * 64 + lane, r = at / CHUNKS, pos = at - r * CHUNKS, in_page = d.shift == 4 ? r & 15 : r;
+        k_offset[o] = (uint32_t)(in_page * (int)kstep + place<EP>(pos, r) * 16);
+        v_offset[o] = (uint32_t)(in_page * (int)vstep + pos * 16);
+    }
+    const int krow = (m >> 2) * 8 + (m & 3);                   // and that row + 4, whose chunks have the same order
+    uint32_t k_at[KC];
+#pragma unroll
+    for (int e = 0; e < KC; ++e) k_at[e] = krow * ROW + place<EP>(4 * e + c, krow) * 16;
+    const uint32_t v_at = R * c * ROW + m * (EP * 2);
+
+    const Cut<STEP, WIDE> cut(a, lane);
+    const int mine = blockIdx.x % XCDS * (a.workgroups / XCDS) + blockIdx.x / XCDS;
+    for (int x = mine; x < a.slots; x += a.workgroups) {
+        int before;
+        const int i = cut.find(x, before);
+        if (i < 0) return;
+        const Prefix prefix = prefix_at(d, a.prefixes, i);
+        const int blocks = cut.blocks_of(prefix), pieces = cut.pieces_of(prefix), n = cut.steps_of_pages(prefix.pages);
+        const int part = uniform(quotient(x - before, blocks)), column0 = uniform(x - before - part * blocks) * WIDE + wave * CT * TILE;
+        const int problem = uniform(quotient(part, pieces)), j = part - problem * pieces;
+        const int layer = uniform(quotient(problem, d.Hkv)), head = problem - layer * d.Hkv;
+        const int columns = prefix.count * d.G, s = prefix.first + first_member(a, prefix, lane);
+        if (s >= prefix.first + prefix.count) continue;
+        const int off = uniform(j * cut.run), count = uniform(min(cut.run, n - off));
+        const bool active = column0 < columns;
+
+        lds_barrier();                                         // the piece before has been read
+        int ids = -1, base = -1 << 30;                         // pages of 64 places at a time, one per lane
+        uint32_t there = 0;                                    // two bits a step, the newest lowest: whether its first and its last 16 rows exist
+        const char *k_head = a.pv.k + (layer * d.ks[0] + head * d.ks[2]) * 2, *v_head = a.pv.v + (layer * d.vs[0] + head * d.vs[2]) * 2;
+        auto issue = [&](int st, int stage) {
+            const int r0 = st * STEP, e0 = r0 >> d.shift;
+            if (e0 - base >= 64) {
+                base = e0;
+                ids = e0 + lane < prefix.pages ? page_at(d, a.pv.table, s, e0 + lane) : -1;
+            }
+            const int in_page = r0 & (d.page - 1), id0 = of_lane(ids, e0 - base);
+            const int id1 = d.shift > 4 ? id0 : e0 - base < 63 ? of_lane(ids, e0 - base + 1) : -1;
+            there = there << 2 | (id0 >= 0 ? 1u : 0u) | (id1 >= 0 ? 2u : 0u);
+            const uint32_t to = uniform((int)lds_address(lds) + stage * 2 * KV);
+#pragma unroll
+            for (int o = 0; o < OWN; ++o) {
+                const int64_t id = max(2 * piece[o] >= PIECES ? id1 : id0, 0);
+                piece_to_lds(k_offset[o], k_head + (id * d.ks[1] + in_page * d.ks[3]) * 2, to + piece[o] * 1024);
+                piece_to_lds(v_offset[o], v_head + (id * d.vs[1] + in_page * d.vs[3]) * 2, to + KV + piece[o] * 1024);
+            }
+        };
+        u32x4 q[CT][KC];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const int col = min(column0 + t * TILE + m, columns - 1), at = sablock::quotient(col, a.inv_group), g = col - at * d.G;
+            const int64_t qrow = (((int64_t)(prefix.first + at) * d.n_layers + layer) * d.Hq + head * d.G + g) * D;
+#pragma unroll
+            for (int e = 0; e < KC; ++e) q[t][e] = *reinterpret_cast<const u32x4 *>(a.q + qrow * 2 + e * 64 + c * 16);
+        }
+        // here, in front of the loads that the compiler does not count: it would wait for these, and all of those, in every step
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int e = 0; e < KC; ++e) asm volatile("" : "+v"(q[t][e]));
+        Columns<CT, EP, R> own;
+        own.clear();
+#pragma unroll
+        for (int t = 0; t < STAGES - 1; ++t) issue(off + min(t, count - 1), t);
+        for (int st = 0, stage = 0; st < count; ++st) {
+            wait_for_pieces<(STAGES - 2) * 2 * OWN>();
+            lds_barrier();
+            issue(off + min(st + STAGES - 1, count - 1), (stage + STAGES - 1) % STAGES);
+            const char *kt = lds + stage * 2 * KV, *vt = kt + KV;
+            stage = (stage + 1) % STAGES;
+            if (!active) continue;
+            float z[CT][R];
+            {
+                u32x4 k[KT][KC];
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int e = 0; e < KC; ++e) k[t][e] = *reinterpret_cast<const u32x4 *>(kt + k_at[e] + t * 4 * ROW);
+                f32x4 r[CT][KT];
+#pragma unroll
+                for (int e = 0; e < KC; ++e)
+#pragma unroll
+                    for (int u = 0; u < CT; ++u)
+#pragma unroll
+                        for (int t = 0; t < KT; ++t)
+                            r[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][e]), __builtin_bit_cast(bf16x8, q[u][e]),
+                                                                             e ? r[u][t] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int u = 0; u < CT; ++u)
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) z[u][4 * t + w] = r[u][t][w];
+            }
+            // all results are read before any branch, see decode_paged_kernel
+            float most[CT];
+            own.largest(z, most);
+#pragma unroll
+            for (int u = 0; u < CT; ++u) asm volatile("" : "+v"(most[u]));
+            uint32_t v[R][VW];
+#pragma unroll
+            for (int r = 0; r < R; ++r) row_of_lds<VW>(v[r], vt + v_at + r * ROW);
+            const uint32_t now = there >> 2 * (STAGES - 1) & 3;
+            if (now != 3 && !(now >> (c >> 1) & 1)) {
+#pragma unroll
+                for (int u = 0; u < CT; ++u) {
+                    most[u] = -INFINITY;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) z[u][r] = -INFINITY;
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) v[r][w] = 0;
+            }
+            own.template take<true>(z, most, a.qscale);
+            own.template add_bf16<true>(z, v);
+        }
+        wait_for_pieces<0>();                                  // those that came again for the last steps: LDS may be another workgroup's soon
+        if (!active) continue;
+#pragma unroll
+        for (int u = 0; u < CT; ++u) {
+            own.den[u] = over_quarters(own.den[u], false);
+            const int col = column0 + u * TILE + m;
+            if (col >= columns) continue;
+            const int64_t slot = (int64_t)x * WIDE + wave * CT * TILE + u * TILE + m;          // elements EP (4 c + w) + e of the column
+            if (c == 0) *reinterpret_cast<f32x2 *>(a.piece_weights + slot * 2) = f32x2{own.ref[u], own.den[u]};
+            float *o = a.piece_sums + slot * D + EP * 4 * c;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+#pragma unroll
+                for (int e = 0; e < EP; ++e) o[EP * w + e] = own.acc[u][e][w];
         }
     }
 }
@@ -421,25 +654,30 @@ join_kernel(PrefixArgs a)
 
 constexpr int prefix_step(bool bf16, int D) { return bf16 && D <= 128 ? 32 : 16; }
 constexpr int prefix_tiles(bool bf16, int D) { return D <= (bf16 ? 128 : 64) ? 2 : 1; }
-int prefix_columns(const PageDims &d) { return prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
+// Prefixes have more than 64 columns on average, and the rows of a step lie within reach of 31 bits
+bool prefix_wide(const PageDims &d, int n_prefixes)
+{
+    const int64_t reach = 31 * 2 * std::max(d.ks[3], d.vs[3]);
+    return d.dtype == SABLOCK_BF16 && d.D <= 128 && (int64_t)d.n_seq * d.G > 64 * (int64_t)n_prefixes && reach + 256 < (int64_t)1 << 31;
+}
+int prefix_columns(const PageDims &d, int n_prefixes) { return prefix_wide(d, n_prefixes) ? WIDE : prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
 int prefix_workgroups(const PageDims &d) { return (d.cus * 2 + XCDS - 1) / XCDS * XCDS; }
 // pieces at most: one more than its share for every workgroup, and one for every block of columns, of which the last ones of prefixes of two sequences
 // or more may be short
 int prefix_slots(const PageDims &d, int n_prefixes)
 {
-    const int64_t blocks = ((int64_t)d.n_seq * d.G) / prefix_columns(d) + std::min(n_prefixes, d.n_seq / 2);
+    const int64_t blocks = ((int64_t)d.n_seq * d.G) / prefix_columns(d, n_prefixes) + std::min(n_prefixes, d.n_seq / 2);
     return (int)(prefix_workgroups(d) + (int64_t)d.n_layers * d.Hkv * blocks);
 }
 size_t stats_bytes(const PageDims &d) { return align256((size_t)d.P * d.G * 8); }
-size_t weights_bytes(const PageDims &d, int slots) { return align256((size_t)slots * prefix_columns(d) * 8); }
-size_t sums_bytes(const PageDims &d, int slots) { return align256((size_t)slots * prefix_columns(d) * d.D * 4); }
+size_t weights_bytes(const PageDims &d, int n_prefixes) { return align256((size_t)prefix_slots(d, n_prefixes) * prefix_columns(d, n_prefixes) * 8); }
+size_t sums_bytes(const PageDims &d, int n_prefixes) { return align256((size_t)prefix_slots(d, n_prefixes) * prefix_columns(d, n_prefixes) * d.D * 4); }
 
 }  // namespace
 
 size_t decode_prefix_ws_bytes(const PageDims &d, int32_t n_prefixes)
 {
-    const int slots = prefix_slots(d, n_prefixes);
-    return decode_ws_bytes_of(d) + stats_bytes(d) + weights_bytes(d, slots) + sums_bytes(d, slots);
+    return decode_ws_bytes_of(d) + stats_bytes(d) + weights_bytes(d, n_prefixes) + sums_bytes(d, n_prefixes);
 }
 
 hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView &pv, const int32_t *begin, const int32_t *pages, int32_t n_prefixes,
@@ -453,7 +691,7 @@ hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView
     a.stats = reinterpret_cast<float *>(at);
     at += stats_bytes(d);
     a.piece_weights = reinterpret_cast<float *>(at);
-    a.piece_sums = reinterpret_cast<float *>(at + weights_bytes(d, a.slots));
+    a.piece_sums = reinterpret_cast<float *>(at + weights_bytes(d, n_prefixes));
     const hipError_t own = launch_decode_of(a, d, q, pv, nullptr, 0, out, ws, st);
     if (own != hipSuccess) return own;
     a.workgroups = prefix_workgroups(d);
@@ -469,9 +707,13 @@ hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView
 #undef SABLOCK_PREFIX_B
 #undef SABLOCK_PREFIX_F
 #undef SABLOCK_PREFIX
-    if (!fn) return hipErrorInvalidValue;
     const int step = prefix_step(bf, d.D);
-    const Kern join = prefix_columns(d) == 2 * TILE ? (step == 32 ? join_kernel<32, 2 * TILE> : join_kernel<16, 2 * TILE>) : join_kernel<16, TILE>;
+    Kern join = prefix_tiles(bf, d.D) == 2 ? (step == 32 ? join_kernel<32, 2 * TILE> : join_kernel<16, 2 * TILE>) : join_kernel<16, TILE>;
+    if (prefix_wide(d, n_prefixes)) {
+        fn = d.D == 128 ? prefix_wide_kernel<8> : d.D == 96 ? prefix_wide_kernel<6> : d.D == 64 ? prefix_wide_kernel<4> : prefix_wide_kernel<2>;
+        join = join_kernel<32, WIDE>;
+    }
+    if (!fn) return hipErrorInvalidValue;
     hipLaunchKernelGGL(fn, dim3(a.workgroups), dim3(NT), 0, st, a);
     hipLaunchKernelGGL(join, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
     return hipGetLastError();
