@@ -179,57 +179,57 @@ struct Columns {
                 den[u] += z[u][r];
             }
     }
-    // out^T += V^T P^T, V's rows as dwords of two elements.  SPREAD: products into one accumulator far from each other, as the next one waits for the last
-    // one's result; it takes the registers of all operands at a time
-    template <bool SPREAD> __device__ __forceinline__ void add_bf16(const float (&z)[CT][R], const uint32_t (&v)[R][EP / 2])
+    // Probabilities as three bf16 numbers each, 24 bits; none but the first is ever zero, as zero times an infinite value would be no number.  A part is
+    // the upper half of what is left, which the next difference (of one element: the other's factor is zero) leaves
+    typedef uint32_t Operand __attribute__((ext_vector_type(R / 2)));
+    static __device__ __forceinline__ void split(const float (&z)[CT][R], Operand (&part)[CT][3])
     {
-        typedef uint32_t Operand __attribute__((ext_vector_type(R / 2)));
-        Operand part[CT][3];
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        typedef short s16x2 __attribute__((ext_vector_type(2)));
+        // (-1, 0) and (0, -1), in registers: as a constant of the instruction the first one was taken for another pair
+        uint32_t of_x = 0x0000bf80u, of_y = 0xbf800000u;
+        asm("" : "+s"(of_x), "+s"(of_y));
+        const bf16x2 first = __builtin_bit_cast(bf16x2, of_x), second = __builtin_bit_cast(bf16x2, of_y);
+        const s16x2 least = {0x0d00, 0x0d00};                  // 2^-101
 #pragma unroll
         for (int u = 0; u < CT; ++u)
 #pragma unroll
             for (int r = 0; r < R / 2; ++r) {
-                float lo = z[u][2 * r], hi = z[u][2 * r + 1];
+                float x = z[u][2 * r], y = z[u][2 * r + 1];
 #pragma unroll
                 for (int t = 0; t < 3; ++t) {
-                    part[u][t][r] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
-                    lo = fmaf(z[u][2 * r], PART_LEAST, lo - __uint_as_float(__float_as_uint(lo) & 0xffff0000u));
-                    hi = fmaf(z[u][2 * r + 1], PART_LEAST, hi - __uint_as_float(__float_as_uint(hi) & 0xffff0000u));
+                    const uint32_t top = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);
+                    part[u][t][r] = t ? __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(s16x2, top), least)) : top;
+                    if (t == 2) break;
+                    x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, top), first, x, false);
+                    y = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, top), second, y, false);
                 }
             }
-        auto operand = [&](int e) {
-            Operand o;
+    }
+    // element e of V's rows (dwords of two elements) as operand
+    static __device__ __forceinline__ Operand operand(const uint32_t (&v)[R][(EP + 1) / 2], int e)
+    {
+        Operand o;
 #pragma unroll
-            for (int r = 0; r < R / 2; ++r)
-                o[r] = __builtin_amdgcn_perm(v[2 * r + 1][e / 2], v[2 * r][e / 2], e % 2 ? 0x07060302 : 0x05040100);
-            return o;
-        };
-        auto product = [&](const Operand &o, int e, int u, int t) {
-            if constexpr (R == 8)
-                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part[u][t]), acc[u][e], 0, 0, 0);
-            else
-                acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, o), __builtin_bit_cast(s16x4, part[u][t]), acc[u][e], 0, 0, 0);
-        };
-        if constexpr (SPREAD) {
-            Operand o[EP];
+        for (int r = 0; r < R / 2; ++r) o[r] = __builtin_amdgcn_perm(v[2 * r + 1][e / 2], v[2 * r][e / 2], e % 2 ? 0x07060302 : 0x05040100);
+        return o;
+    }
+    __device__ __forceinline__ void product(const Operand &o, const Operand &part, int e, int u)
+    {
+        if constexpr (R == 8)
+            acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, part), acc[u][e], 0, 0, 0);
+        else
+            acc[u][e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, o), __builtin_bit_cast(s16x4, part), acc[u][e], 0, 0, 0);
+    }
+    // out^T += V^T P^T, products into one accumulator far from each other: the next one waits for the last one's result
+    __device__ __forceinline__ void multiply(const Operand (&o)[EP], const Operand (&part)[CT][3])
+    {
 #pragma unroll
-            for (int e = 0; e < EP; ++e) o[e] = operand(e);
+        for (int t = 2; t >= 0; --t)
 #pragma unroll
-            for (int t = 2; t >= 0; --t)
+            for (int e = 0; e < EP; ++e)
 #pragma unroll
-                for (int e = 0; e < EP; ++e)
-#pragma unroll
-                    for (int u = 0; u < CT; ++u) product(o[e], e, u, t);
-        } else {
-#pragma unroll
-            for (int e = 0; e < EP; ++e) {
-                const Operand o = operand(e);
-#pragma unroll
-                for (int u = 0; u < CT; ++u)
-#pragma unroll
-                    for (int t = 2; t >= 0; --t) product(o, e, u, t);
-            }
-        }
+                for (int u = 0; u < CT; ++u) product(o[e], part[u][t], e, u);
     }
 };
 
@@ -359,7 +359,16 @@ prefix_kernel(PrefixArgs a)
             own.largest(z, most);
             own.template take<false>(z, most, 1.f);
             if constexpr (BF16) {
-                own.template add_bf16<false>(z, v);
+                typename Columns<CT, EP, R>::Operand p_part[CT][3];
+                own.split(z, p_part);
+#pragma unroll
+                for (int e = 0; e < EP; ++e) {
+                    const auto o = own.operand(v, e);
+#pragma unroll
+                    for (int u = 0; u < CT; ++u)
+#pragma unroll
+                        for (int t = 2; t >= 0; --t) own.product(o, p_part[u][t], e, u);
+                }
             } else {
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -587,7 +596,11 @@ prefix_wide_kernel(PrefixArgs a)
                     for (int w = 0; w < VW; ++w) v[r][w] = 0;
             }
             own.template take<true>(z, most, a.qscale);
-            own.template add_bf16<true>(z, v);
+            typename Columns<CT, EP, R>::Operand p_part[CT][3], o[EP];
+            own.split(z, p_part);
+#pragma unroll
+            for (int e = 0; e < EP; ++e) o[e] = own.operand(v, e);
+            own.multiply(o, p_part);
         }
         wait_for_pieces<0>();                                  // those that came again for the last steps: LDS may be another workgroup's soon
         if (!active) continue;

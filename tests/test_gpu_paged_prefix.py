@@ -224,3 +224,28 @@ def test_twice_the_same_on_any_stream_and_in_a_graph(torch_cuda):  # noqa: F811
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
         _check(c, q, b, m)
+
+
+@pytest.mark.parametrize("dtype,G,count", [("bf16", 8, 4), ("bf16", 8, 40), ("f32", 8, 4)])
+def test_probabilities_are_fp32(torch_cuda, dtype, G, count):  # noqa: F811
+    # As in the test of the attention without prefixes: three rows whose logits are exact products, here the prefix's, whose other rows have no share.  The
+    # shares' sum to 2^-19, each share to 2^-19.7 and 2^-19, and for what the join multiplies and divides, four roundings more, 2^-22
+    torch = torch_cuda
+    D, n = 64, 6 * count
+    c = Sharing(torch, 1, [(count, 1)] * 6, [0] * n, heads=1, group=G, D=D, dtype=dtype)
+    at = c.table[::count, 0].long()
+    first = (torch.rand((6, 3), generator=c.gen, device="cuda") * 2 - 1).to(torch.bfloat16)
+    c.k_pool[0, at, 0] = 0.0
+    c.k_pool[0, at, 0, :, 0] = -1e6
+    c.k_pool[0, at, 0, :3, 0] = first.to(c.dt)
+    c.v_pool[0, at, 0] = 0.0
+    c.v_pool[0, at, 0, :3, 0] = 1.0
+    for r in range(3):
+        c.v_pool[0, at, 0, r, 1 + r] = 1.0
+    q = torch.zeros((n, 1, G, D), dtype=c.dt, device="cuda")
+    q[..., 0] = torch.arange(1, G + 1, device="cuda").to(c.dt)
+    got = c.decode_prefix(q)[:, 0].double().cpu()
+    share = torch.softmax(first.double().cpu()[:, None] * torch.arange(1, G + 1, dtype=torch.float64)[:, None] / 8, dim=-1).repeat_interleave(count, dim=0)
+    assert bool(((got[..., 0] - 1).abs() <= 2.0 ** -19 + 2.0 ** -22).all()), float((got[..., 0] - 1).abs().max())
+    assert bool(((got[..., 1:4] - share).abs() <= (2.0 ** -19.7 + 2.0 ** -19 + 2.0 ** -22) * share).all())
+    assert not got[..., 4:].any()
