@@ -899,6 +899,8 @@ static sablock_status make_prefix_pages(const char *who, const sablock_pages *pa
 {
     sablock_status st = make_decode_pages(who, pages, pd);
     if (st != SABLOCK_OK) return st;
+    if (!decode_prefix_supported(*pd))
+        return fail(SABLOCK_ERR_UNSUPPORTED, "%s: need n_seq * n_layers * n_kv_heads * (max_pages * page_size / 16 + 1) < 2^30", who);
     if (n_prefixes < 1) return fail(SABLOCK_ERR_INVALID_ARG, "%s: n_prefixes must be >= 1", who);
     if (n_prefixes > MAX_PAGED_SEQ) return fail(SABLOCK_ERR_UNSUPPORTED, "%s: n_prefixes %d: at most %d per call", who, n_prefixes, MAX_PAGED_SEQ);
     return SABLOCK_OK;

@@ -110,7 +110,7 @@ struct DecodePagedArgs {
     float *sums;                 // pieces [2 * workgroups][G][D]
     static constexpr bool STATS = false;         // a problem's reference and denominator go out too
     static constexpr bool LOGITS = false;        // and its logits
-    static constexpr bool SKIP = false;          // the first pages of some sequences are another kernel's: a.skipped(s, rows) of them
+    static constexpr bool SKIP = false;          // the first workgroups read the first pages of some sequences: see paged_prefix.hip
 };
 
 // rows of a sequence that are this kernel's
@@ -255,6 +255,23 @@ __device__ __forceinline__ float over_quarters(float x, bool take_max)        //
     return take_max ? fmaxf(x, y) : x + y;
 }
 
+template <typename Args> constexpr int shared_floats(int own)
+{
+    if constexpr (Args::SKIP) return own > Args::FLOATS ? own : Args::FLOATS;
+    else return own;
+}
+template <typename Args> constexpr int shared_alignment()
+{
+    if constexpr (Args::SKIP) return 1024;
+    else return 4;
+}
+// number of a workgroup among those that see to the sequences' own rows
+template <typename Args> __device__ __forceinline__ uint32_t own_block(const Args &a)
+{
+    if constexpr (Args::SKIP) return blockIdx.x - a.prefix_workgroups;
+    else return blockIdx.x;
+}
+
 // EP: elements of a row per lane in the second product, D / 16.  SHARED: some problems may be long; else there is nothing but a workgroup per
 // problem (whose registers let a third one reside, heads of 128).
 template <bool BF16, int EP, int STEP, bool SHARED, typename Args>
@@ -267,9 +284,15 @@ decode_paged_kernel(Args a)
     constexpr int VW = EP * ELT / 4;                           // dwords of a row per lane in the second
     constexpr int KEEP = D / 4 + 2;                            // registers of a lane that wavefronts join
     constexpr int KEPT = Args::LOGITS ? kept_logits(BF16, D, SHARED) : 1;      // of a wavefront
-    __shared__ float sh[(NW - 1) * KEEP * 64];
+    __shared__ __attribute__((aligned(shared_alignment<Args>()))) float sh[shared_floats<Args>((NW - 1) * KEEP * 64)];
     __shared__ __attribute__((aligned(16))) float logits_sh[NW * KEPT];
     __shared__ f32x2 stats_sh[Args::LOGITS ? 16 : 1];
+    if constexpr (Args::SKIP) {
+        if ((int)blockIdx.x < a.prefix_workgroups) {
+            a.prefix_part(sh);
+            return;
+        }
+    }
     const PageDims &d = a.d;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, c = lane >> 4;
@@ -500,7 +523,7 @@ decode_paged_kernel(Args a)
                     if (c == 0) stats_sh[m] = f32x2{top, f};
                 }
             } else {
-                const int64_t slot = 2 * (int64_t)(blockIdx.x - d.P) + (off == 0);
+                const int64_t slot = 2 * (int64_t)(own_block(a) - d.P) + (off == 0);
                 o = a.sums + (slot * d.G + m) * D;
                 if (c == 0) {
                     a.weights[(slot * d.G + m) * 2] = top;
@@ -534,14 +557,14 @@ decode_paged_kernel(Args a)
         }
     };
     if constexpr (!SHARED) {
-        const int s = seq_of_problem(d, blockIdx.x), n = uniform(steps_of<STEP>(a, s));
-        piece(blockIdx.x, s, 0, n, n);
+        const int s = seq_of_problem(d, own_block(a)), n = uniform(steps_of<STEP>(a, s));
+        piece(own_block(a), s, 0, n, n);
         return;
     }
     // one call of the above, whatever the workgroup's part is: its code is long, and comes cold from memory
-    const int me = (int)blockIdx.x - d.P;                      // the first ones see to short problems
+    const int me = (int)own_block(a) - d.P;                     // the first ones see to short problems
     Places<STEP, Args> places(a, lane);
-    int p = blockIdx.x, s = 0, off = 0, count = 0, n = 0;
+    int p = own_block(a), s = 0, off = 0, count = 0, n = 0;
     int x = 0, to = 0, seq_from = 0, seq_to = 0, units = 0;    // seq_from, seq_to: all units of sequence s
     if (me < 0) {
         s = seq_of_problem(d, p);
@@ -684,10 +707,8 @@ size_t decode_ws_bytes_of(const PageDims &d)
     return align256(rows * 8) + align256(rows * d.D * 4);
 }
 
-// The arguments that all such calls share, and the launch
-template <typename Args>
-hipError_t launch_decode_of(Args &a, const PageDims &d, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out, void *ws,
-                            hipStream_t st, int more_merging = 0)
+// The arguments that all such calls share
+inline void fill_args(DecodePagedArgs &a, const PageDims &d, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out, void *ws)
 {
     a.d = d;
     a.pv = pv;
@@ -696,14 +717,22 @@ hipError_t launch_decode_of(Args &a, const PageDims &d, const void *q, const Pag
     a.n_listed = n_listed;
     a.qscale = (float)(1.4426950408889634 / sqrt((double)d.D));
     a.out = out;
+    a.weights = static_cast<float *>(ws);
+    a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups_of(d) * d.G * 8));
+}
+
+// and the launch
+template <typename Args>
+hipError_t launch_decode_of(Args &a, const PageDims &d, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out, void *ws,
+                            hipStream_t st, int more_merging = 0)
+{
+    fill_args(a, d, q, pv, list, n_listed, out, ws);
     const int64_t capacity = (int64_t)(list ? std::min(n_listed, d.max_pages) : d.max_pages) * d.page;
     // no problem can be longer; or tables with room for so many rows that 32 bits do not count all steps, with a workgroup's run to spare
     const bool bf = d.dtype == SABLOCK_BF16, alone = capacity <= rows_alone(d) || d.P * (capacity / 16 + 1) >= 1 << 30;
     const int workgroups = workgroups_of(d), step = step_rows(bf, d.D, alone);
     a.limit = (rows_alone(d) + step - 1) / step;
     a.workgroups = alone ? 0 : workgroups;
-    a.weights = static_cast<float *>(ws);
-    a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(2 * (size_t)workgroups * d.G * 8));
     using Kern = void (*)(Args);
     Kern fn = nullptr;
 #define SABLOCK_PAGED(BV, EV)                                                                                             \

@@ -1,10 +1,10 @@
 // Decode attention of a batch whose sequences have their first pages in common: those are read once for all of them.
 //
-//   decode_paged_kernel (paged_decode.h)   every sequence's own rows, with the reference and denominator of each head.
-//   prefix_kernel    The columns of a prefix are the queries of all its sequences and of the KV head's query heads, side by side without a gap;
-//       its rows are cut into pieces.  A workgroup takes a block of columns over a piece of the rows and leaves references, denominators
-//       and numerators in the workspace.  Pieces are dealt out by every workgroup for itself: the prefixes, which only the device knows, are few.
-//   join_kernel      joins the pieces of a sequence's prefix with its own rows.
+//   decode_paged_kernel (paged_decode.h)   sees to the sequences' own rows, and its first workgroups to the prefixes.  The columns of a prefix are the
+//       queries of all its sequences and of the KV head's query heads, side by side without a gap; its rows are cut into pieces.  A workgroup takes a
+//       block of columns over a piece of the rows and leaves references, denominators and numerators in the workspace.  Pieces are dealt out by
+//       every workgroup for itself: the prefixes, which only the device knows, are few.
+//   join_kernel      joins the pieces of a sequence's prefix and those of its own rows, or what a workgroup had finished of these.
 //
 // A sequence takes part in its prefix if all the prefix's rows are its own; one that ends before reads its rows by itself, so that no row of
 // the prefix has to be masked for one column and not for another.
@@ -38,6 +38,7 @@ struct PrefixArgs : DecodePagedArgs {
     PrefixView prefixes;
     float *stats;                // [P][G][2] of the sequences' own rows: reference (log2 domain), 1 / denominator
     uint32_t inv_group;          // ceil(2^32 / G)
+    int prefix_workgroups;       // that see to the prefixes, a multiple of XCDS
     int slots;                   // pieces that the workspace has room for
     float *piece_weights;        // [slots][columns][2]: reference, denominator
     float *piece_sums;           // [slots][columns][D]
@@ -79,7 +80,7 @@ struct Cut {
         }
         steps = over_wave(steps);
         blocks = over_wave(blocks);
-        const int64_t free = a.workgroups - blocks, shares = free > 0 ? free : a.workgroups;
+        const int64_t free = a.prefix_workgroups - blocks, shares = free > 0 ? free : a.prefix_workgroups;
         run = (int)min(max((int64_t)LEAST_STEPS, (steps + shares - 1) / shares), (int64_t)1 << 27);      // no table has room for more
     }
     __device__ Prefix at(int i) const { return i < a.prefixes.n ? prefix_at(a.d, a.prefixes, i) : Prefix{0, 0, 0}; }
@@ -236,12 +237,10 @@ struct Columns {
 // CT: tiles of 16 columns of a workgroup, which every wavefront has; the steps of a piece are shared among the wavefronts.  A step is that of
 // decode_paged_kernel, with the operands of K and V used for all tiles.
 template <bool BF16, int EP, int STEP, int CT>
-__global__ void __launch_bounds__(NT)
-prefix_kernel(PrefixArgs a)
+__device__ __forceinline__ void narrow_prefixes(const PrefixArgs &a, float *sh)
 {
     constexpr int D = EP * 16, ELT = BF16 ? 2 : 4, R = STEP / 4, KT = STEP / 16, KC = D * ELT / 64, VW = EP * ELT / 4, KEEP = D / 4 + 2;
     constexpr int COLUMNS = CT * TILE;
-    __shared__ float sh[(NW - 1) * KEEP * 64];
     const PageDims &d = a.d;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, c = lane >> 4;
@@ -249,8 +248,8 @@ prefix_kernel(PrefixArgs a)
     const int64_t kstep = d.ks[3] * ELT, vstep = d.vs[3] * ELT;
     const Cut<STEP, COLUMNS> cut(a, lane);
     // The blocks of columns over the same rows follow each other, and workgroups that follow each other are an XCD's: workgroups go round the eight
-    const int mine = blockIdx.x % XCDS * (a.workgroups / XCDS) + blockIdx.x / XCDS;
-    for (int x = mine; x < a.slots; x += a.workgroups) {
+    const int mine = blockIdx.x % XCDS * (a.prefix_workgroups / XCDS) + blockIdx.x / XCDS;
+    for (int x = mine; x < a.slots; x += a.prefix_workgroups) {
         int before;
         const int i = cut.find(x, before);
         if (i < 0) return;
@@ -463,13 +462,13 @@ template <int EP> __device__ __forceinline__ int place(int chunk, int row)
     return chunk ^ (EP == 8 ? (row >> 3) * 4 + (row & 3) : EP == 4 ? (row >> 3) * 2 + (row >> 1 & 1) : row >> 3);
 }
 
+constexpr int wide_bytes(int D) { return STAGES * 2 * 32 * D * 2; }
 template <int EP>
-__global__ void __launch_bounds__(NT, 2)
-prefix_wide_kernel(PrefixArgs a)
+__device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
 {
     constexpr int D = EP * 16, STEP = 32, R = 8, KT = 2, CT = WIDE_TILES, KC = D / 32, VW = EP / 2;
     constexpr int ROW = D * 2, CHUNKS = D / 8, PIECES = D / 16, OWN = (PIECES + NW - 1) / NW, KV = STEP * ROW;
-    __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * KV];
+    static_assert(wide_bytes(D) == STAGES * 2 * KV);
     const PageDims &d = a.d;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, c = lane >> 4;
@@ -491,8 +490,8 @@ prefix_wide_kernel(PrefixArgs a)
     const uint32_t v_at = R * c * ROW + m * (EP * 2);
 
     const Cut<STEP, WIDE> cut(a, lane);
-    const int mine = blockIdx.x % XCDS * (a.workgroups / XCDS) + blockIdx.x / XCDS;
-    for (int x = mine; x < a.slots; x += a.workgroups) {
+    const int mine = blockIdx.x % XCDS * (a.prefix_workgroups / XCDS) + blockIdx.x / XCDS;
+    for (int x = mine; x < a.slots; x += a.prefix_workgroups) {
         int before;
         const int i = cut.find(x, before);
         if (i < 0) return;
@@ -620,7 +619,19 @@ prefix_wide_kernel(PrefixArgs a)
     }
 }
 
-// grid (G, problems): the pieces of a sequence's prefix and what its own rows gave
+constexpr int prefix_tiles(bool bf16, int D) { return D <= (bf16 ? 128 : 64) ? 2 : 1; }
+
+// The arguments by what the first workgroups do
+template <bool BF16, int EP, bool MANY> struct PrefixPart : PrefixArgs {
+    static constexpr int FLOATS = MANY ? wide_bytes(EP * 16) / 4 : 0;          // of LDS
+    __device__ __forceinline__ void prefix_part(float *sh) const
+    {
+        if constexpr (MANY) wide_prefixes<EP>(*this, reinterpret_cast<char *>(sh));
+        else narrow_prefixes<BF16, EP, step_rows(BF16, EP * 16, false), prefix_tiles(BF16, EP * 16)>(*this, sh);
+    }
+};
+
+// grid (G, problems)
 template <int STEP, int COLUMNS>
 __global__ void __launch_bounds__(MERGE_T)
 join_kernel(PrefixArgs a)
@@ -628,45 +639,69 @@ join_kernel(PrefixArgs a)
     __shared__ f32x4 sum[MERGE_T];
     const PageDims &d = a.d;
     const int g = blockIdx.x, p = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
-    const int s = seq_of_problem(d, p), skip = a.skipped(s, rows_of(d, a.pv.lengths, s));
-    if (skip == 0) return;                                     // its own rows are all
-    const int i = uniform(prefix_of(a.prefixes, s));
-    const Prefix prefix = prefix_at(d, a.prefixes, i);
-    const Cut<STEP, COLUMNS> cut(a, lane);
-    const int pieces = cut.pieces_of(prefix), blocks = cut.blocks_of(prefix), column = (s - prefix.first) * d.G + g, block = column / COLUMNS;
-    const int64_t first = cut.before(i) + (int64_t)(p - s * cut.heads) * pieces * blocks + block;
-    if (first + (int64_t)(pieces - 1) * blocks >= a.slots) return;             // prefixes that do not follow each other
-    auto slot = [&](int j) { return (first + (int64_t)j * blocks) * COLUMNS + column - block * COLUMNS; };
-    auto weight = [&](int j) { return *reinterpret_cast<const f32x2 *>(a.piece_weights + slot(j) * 2); };
-    const f32x2 own = *reinterpret_cast<const f32x2 *>(a.stats + ((int64_t)p * d.G + g) * 2);
-    float m = own[0];
-    for (int j = lane; j < pieces; j += 64) m = fmaxf(m, weight(j)[0]);
+    const int s = seq_of_problem(d, p), skip = a.skipped(s, rows_of(d, a.pv.lengths, s)), n = shared_steps_of<STEP>(a, s);
+    if (skip == 0 && n == 0) return;                           // finished
+    // Entries: the prefix's pieces, then those of the own rows, or what they gave
+    int pieces = 0, own_pieces = 1;
+    int64_t first = 0, by = 0, own_first = -1;                 // rows of weights and sums; own_first < 0: finished
+    if (skip) {
+        const int i = uniform(prefix_of(a.prefixes, s));
+        const Prefix prefix = prefix_at(d, a.prefixes, i);
+        const Cut<STEP, COLUMNS> cut(a, lane);
+        const int blocks = cut.blocks_of(prefix), column = (s - prefix.first) * d.G + g, block = column / COLUMNS;
+        pieces = cut.pieces_of(prefix);
+        const int64_t at = cut.before(i) + (int64_t)(p - s * cut.heads) * pieces * blocks + block;
+        if (at + (int64_t)(pieces - 1) * blocks >= a.slots) return;            // prefixes that do not follow each other
+        first = at * COLUMNS + column - block * COLUMNS;
+        by = (int64_t)blocks * COLUMNS;
+    }
+    if (n) {
+        Places<STEP, PrefixArgs> places(a, lane);
+        places.deal();
+        const int units = places.units_of(n), at = places.before(s) * places.heads + (p - s * places.heads) * units;
+        const int from = places.whole ? at : quotient(at, places.run), count = places.whole ? units : quotient(at + n - 1, places.run) - from + 1;
+        if (count > 1) {
+            own_first = from;
+            own_pieces = count;
+        } else if (skip == 0) return;
+    }
+    struct Entry { f32x2 weight; const float *sums; };         // reference, denominator; numerators
+    float *out = a.out + (((int64_t)s * d.n_layers + layer_of_problem(d, p)) * d.Hq + head_of_problem(d, p) * d.G + g) * d.D;
+    auto entry = [&](int j) {
+        if (j < pieces) return Entry{*reinterpret_cast<const f32x2 *>(a.piece_weights + (first + j * by) * 2), a.piece_sums + (first + j * by) * d.D};
+        if (own_first >= 0) {
+            const int64_t slot = (2 * (own_first + j - pieces) + (j == pieces)) * d.G + g;
+            return Entry{*reinterpret_cast<const f32x2 *>(a.weights + slot * 2), a.sums + slot * d.D};
+        }
+        const f32x2 x = *reinterpret_cast<const f32x2 *>(a.stats + ((int64_t)p * d.G + g) * 2);
+        return Entry{f32x2{x[0], x[1] == 0.f ? 0.f : 1.f / x[1]}, out};
+    };
+    const int entries = pieces + own_pieces;
+    float m = -FLT_MAX, den = 0.f;
+    for (int j = lane; j < entries; j += 64) m = fmaxf(m, entry(j).weight[0]);
     m = over_lanes<1>(m, true);
-    float den = 0.f;
-    for (int j = lane; j < pieces; j += 64) {
-        const f32x2 w = weight(j);
+    for (int j = lane; j < entries; j += 64) {
+        const f32x2 w = entry(j).weight;
         den += w[1] * __builtin_amdgcn_exp2f(w[0] - m);
     }
     den = over_lanes<1>(den, false);
-    const float own_den = own[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(own[0] - m) / own[1];
-    den += own_den;
     const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
     f32x4 t{0.f, 0.f, 0.f, 0.f};
     if (group < groups)
-        for (int j = group; j < pieces; j += groups)
-            t += *reinterpret_cast<const f32x4 *>(a.piece_sums + slot(j) * d.D + 4 * c) * __builtin_amdgcn_exp2f(weight(j)[0] - m);
+        for (int j = group; j < entries; j += groups) {
+            const Entry e = entry(j);
+            const f32x4 x = *reinterpret_cast<const out4 *>(e.sums + 4 * c);
+            const bool finished = j >= pieces && own_first < 0;                // what is finished is divided by its denominator
+            const float w = __builtin_amdgcn_exp2f(e.weight[0] - m) * (finished ? e.weight[1] : 1.f);
+            if (!finished || w != 0.f) t += x * w;
+        }
     sum[tid] = t;
     __syncthreads();
     if (group > 0) return;
     for (int j = 1; j < groups; ++j) t += sum[j * per + c];
-    out4 *out = reinterpret_cast<out4 *>(a.out + (((int64_t)s * d.n_layers + layer_of_problem(d, p)) * d.Hq + head_of_problem(d, p) * d.G + g) * d.D + 4 * c);
-    const f32x4 mine = *out;
-    if (own_den != 0.f) t += mine * own_den;
-    *out = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
+    *reinterpret_cast<out4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
 }
 
-constexpr int prefix_step(bool bf16, int D) { return bf16 && D <= 128 ? 32 : 16; }
-constexpr int prefix_tiles(bool bf16, int D) { return D <= (bf16 ? 128 : 64) ? 2 : 1; }
 // Prefixes have more than 64 columns on average, and the rows of a step lie within reach of 31 bits
 bool prefix_wide(const PageDims &d, int n_prefixes)
 {
@@ -674,13 +709,13 @@ bool prefix_wide(const PageDims &d, int n_prefixes)
     return d.dtype == SABLOCK_BF16 && d.D <= 128 && (int64_t)d.n_seq * d.G > 64 * (int64_t)n_prefixes && reach + 256 < (int64_t)1 << 31;
 }
 int prefix_columns(const PageDims &d, int n_prefixes) { return prefix_wide(d, n_prefixes) ? WIDE : prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
-int prefix_workgroups(const PageDims &d) { return (d.cus * 2 + XCDS - 1) / XCDS * XCDS; }
+int prefix_workgroups(const PageDims &d, int n_prefixes) { return (d.cus * (prefix_wide(d, n_prefixes) ? 1 : 2) + XCDS - 1) / XCDS * XCDS; }
 // pieces at most: one more than its share for every workgroup, and one for every block of columns, of which the last ones of prefixes of two sequences
 // or more may be short
 int prefix_slots(const PageDims &d, int n_prefixes)
 {
     const int64_t blocks = ((int64_t)d.n_seq * d.G) / prefix_columns(d, n_prefixes) + std::min(n_prefixes, d.n_seq / 2);
-    return (int)(prefix_workgroups(d) + (int64_t)d.n_layers * d.Hkv * blocks);
+    return (int)(prefix_workgroups(d, n_prefixes) + (int64_t)d.n_layers * d.Hkv * blocks);
 }
 size_t stats_bytes(const PageDims &d) { return align256((size_t)d.P * d.G * 8); }
 size_t weights_bytes(const PageDims &d, int n_prefixes) { return align256((size_t)prefix_slots(d, n_prefixes) * prefix_columns(d, n_prefixes) * 8); }
@@ -693,41 +728,43 @@ size_t decode_prefix_ws_bytes(const PageDims &d, int32_t n_prefixes)
     return decode_ws_bytes_of(d) + stats_bytes(d) + weights_bytes(d, n_prefixes) + sums_bytes(d, n_prefixes);
 }
 
+// 32 bits count all steps, as they do not where a table has room for more
+bool decode_prefix_supported(const PageDims &d) { return decode_paged_supported(d) && d.P * (((int64_t)d.max_pages << d.shift) / 16 + 1) < 1 << 30; }
+
 hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView &pv, const int32_t *begin, const int32_t *pages, int32_t n_prefixes,
                                 float *out, void *ws, hipStream_t st)
 {
     PrefixArgs a;
+    fill_args(a, d, q, pv, nullptr, 0, out, ws);
     a.prefixes = PrefixView{begin, pages, n_prefixes};
     a.inv_group = inverse_of((uint32_t)d.G);
+    a.prefix_workgroups = prefix_workgroups(d, n_prefixes);
     a.slots = prefix_slots(d, n_prefixes);
     char *at = static_cast<char *>(ws) + decode_ws_bytes_of(d);
     a.stats = reinterpret_cast<float *>(at);
     at += stats_bytes(d);
     a.piece_weights = reinterpret_cast<float *>(at);
     a.piece_sums = reinterpret_cast<float *>(at + weights_bytes(d, n_prefixes));
-    const hipError_t own = launch_decode_of(a, d, q, pv, nullptr, 0, out, ws, st);
-    if (own != hipSuccess) return own;
-    a.workgroups = prefix_workgroups(d);
-    const bool bf = d.dtype == SABLOCK_BF16;
-    using Kern = void (*)(PrefixArgs);
-    Kern fn = nullptr;
-#define SABLOCK_PREFIX(BV, EV)                                                                                            \
-    if (bf == BV && d.D == EV * 16) fn = prefix_kernel<BV, EV, prefix_step(BV, EV * 16), prefix_tiles(BV, EV * 16)>;
-#define SABLOCK_PREFIX_F(EV) SABLOCK_PREFIX(false, EV)
-#define SABLOCK_PREFIX_B(EV) SABLOCK_PREFIX(true, EV) SABLOCK_PREFIX(false, EV)
-    SABLOCK_PREFIX_F(1) SABLOCK_PREFIX_B(2) SABLOCK_PREFIX_F(3) SABLOCK_PREFIX_B(4) SABLOCK_PREFIX_F(5) SABLOCK_PREFIX_B(6) SABLOCK_PREFIX_F(7) SABLOCK_PREFIX_B(8)
+    const bool bf = d.dtype == SABLOCK_BF16, wide = prefix_wide(d, n_prefixes);
+    const int step = step_rows(bf, d.D, false);
+    a.workgroups = workgroups_of(d);
+    a.limit = (rows_alone(d) + step - 1) / step;
+    const dim3 grid(a.prefix_workgroups + d.P + a.workgroups);
+    using Join = void (*)(PrefixArgs);
+    const Join join = wide ? join_kernel<32, WIDE> : prefix_tiles(bf, d.D) == 1 ? join_kernel<16, TILE> : step == 32 ? join_kernel<32, 2 * TILE> : join_kernel<16, 2 * TILE>;
+#define SABLOCK_PREFIX(BV, EV, WV)                                                                                                            \
+    if (bf == BV && d.D == EV * 16 && wide == WV)                                                                                             \
+        hipLaunchKernelGGL((decode_paged_kernel<BV, EV, step_rows(BV, EV * 16, false), true, PrefixPart<BV, EV, WV>>), grid, dim3(NT), 0, st, \
+                           PrefixPart<BV, EV, WV>{a});
+#define SABLOCK_PREFIX_F(EV) SABLOCK_PREFIX(false, EV, false)
+#define SABLOCK_PREFIX_B(EV) SABLOCK_PREFIX(true, EV, false) SABLOCK_PREFIX(false, EV, false)
+#define SABLOCK_PREFIX_W(EV) SABLOCK_PREFIX(true, EV, true) SABLOCK_PREFIX_B(EV)
+    SABLOCK_PREFIX_F(1) SABLOCK_PREFIX_W(2) SABLOCK_PREFIX_F(3) SABLOCK_PREFIX_W(4) SABLOCK_PREFIX_F(5) SABLOCK_PREFIX_W(6) SABLOCK_PREFIX_F(7) SABLOCK_PREFIX_W(8)
     SABLOCK_PREFIX_F(9) SABLOCK_PREFIX_B(10) SABLOCK_PREFIX_F(11) SABLOCK_PREFIX_B(12) SABLOCK_PREFIX_F(13) SABLOCK_PREFIX_B(14) SABLOCK_PREFIX_F(15) SABLOCK_PREFIX_B(16)
+#undef SABLOCK_PREFIX_W
 #undef SABLOCK_PREFIX_B
 #undef SABLOCK_PREFIX_F
 #undef SABLOCK_PREFIX
-    const int step = prefix_step(bf, d.D);
-    Kern join = prefix_tiles(bf, d.D) == 2 ? (step == 32 ? join_kernel<32, 2 * TILE> : join_kernel<16, 2 * TILE>) : join_kernel<16, TILE>;
-    if (prefix_wide(d, n_prefixes)) {
-        fn = d.D == 128 ? prefix_wide_kernel<8> : d.D == 96 ? prefix_wide_kernel<6> : d.D == 64 ? prefix_wide_kernel<4> : prefix_wide_kernel<2>;
-        join = join_kernel<32, WIDE>;
-    }
-    if (!fn) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(fn, dim3(a.workgroups), dim3(NT), 0, st, a);
     hipLaunchKernelGGL(join, dim3(d.G, d.P), dim3(MERGE_T), 0, st, a);
     return hipGetLastError();
 }

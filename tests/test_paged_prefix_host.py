@@ -17,7 +17,7 @@ def _call(lib, pages=None, **changed):  # noqa: F811
     return lib.sablock_decode_prefix_paged(ctypes.byref(pages or _pages()), *a.values(), None)
 
 
-@pytest.mark.parametrize("change,status", BAD_PAGES + [(dict(n_q_heads=34), 2), (dict(head_dim=48), 2), (dict(head_dim=24, dtype=0), 2)], ids=lambda c: str(c))
+@pytest.mark.parametrize("change,status", BAD_PAGES + [(dict(n_q_heads=34), 2), (dict(head_dim=48), 2), (dict(head_dim=24, dtype=0), 2), (dict(n_seq=3, max_pages=1 << 26), 2)], ids=lambda c: str(c))
 def test_caches(lib, change, status):  # noqa: F811
     assert _call(lib, _pages(**change)) == status
     n = ctypes.c_size_t(7)
