@@ -22,10 +22,10 @@ __device__ __forceinline__ Prefix prefix_at(const PageDims &d, const PrefixView 
     const int from = min(max(v.begin[i], 0), d.n_seq), to = min(max(v.begin[i + 1], 0), d.n_seq);
     return Prefix{from, max(to - from, 0), to - from > 1 ? min(max(v.pages[i], 0), d.max_pages) : 0};
 }
-// the prefix of sequence s: the last one that begins at it or before, -1 for none
+// the prefix that sequence s may have: the last one that begins at it or before, or the first
 __device__ __forceinline__ int prefix_of(const PrefixView &v, int s)
 {
-    int lo = -1, hi = v.n;
+    int lo = 0, hi = v.n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (v.begin[mid] <= s) lo = mid;
@@ -46,10 +46,8 @@ struct PrefixArgs : DecodePagedArgs {
     // pages in front of the own rows of sequence s
     __device__ __forceinline__ int skipped(int s, int rows) const
     {
-        const int i = prefix_of(prefixes, s);
-        if (i < 0) return 0;
-        const Prefix x = prefix_at(d, prefixes, i);
-        return s < x.first + x.count && rows >> d.shift >= x.pages ? x.pages : 0;
+        const Prefix x = prefix_at(d, prefixes, prefix_of(prefixes, s));
+        return s >= x.first && s < x.first + x.count && rows >> d.shift >= x.pages ? x.pages : 0;
     }
 };
 
@@ -67,13 +65,14 @@ __device__ __forceinline__ int64_t over_wave(int64_t x)
 template <int STEP, int COLUMNS>
 struct Cut {
     const PrefixArgs &a;
-    int lane, run, heads;
-    struct Part { int first, count, pages, blocks, pieces; };  // blocks of columns of one problem; pieces of a block
+    int lane, run, heads, total;                               // total: pieces of all
+    Prefix own;                                                // of the first 64, the lane's
     __device__ Cut(const PrefixArgs &args, int l) : a(args), lane(l), heads(args.d.n_layers * args.d.Hkv)
     {
+        own = load(lane);
         int64_t steps = 0, blocks = 0;
         for (int base = 0; base < a.prefixes.n; base += 64) {
-            const Prefix x = at(base + lane);
+            const Prefix x = at(base);
             const int64_t b = x.pages ? (int64_t)heads * blocks_of(x) : 0;
             steps += b * steps_of_pages(x.pages);
             blocks += b;
@@ -82,18 +81,24 @@ struct Cut {
         blocks = over_wave(blocks);
         const int64_t free = a.prefix_workgroups - blocks, shares = free > 0 ? free : a.prefix_workgroups;
         run = (int)min(max((int64_t)LEAST_STEPS, (steps + shares - 1) / shares), (int64_t)1 << 27);      // no table has room for more
+        total = before(a.prefixes.n);
     }
-    __device__ Prefix at(int i) const { return i < a.prefixes.n ? prefix_at(a.d, a.prefixes, i) : Prefix{0, 0, 0}; }
+    __device__ Prefix load(int i) const { return i < a.prefixes.n ? prefix_at(a.d, a.prefixes, i) : Prefix{0, 0, 0}; }
+    __device__ Prefix at(int base) const { return base == 0 ? own : load(base + lane); }               // a lane's of 64
+    __device__ Prefix get(int i) const                         // the same for all
+    {
+        return i < 64 ? Prefix{of_lane(own.first, i), of_lane(own.count, i), of_lane(own.pages, i)} : prefix_at(a.d, a.prefixes, i);
+    }
+    __device__ int all_of(const Prefix &x) const { return x.pages ? heads * blocks_of(x) * pieces_of(x) : 0; }
     __device__ int blocks_of(const Prefix &x) const { return (x.count * a.d.G + COLUMNS - 1) / COLUMNS; }
     __device__ int steps_of_pages(int pages) const { return ((pages << a.d.shift) + STEP - 1) / STEP; }
     __device__ int pieces_of(const Prefix &x) const { return x.pages ? (steps_of_pages(x.pages) + run - 1) / run : 0; }
-    // the prefix that piece x of all lies in, and the pieces in front of it; -1 behind the last piece
+    // the prefix that piece x of all lies in, and the pieces in front of it
     __device__ int find(int x, int &before) const
     {
         before = 0;
         for (int base = 0; base < a.prefixes.n; base += 64) {
-            const Prefix own = at(base + lane);
-            const int n = own.pages ? heads * blocks_of(own) * pieces_of(own) : 0, upto = sum_upto_lane(n) + before;
+            const int n = all_of(at(base)), upto = sum_upto_lane(n) + before;
             const unsigned long long behind = __ballot(upto > x);
             if (behind) {
                 const int l = uniform(__ffsll(behind) - 1);
@@ -108,12 +113,15 @@ struct Cut {
     __device__ int before(int i) const
     {
         int sum = 0;
-        for (int base = 0; base < i; base += 64) {
-            const Prefix own = at(base + lane);
-            const int n = base + lane < i && own.pages ? heads * blocks_of(own) * pieces_of(own) : 0;
-            sum += of_lane(sum_upto_lane(n), 63);
-        }
+        for (int base = 0; base < i; base += 64) sum += of_lane(sum_upto_lane(base + lane < i ? all_of(at(base)) : 0), 63);
         return sum;
+    }
+    // f(piece) for the workgroup's pieces.  Those that follow each other are an XCD's, which workgroups go round: blocks of columns over the same rows
+    // find each other's rows in its L2
+    template <typename F> __device__ __forceinline__ void each_piece(F &&f) const
+    {
+        const int n = min(total, a.slots), share = (n + XCDS - 1) / XCDS, from = blockIdx.x % XCDS * share, to = min(n, from + share);
+        for (int x = from + (int)blockIdx.x / XCDS; x < to; x += a.prefix_workgroups / XCDS) f(x);
     }
 };
 
@@ -247,20 +255,19 @@ __device__ __forceinline__ void narrow_prefixes(const PrefixArgs &a, float *sh)
     const int krow = KT == 2 ? (m >> 2) * 8 + (m & 3) : m, row = R * c;
     const int64_t kstep = d.ks[3] * ELT, vstep = d.vs[3] * ELT;
     const Cut<STEP, COLUMNS> cut(a, lane);
-    // The blocks of columns over the same rows follow each other, and workgroups that follow each other are an XCD's: workgroups go round the eight
-    const int mine = blockIdx.x % XCDS * (a.prefix_workgroups / XCDS) + blockIdx.x / XCDS;
-    for (int x = mine; x < a.slots; x += a.prefix_workgroups) {
+    cut.each_piece([&](int x) __attribute__((always_inline)) {
         int before;
-        const int i = cut.find(x, before);
-        if (i < 0) return;
-        const Prefix prefix = prefix_at(d, a.prefixes, i);
+        const Prefix prefix = cut.get(cut.find(x, before));
         const int blocks = cut.blocks_of(prefix), pieces = cut.pieces_of(prefix), n = cut.steps_of_pages(prefix.pages);
         const int part = uniform(quotient(x - before, blocks)), column0 = uniform(x - before - part * blocks) * COLUMNS;
         const int problem = uniform(quotient(part, pieces)), j = part - problem * pieces;
         const int layer = uniform(quotient(problem, d.Hkv)), head = problem - layer * d.Hkv;
+        const int off = j * cut.run, count = min(cut.run, n - off), from = off + (int)((int64_t)count * wave / NW), to = off + (int)((int64_t)count * (wave + 1) / NW);
+        // pages of 64 places at a time, one per lane; the first ones of the first sequence, in case that it takes part
+        int base = from * STEP >> d.shift, ids = base + lane < prefix.pages ? page_at(d, a.pv.table, prefix.first, base + lane) : -1;
         const int columns = prefix.count * d.G, s = prefix.first + first_member(a, prefix, lane);     // the table's row that is read
-        if (s >= prefix.first + prefix.count) continue;
-        const int off = j * cut.run, count = min(cut.run, n - off);
+        if (s >= prefix.first + prefix.count) return;
+        if (s > prefix.first) base = -1 << 30;
 
         u32x4 q[CT][KC];
 #pragma unroll
@@ -272,8 +279,6 @@ __device__ __forceinline__ void narrow_prefixes(const PrefixArgs &a, float *sh)
         }
         Columns<CT, EP, R> own;
         own.clear();
-        const int from = off + (int)((int64_t)count * wave / NW), to = off + (int)((int64_t)count * (wave + 1) / NW);
-        int ids = -1, base = -1 << 30;                         // pages of 64 places at a time, one per lane
         const char *kat = nullptr, *vat = nullptr;
         bool whole = false, there = false;                     // all rows of the step exist; this lane's results' rows do
         auto locate = [&](int st) {
@@ -426,7 +431,7 @@ __device__ __forceinline__ void narrow_prefixes(const PrefixArgs &a, float *sh)
                 }
             }
         }
-    }
+    });
 }
 
 typedef __attribute__((address_space(3))) const void *lds_ptr;
@@ -490,18 +495,15 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
     const uint32_t v_at = R * c * ROW + m * (EP * 2);
 
     const Cut<STEP, WIDE> cut(a, lane);
-    const int mine = blockIdx.x % XCDS * (a.prefix_workgroups / XCDS) + blockIdx.x / XCDS;
-    for (int x = mine; x < a.slots; x += a.prefix_workgroups) {
+    cut.each_piece([&](int x) __attribute__((always_inline)) {
         int before;
-        const int i = cut.find(x, before);
-        if (i < 0) return;
-        const Prefix prefix = prefix_at(d, a.prefixes, i);
+        const Prefix prefix = cut.get(cut.find(x, before));
         const int blocks = cut.blocks_of(prefix), pieces = cut.pieces_of(prefix), n = cut.steps_of_pages(prefix.pages);
         const int part = uniform(quotient(x - before, blocks)), column0 = uniform(x - before - part * blocks) * WIDE + wave * CT * TILE;
         const int problem = uniform(quotient(part, pieces)), j = part - problem * pieces;
         const int layer = uniform(quotient(problem, d.Hkv)), head = problem - layer * d.Hkv;
         const int columns = prefix.count * d.G, s = prefix.first + first_member(a, prefix, lane);
-        if (s >= prefix.first + prefix.count) continue;
+        if (s >= prefix.first + prefix.count) return;
         const int off = uniform(j * cut.run), count = uniform(min(cut.run, n - off));
         const bool active = column0 < columns;
 
@@ -602,7 +604,7 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
             own.multiply(o, p_part);
         }
         wait_for_pieces<0>();                                  // those that came again for the last steps: LDS may be another workgroup's soon
-        if (!active) continue;
+        if (!active) return;
 #pragma unroll
         for (int u = 0; u < CT; ++u) {
             own.den[u] = over_quarters(own.den[u], false);
@@ -616,7 +618,7 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
 #pragma unroll
                 for (int e = 0; e < EP; ++e) o[EP * w + e] = own.acc[u][e][w];
         }
-    }
+    });
 }
 
 constexpr int prefix_tiles(bool bf16, int D) { return D <= (bf16 ? 128 : 64) ? 2 : 1; }
@@ -631,6 +633,7 @@ template <bool BF16, int EP, bool MANY> struct PrefixPart : PrefixArgs {
     }
 };
 
+constexpr int JOIN_EARLY = 4;
 // grid (G, problems)
 template <int STEP, int COLUMNS>
 __global__ void __launch_bounds__(MERGE_T)
@@ -646,8 +649,8 @@ join_kernel(PrefixArgs a)
     int64_t first = 0, by = 0, own_first = -1;                 // rows of weights and sums; own_first < 0: finished
     if (skip) {
         const int i = uniform(prefix_of(a.prefixes, s));
-        const Prefix prefix = prefix_at(d, a.prefixes, i);
         const Cut<STEP, COLUMNS> cut(a, lane);
+        const Prefix prefix = cut.get(i);
         const int blocks = cut.blocks_of(prefix), column = (s - prefix.first) * d.G + g, block = column / COLUMNS;
         pieces = cut.pieces_of(prefix);
         const int64_t at = cut.before(i) + (int64_t)(p - s * cut.heads) * pieces * blocks + block;
@@ -676,25 +679,32 @@ join_kernel(PrefixArgs a)
         const f32x2 x = *reinterpret_cast<const f32x2 *>(a.stats + ((int64_t)p * d.G + g) * 2);
         return Entry{f32x2{x[0], x[1] == 0.f ? 0.f : 1.f / x[1]}, out};
     };
-    const int entries = pieces + own_pieces;
-    float m = -FLT_MAX, den = 0.f;
-    for (int j = lane; j < entries; j += 64) m = fmaxf(m, entry(j).weight[0]);
+    const int entries = pieces + own_pieces, per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
+    // the first of the numerators are on their way while the weights are formed
+    f32x4 early[JOIN_EARLY], t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < JOIN_EARLY; ++e) early[e] = *reinterpret_cast<const out4 *>(entry(min(group + e * groups, entries - 1)).sums + 4 * c);
+    const f32x2 mine = entry(min(lane, entries - 1)).weight;
+    float m = mine[0], den = 0.f;
+    for (int j = lane + 64; j < entries; j += 64) m = fmaxf(m, entry(j).weight[0]);
     m = over_lanes<1>(m, true);
     for (int j = lane; j < entries; j += 64) {
-        const f32x2 w = entry(j).weight;
+        const f32x2 w = j == lane ? mine : entry(j).weight;
         den += w[1] * __builtin_amdgcn_exp2f(w[0] - m);
     }
     den = over_lanes<1>(den, false);
-    const int per = d.D / 4, groups = MERGE_T / per, group = tid / per, c = tid - group * per;
-    f32x4 t{0.f, 0.f, 0.f, 0.f};
-    if (group < groups)
-        for (int j = group; j < entries; j += groups) {
-            const Entry e = entry(j);
-            const f32x4 x = *reinterpret_cast<const out4 *>(e.sums + 4 * c);
-            const bool finished = j >= pieces && own_first < 0;                // what is finished is divided by its denominator
-            const float w = __builtin_amdgcn_exp2f(e.weight[0] - m) * (finished ? e.weight[1] : 1.f);
-            if (!finished || w != 0.f) t += x * w;
-        }
+    auto add = [&](int j, const f32x4 &x) {
+        const f32x2 e = entry(j).weight;
+        const bool finished = j >= pieces && own_first < 0;    // what is finished is divided by its denominator
+        const float w = __builtin_amdgcn_exp2f(e[0] - m) * (finished ? e[1] : 1.f);
+        if (!finished || w != 0.f) t += x * w;
+    };
+    if (group < groups) {
+#pragma unroll
+        for (int e = 0; e < JOIN_EARLY; ++e)
+            if (group + e * groups < entries) add(group + e * groups, early[e]);
+        for (int j = group + JOIN_EARLY * groups; j < entries; j += groups) add(j, *reinterpret_cast<const out4 *>(entry(j).sums + 4 * c));
+    }
     sum[tid] = t;
     __syncthreads();
     if (group > 0) return;
