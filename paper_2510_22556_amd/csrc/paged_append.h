@@ -34,16 +34,15 @@ struct NormedAppendArgs : AppendArgs {
     float eps, per_element;                                    // 1 / D
 };
 
-// sum over the lanes of a row, a power of two of them
-__device__ __forceinline__ float over_row(float x, int lanes)
+// sums over the lanes of a row, a power of two of them, for B rows at a time
+template <int B> __device__ __forceinline__ void over_row(float (&x)[B], int lanes)
 {
-    if (lanes > 1) x += xor_lane<1>(x);
-    if (lanes > 2) x += xor_lane<2>(x);
-    if (lanes > 4) x += xor_lane<4>(x);
-    if (lanes > 8) x += xor_lane<8>(x);
-    if (lanes > 16) x += xor_lane<16>(x);
-    if (lanes > 32) x += xor_lane<32>(x);
-    return x;
+#define SABLOCK_OVER(M)                                        \
+    if (lanes > M) {                                           \
+        _Pragma("unroll") for (int i = 0; i < B; ++i) x[i] += xor_lane<M>(x[i]); \
+    }
+    SABLOCK_OVER(1) SABLOCK_OVER(2) SABLOCK_OVER(4) SABLOCK_OVER(8) SABLOCK_OVER(16) SABLOCK_OVER(32)
+#undef SABLOCK_OVER
 }
 
 // grid (touched pages, sequences x layers, parts of the head rows).  The angle of a (token, pair) is the same for all heads: formed
@@ -95,7 +94,7 @@ append_paged_kernel(Args a)
         const int64_t *st = is_k ? a.t.ks : is_v ? a.t.vs : a.t.qs;
         return Source{(is_k ? a.k : is_v ? a.v : a.q) + (s * st[0] + layer * st[1] + head * st[2]) * E::BYTES + min(c, a.chunks - 1) * 16, st[3] * E::BYTES};
     };
-    // weights of this chunk's elements and, SPLIT, of those that its pairs have in the other chunk; V's lanes load q's or K's, and do not use them
+    // weights of this chunk's elements and, SPLIT, of those that its pairs have in the other chunk, with the sign that they come with; V's lanes load q's or K's, and do not use them
     struct Weights { float own[NORM ? E::N : 1], other[NORM && SPLIT ? E::N : 1]; };
     auto load_weights = [&](int base, Weights &w) {
         if constexpr (NORM) {
@@ -111,7 +110,7 @@ append_paged_kernel(Args a)
                 if constexpr (SPLIT) {
                     const f32x4 z = *reinterpret_cast<const f32x4 *>(at + partner_chunk * E::N + e);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w.other[e + j] = z[j];
+                    for (int j = 0; j < 4; ++j) w.other[e + j] = upper ? z[j] : -z[j];
                 }
             }
         }
@@ -159,6 +158,21 @@ append_paged_kernel(Args a)
                 step = d.D * E::BYTES;
                 dst = a.q_out + ((((int64_t)s * d.n_layers + layer) * d.Hq + head) * a.t.n_new + t0 - first) * step + c * 16;
             }
+            float over[NORM ? B : 1];                          // 1 / root mean square of the rows, for all of them at a time: each is a chain of lane exchanges
+            if constexpr (NORM) {
+                if (__ballot(!is_v)) {
+#pragma unroll
+                    for (int i = 0; i < B; ++i) {
+                        over[i] = 0.f;
+#pragma unroll
+                        for (int e = 0; e < E::N; ++e) over[i] = fmaf(E::get(x[i], e), E::get(x[i], e), over[i]);
+                        over[i] = c < a.chunks ? over[i] : 0.f;
+                    }
+                    over_row<B>(over, a.lanes);
+#pragma unroll
+                    for (int i = 0; i < B; ++i) over[i] = __builtin_amdgcn_rsqf(fmaf(over[i], a.per_element, a.eps));
+                }
+            }
             auto turn_row = [&](int i) {
                 u32x4 w = x[i], o{0, 0, 0, 0};
                 if constexpr (SPLIT) {
@@ -167,23 +181,17 @@ append_paged_kernel(Args a)
                 }
                 float y[E::N];
                 if constexpr (NORM) {
-                    float sum = 0.f;                           // of squares, of the row: it lies in consecutive lanes
-#pragma unroll
-                    for (int e = 0; e < E::N; ++e) sum = fmaf(E::get(w, e), E::get(w, e), sum);
-                    sum = over_row(c < a.chunks ? sum : 0.f, a.lanes);
-                    const float over = rsqrtf(fmaf(sum, a.per_element, a.eps));
                     if (is_v) return w;
 #pragma unroll
-                    for (int e = 0; e < E::N; ++e) y[e] = E::get(w, e) * over * weights.own[e];
+                    for (int e = 0; e < E::N; ++e) y[e] = E::get(w, e) * weights.own[e];
                     if (turned) {
                         const float4 *angles = reinterpret_cast<const float4 *>(turn + min(group + (bt * B + i) * a.groups, n - 1) * half + angle);
                         if constexpr (SPLIT) {
-                            const float signed_over = upper ? over : -over;
 #pragma unroll
                             for (int e = 0; e < E::N; e += 2) {
                                 const float4 t = angles[e / 2];
-                                y[e] = y[e] * t.x + E::get(o, e) * signed_over * weights.other[e] * t.y;
-                                y[e + 1] = y[e + 1] * t.z + E::get(o, e + 1) * signed_over * weights.other[e + 1] * t.w;
+                                y[e] = y[e] * t.x + E::get(o, e) * weights.other[e] * t.y;
+                                y[e + 1] = y[e + 1] * t.z + E::get(o, e + 1) * weights.other[e + 1] * t.w;
                             }
                         } else {
 #pragma unroll
@@ -195,6 +203,8 @@ append_paged_kernel(Args a)
                             }
                         }
                     }
+#pragma unroll
+                    for (int e = 0; e < E::N; ++e) y[e] *= over[i];
                     return E::pack(y);
                 }
                 if (!turned || is_v) return w;

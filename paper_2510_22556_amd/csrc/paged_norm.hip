@@ -6,6 +6,8 @@
 // nothing.  All in fp32, one rounding to the cache's type.
 #include "paged_append.h"
 
+#include <cfloat>
+
 namespace sablock {
 
 hipError_t launch_append_normed_paged(const PageDims &pd, const TokenDims &td, const NormDims &nd, const void *q, const void *k, const void *v,
@@ -19,7 +21,7 @@ hipError_t launch_append_normed_paged(const PageDims &pd, const TokenDims &td, c
     a.q_layer = nd.per_head ? (int64_t)pd.Hq * pd.D : pd.D;
     a.k_layer = nd.per_head ? (int64_t)pd.Hkv * pd.D : pd.D;
     a.head = nd.per_head ? pd.D : 0;
-    a.eps = nd.eps;
+    a.eps = std::max(nd.eps, FLT_MIN);                         // what the reciprocal root takes
     a.per_element = 1.f / (float)pd.D;
     return launch_append(a, grid, one, st);
 }
