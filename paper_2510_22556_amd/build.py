@@ -15,7 +15,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["api.hip", "score_generic.hip", "score_mfma.hip", "refine.hip", "search_select.hip", "compact.hip", "segment.hip", "decode.hip", "window_attn.hip",
            "paged.hip", "paged_decode.hip", "paged_select.hip", "paged_norm.hip", "paged_evict.hip", "paged_weigh.hip", "paged_prefix.hip"]
-HEADERS = ["paged_rows.h", "paged_append.h", "paged_decode.h"]    # of the paged cache's kernels
+HEADERS = ["paged_rows.h", "paged_append.h", "paged_decode.h", "paged_pick.h"]    # of the paged cache's kernels
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function",
          # keep packed fp32 instructions out of the generated code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,10 +1,12 @@
 // Eviction from the paged cache: of every problem the rows that have gathered the most weight, with the first and the last ones, into the pages of
 // another table, in their order.
 //
-//   row_keys_kernel    the weights of a problem's rows, out of its pages, as whole numbers of the same order, side by side.
-//   pick_pages_kernel  (paged_select.hip) takes rows here: the first, the last, and the largest of the others, ascending.
+//   pick_rows_kernel   the choice, by a workgroup per problem: a key per row in registers, out of the problem's pages.  Tables with room for up to 16 384 rows.
+//   row_keys_kernel, pick_pages_kernel (paged_select.hip)   the same for larger tables: the weights of a problem's rows as whole numbers of the same order, side
+//       by side, and the choice among those.
 //   evict_kernel       a workgroup fills one page of one problem: K, V and weights of its rows, and the page's bounds.  The rows' places are found
 //       once, by a thread each, and wait in LDS: list, table and row are loads that depend on each other.
+#include "paged_pick.h"
 #include "paged_rows.h"
 
 namespace sablock {
@@ -12,6 +14,8 @@ namespace {
 
 constexpr int KEY_ROWS = 4;                    // of a thread, in one page
 constexpr int KEY_WGS = 8;                     // workgroups of the keys per compute unit, at most
+
+__device__ __forceinline__ uint32_t row_key(float w) { return w == w ? ordered_key(w) : NOT_A_NUMBER; }
 
 // grid (parts, problems)
 __global__ void __launch_bounds__(NT)
@@ -26,7 +30,7 @@ row_keys_kernel(PageDims d, PageView pv, const float *weights, uint32_t *keys, i
         if (id >= 0) w = *reinterpret_cast<const f32x4 *>(weights + weight_at(d, layer, id, head) + (r & (d.page - 1)));
         u32x4 key;
 #pragma unroll
-        for (int i = 0; i < KEY_ROWS; ++i) key[i] = w[i] == w[i] ? ordered_key(w[i]) : NOT_A_NUMBER;
+        for (int i = 0; i < KEY_ROWS; ++i) key[i] = row_key(w[i]);
         *reinterpret_cast<u32x4 *>(keys + (int64_t)p * stride + r) = key;
     }
 }
@@ -77,6 +81,31 @@ evict_kernel(PageDims d, PageView pv, EvictDims ed, int chunks)
     store_joined<BF16>(b, sh, groups, chunks, group, c, active, d.D * E::BYTES, false, [&](int place) { return at + place * 16; });
 }
 
+// grid P
+template <int RUN>
+__global__ void __launch_bounds__(PICK_NT)
+pick_rows_kernel(PageDims d, PageView pv, EvictDims ed)
+{
+    __shared__ PickShared sh;
+    const int p = blockIdx.x, s = seq_of_problem(d, p), layer = layer_of_problem(d, p), head = head_of_problem(d, p), tid = threadIdx.x;
+    const int capacity = d.max_pages << d.shift;
+    uint32_t own[RUN];
+#pragma unroll
+    for (int j = 0; j < RUN; j += KEY_ROWS) {                  // before the length is known: whatever lies behind it is not looked at
+        const int r = min(tid * RUN + j, capacity - KEY_ROWS), id = page_at(d, pv.table, s, r >> d.shift);
+        const f32x4 w = *reinterpret_cast<const f32x4 *>(ed.weights + weight_at(d, layer, max(id, 0), head) + (r & (d.page - 1)));
+#pragma unroll
+        for (int i = 0; i < KEY_ROWS; ++i) own[j + i] = id < 0 ? ordered_key(-INFINITY) : row_key(w[i]);
+    }
+    const int n = rows_of(d, pv.lengths, s);
+    int32_t *list = ed.rows_out + (int64_t)p * ed.n_keep;
+    if (n <= ed.n_keep) {
+        for (int i = tid; i < ed.n_keep; i += PICK_NT) list[i] = i < n ? i : -1;
+        return;
+    }
+    pick<RUN>(sh, own, nullptr, n, ed.n_keep, ed.n_first, ed.n_last, [&](int at, int i) __attribute__((always_inline)) { list[at] = i; });
+}
+
 int64_t row_stride(const PageDims &d) { return (int64_t)d.max_pages << d.shift; }
 
 }  // namespace
@@ -85,21 +114,24 @@ size_t evict_ws_bytes(const PageDims &d) { return align256((size_t)d.P * row_str
 
 hipError_t launch_evict(const PageDims &d, const PageView &pv, const EvictDims &ed, void *ws, hipStream_t st)
 {
-    uint32_t *keys = static_cast<uint32_t *>(ws);
-    const int64_t rows = row_stride(d), most = (rows + NT * KEY_ROWS - 1) / (NT * KEY_ROWS);
-    if (rows > ed.n_keep) {                                    // otherwise every row stays
-        const int64_t parts = std::min<int64_t>(most, (KEY_WGS * d.cus + d.P - 1) / d.P);
-        hipLaunchKernelGGL(row_keys_kernel, dim3((unsigned)parts, d.P), dim3(NT), 0, st, d, pv, ed.weights, keys, rows);
+    const int64_t rows = row_stride(d), pages = (std::min<int64_t>(rows, ed.n_keep) + d.page - 1) >> d.shift, run = (rows + PICK_NT - 1) / PICK_NT;
+    const int chunks = d.D * elt_bytes(d) / 16;
+    if (run <= 16) {                                           // keys per thread
+        hipLaunchKernelGGL(run <= 4 ? pick_rows_kernel<4> : run <= 8 ? pick_rows_kernel<8> : pick_rows_kernel<16>, dim3(d.P), dim3(PICK_NT), 0, st, d, pv, ed);
+    } else {
+        uint32_t *keys = static_cast<uint32_t *>(ws);
+        if (rows > ed.n_keep) {                                // otherwise every row stays
+            const int64_t most = (rows + NT * KEY_ROWS - 1) / (NT * KEY_ROWS), parts = std::min<int64_t>(most, (KEY_WGS * d.cus + d.P - 1) / d.P);
+            hipLaunchKernelGGL(row_keys_kernel, dim3((unsigned)parts, d.P), dim3(NT), 0, st, d, pv, ed.weights, keys, rows);
+        }
+        PageDims as_rows = d;                                  // pages of one row
+        as_rows.page = 1;
+        as_rows.shift = 0;
+        as_rows.max_pages = (int32_t)rows;
+        const hipError_t picked = launch_pick(as_rows, pv, ed.n_keep, ed.n_first, ed.n_last, keys, (int32_t)rows, ed.rows_out, st);
+        if (picked != hipSuccess) return picked;
     }
-    PageDims as_rows = d;                                      // pages of one row
-    as_rows.page = 1;
-    as_rows.shift = 0;
-    as_rows.max_pages = (int32_t)rows;
-    const hipError_t picked = launch_pick(as_rows, pv, ed.n_keep, ed.n_first, ed.n_last, keys, (int32_t)rows, ed.rows_out, st);
-    if (picked != hipSuccess) return picked;
-    const int64_t pages = (std::min<int64_t>(rows, ed.n_keep) + d.page - 1) >> d.shift;
-    hipLaunchKernelGGL(d.dtype == SABLOCK_BF16 ? evict_kernel<true> : evict_kernel<false>, dim3((unsigned)pages, d.P), dim3(NT), 0, st, d, pv, ed,
-                       d.D * elt_bytes(d) / 16);
+    hipLaunchKernelGGL(d.dtype == SABLOCK_BF16 ? evict_kernel<true> : evict_kernel<false>, dim3((unsigned)pages, d.P), dim3(NT), 0, st, d, pv, ed, chunks);
     return hipGetLastError();
 }
 
