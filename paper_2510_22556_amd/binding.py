@@ -692,13 +692,14 @@ def sablock_evict_paged(pages: CPages, page_table, lengths, weights, k_pool, v_p
 
 
 class PagedCache:
-    """Pools, page table and lengths of a paged cache, page bounds where asked for, and the workspaces of the calls that read it.
+    """Pools, page table and lengths of a paged cache, page bounds and the rows' gathered weights where asked for, and the workspaces of the calls that read
+    it (``n_prefixes``: of attention with so many common prefixes at most).
 
     Which pages a sequence has is the caller's to say: ``page_table`` starts as -1 (no page).  The workspaces serve one call at a time:
     calls that may overlap, on two streams or in two captured graphs, bring their own."""
 
     def __init__(self, n_seq: int, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, max_pages: int,
-                 dtype, device, bounds: bool = True):
+                 dtype, device, bounds: bool = True, weights: bool = False, n_prefixes: int = 0):
         import torch
 
         self.k_pool, self.v_pool = (torch.zeros((n_layers, n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device) for _ in range(2))
@@ -707,7 +708,14 @@ class PagedCache:
         self.lengths = torch.zeros((n_seq,), dtype=torch.int32, device=device)
         self.pages = make_pages(self.k_pool, self.v_pool, self.page_table, n_q_heads)
         self.ws = torch.empty((sablock_decode_paged_workspace_bytes(self.pages),), dtype=torch.uint8, device=device)
-        self.select_ws = torch.empty((sablock_select_pages_workspace_bytes(self.pages),), dtype=torch.uint8, device=device) if bounds else None
+        def workspace(size):
+            return torch.empty((size(self.pages),), dtype=torch.uint8, device=device)
+
+        self.select_ws = workspace(sablock_select_pages_workspace_bytes) if bounds else None
+        self.weights = torch.zeros((n_layers, n_pages, n_kv_heads, page_size), dtype=torch.float32, device=device) if weights else None
+        self.weighed_ws = workspace(sablock_decode_weighed_paged_workspace_bytes) if weights else None
+        self.evict_ws = workspace(sablock_evict_paged_workspace_bytes) if weights else None
+        self.prefix_ws = workspace(lambda pages: sablock_decode_prefix_paged_workspace_bytes(pages, n_prefixes)) if n_prefixes else None
 
 
 class Buffers:
