@@ -456,8 +456,8 @@ typedef struct {
 /* sablock_append_paged with a norm of every head of q and of k in front of the rotation, for models that have one: the same arguments,
  * rows, positions, counts and bounds; V is copied as it is.  The norm covers the whole head whatever R is.
  *   q_weight, k_weight  fp32, dense, 16-byte aligned, laid out as norms->per_head says; q_weight may be NULL where q is
- * Squares, their sum, the norm and the rotation in fp32, one rounding to the dtype.  A head whose squares' sum passes fp32 becomes zeros; one
- * with an element that is no number, or infinite, is no number there or throughout. */
+ * Squares, their sum, x_d w_d, the rotation and the norm's factor, which comes last, in fp32, one rounding to the dtype.  An eps below FLT_MIN
+ * counts as FLT_MIN.  A head whose squares' sum passes fp32 becomes zeros; one with an element that is no number, or infinite, is no number there or throughout. */
 SABLOCK_API sablock_status sablock_append_normed_paged(const sablock_pages *pages, const sablock_new_tokens *tokens,
                                     const sablock_head_norms *norms, const void *q /* nullable */, const void *k, const void *v,
                                     const float *q_weight, const float *k_weight, const int32_t *counts /* nullable */,
@@ -502,7 +502,8 @@ SABLOCK_API sablock_status sablock_select_pages(const sablock_pages *pages, cons
  *   out[h] = softmax_r(<q[h], K[r]> / sqrt(D)) . V[r],   weights[r] <- decay * weights[r] + sum over the G query heads of softmax_r
  *   weights     [n_layers][n_pages][n_kv_heads][page_size] fp32, dense, 16-byte aligned, beside the pools: row r % page_size of its page.  What
  *               sablock_evict_paged takes.  Rows behind a sequence's last stay as they are.
- *   n_new       the last rows of every sequence, which have gathered nothing: their weights are begun, whatever lies there
+ *   n_new       the last rows of every sequence, which have gathered nothing: their weights are begun, whatever lies there.  As in the append, rows
+ *               that the table has no room for are among them
  *   counts      nullable (every sequence has n_new), or [n_seq] int32, taken as 0 .. n_new: both as in the append in front of this step
  *   decay       finite, >= 0: 1 keeps what was gathered, 0 forgets it
  *   ws          at least sablock_decode_weighed_paged_workspace_bytes(pages) bytes, 16-byte aligned: the logits of all rows that the table has

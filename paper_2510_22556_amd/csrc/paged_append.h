@@ -169,8 +169,21 @@ append_paged_kernel(Args a)
                         over[i] = c < a.chunks ? over[i] : 0.f;
                     }
                     over_row<B>(over, a.lanes);
+                    bool beyond = false;
 #pragma unroll
-                    for (int i = 0; i < B; ++i) over[i] = __builtin_amdgcn_rsqf(fmaf(over[i], a.per_element, a.eps));
+                    for (int i = 0; i < B; ++i) {
+                        over[i] = __builtin_amdgcn_rsqf(fmaf(over[i], a.per_element, a.eps));
+                        beyond |= over[i] == 0.f;
+                    }
+                    if (__ballot(beyond && !is_v)) {           // squares that pass fp32: zeros now, as a product with a weight may be infinite
+#pragma unroll
+                        for (int i = 0; i < B; ++i) {
+                            float y[E::N];
+#pragma unroll
+                            for (int e = 0; e < E::N; ++e) y[e] = E::get(x[i], e) * 0.f;       // what is infinite becomes no number
+                            if (over[i] == 0.f && !is_v) x[i] = E::pack(y);
+                        }
+                    }
                 }
             }
             auto turn_row = [&](int i) {

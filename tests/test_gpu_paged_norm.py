@@ -127,6 +127,39 @@ def test_heads_of_zeros_and_of_what_is_no_number(torch_cuda, dtype, n_new):  # n
     assert bool(torch.isnan(call()[0, 0, 2, at]).any())
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_new", [1, 37])
+def test_heads_as_large_as_the_type(torch_cuda, dtype, n_new, interleaved):  # noqa: F811
+    # zeros whatever the weights are; an infinite element is no number, its head's others are zeros; the rows beside stay as they are, and V's do
+    torch = torch_cuda
+    D, R, H = 64, 32, 4
+    c = Cache(torch, 3, [n_new + 20], heads=H, group=1, D=D, dtype=dtype)
+    q, k, v = (c.normal((1, 1, H, n_new, D)) for _ in range(3))
+    freq = torch.tensor([100.0 ** (-2 * i / R) for i in range(R // 2)], dtype=torch.float32, device="cuda")
+    w = torch.full((1, D), 8.0, device="cuda")
+    pos = torch.tensor([5], dtype=torch.int32, device="cuda")
+
+    def call():
+        out = torch.full(q.shape, 77.0, dtype=c.dt, device="cuda")
+        c.B.sablock_append_normed_paged(c.pages, c.B.make_new_tokens(k, v, q, rotary_dim=R, interleaved=interleaved), c.B.make_head_norms(1e-6), k, v, pos, freq,
+                                        c.table, c.lengths, c.k_pool, c.v_pool, q=q, q_out=out, q_weight=w, k_weight=w)
+        return out, c.rows(c.k_pool, 0)[0, :, 20:].clone(), c.rows(c.v_pool, 0)[0, :, 20:].clone()
+
+    clean = call()
+    at, most = n_new // 2, torch.finfo(c.dt).max
+    q[0, 0, 0, at], q[0, 0, 2, at] = most, -most
+    k[0, 0, 1, at], v[0, 0, 1, at], v[0, 0, 3, at, 7] = most, most, INF
+    q[0, 0, 3, at, 60] = INF
+    got = call()
+    assert not got[0][0, 0, 0, at].any() and not got[0][0, 0, 2, at].any() and not got[1][1, at].any()
+    assert bool(torch.isnan(got[0][0, 0, 3, at, 60])) and not got[0][0, 0, 3, at, :60].any()
+    assert bool((got[2][1, at] == most).all()) and got[2][3, at, 7] == INF
+    got[0][0, 0, [0, 2, 3], at], got[1][1, at], got[2][1, at], got[2][3, at, 7] = clean[0][0, 0, [0, 2, 3], at], clean[1][1, at], clean[2][1, at], clean[2][3, at, 7]
+    for a, b in zip(got, clean):
+        assert torch.equal(a, b)
+
+
 def test_weights_of_ones_and_normed_rows_are_the_plain_append(torch_cuda):  # noqa: F811
     # rows whose mean square is one, eps too small to matter: the norm's factor is one to half a step of fp32, the append's result the other call's
     torch = torch_cuda
