@@ -27,7 +27,8 @@ struct WeighedArgs : DecodePagedArgs {
     __device__ __forceinline__ void weigh(int s, int layer, int head, int r, int len, const f32x2 *stats, Logits &&logits_of) const
     {
         const int id = page_at(d, pv.table, s, r >> d.shift);
-        const int fresh = len - (counts ? min(max(counts[s], 0), n_new) : n_new);              // rows from here on have gathered nothing
+        // rows from here on have gathered nothing.  Not rows_of: new rows that the table has no room for are not the last ones that it has
+        const int fresh = max(pv.lengths[s], 0) - (counts ? min(max(counts[s], 0), n_new) : n_new);
         if (id < 0) return;
         f32x4 *at = reinterpret_cast<f32x4 *>(gathered + weight_at(d, layer, id, head) + (r & (d.page - 1)));
         const f32x4 old = *at;

@@ -138,10 +138,18 @@ def test_pages_that_do_not_exist_and_lengths_beyond_the_table(torch_cuda):  # no
     c.table.copy_(full)
     want = _weights(c)
     got = want.clone()
-    _decode(c, q, want, n_new=2)
+    # behind a full table the new rows have no place, and the last ones in front of them have gathered before
+    some = want.clone()
+    _decode(c, q, want, n_new=2, counts=[2, 2, 0])
     c.lengths = torch.tensor([100, 64, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
     _decode(c, q, got, n_new=2)
     assert torch.equal(got, want)
+    c.lengths = torch.tensor([100, 64, 209], dtype=torch.int32, device="cuda")
+    _decode(c, q, some, n_new=2)
+    last = int(full[2, 12])
+    assert bool((some[0, last, :, 15] != want[0, last, :, 15]).all())
+    some[0, last, :, 15] = want[0, last, :, 15]
+    assert torch.equal(some, want)
     c.lengths = torch.tensor([-7, 64, 208], dtype=torch.int32, device="cuda")
     again = was.clone()
     assert not _decode(c, q, again)[0].any()
