@@ -668,9 +668,6 @@ decode_paged_merge_kernel(Args a)
         den += own[1] * w[i];
     }
     den = over_lanes<1>(den, false);
-    if constexpr (Args::STATS) {
-        if (tid == 0) *reinterpret_cast<f32x2 *>(a.stats + ((int64_t)p * d.G + g) * 2) = f32x2{m, den == 0.f ? 0.f : 1.f / den};
-    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // w: other lanes' stores from here on
     f32x4 t{0.f, 0.f, 0.f, 0.f};
     if (group < groups) {

@@ -100,7 +100,7 @@ pick_rows_kernel(PageDims d, PageView pv, EvictDims ed)
     const int n = rows_of(d, pv.lengths, s);
     int32_t *list = ed.rows_out + (int64_t)p * ed.n_keep;
     if (n <= ed.n_keep) {
-        for (int i = tid; i < ed.n_keep; i += PICK_NT) list[i] = i < n ? i : -1;
+        for (uint32_t i = tid; i < (uint32_t)ed.n_keep; i += PICK_NT) list[i] = (int)i < n ? (int)i : -1;
         return;
     }
     pick<RUN>(sh, own, nullptr, n, ed.n_keep, ed.n_first, ed.n_last, [&](int at, int i) __attribute__((always_inline)) { list[at] = i; });

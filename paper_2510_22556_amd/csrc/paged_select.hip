@@ -213,7 +213,7 @@ pick_pages_kernel(PageDims d, PageView pv, int n_pick, int n_first, int n_last, 
     const int n = (rows_of(d, pv.lengths, seq_of_problem(d, p)) + d.page - 1) >> d.shift;
     int32_t *list = list_all + (int64_t)p * n_pick;
     if (n <= n_pick) {
-        for (int i = tid; i < n_pick; i += PICK_NT) list[i] = i < n ? i : -1;
+        for (uint32_t i = tid; i < (uint32_t)n_pick; i += PICK_NT) list[i] = (int)i < n ? (int)i : -1;
         return;
     }
     pick<RUN>(sh, own, keys, n, n_pick, n_first, n_last, [&](int at, int i) __attribute__((always_inline)) { list[at] = i; });
