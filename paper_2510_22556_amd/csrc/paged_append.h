@@ -45,6 +45,21 @@ template <int B> __device__ __forceinline__ void over_row(float (&x)[B], int lan
 #undef SABLOCK_OVER
 }
 
+// numbers of the lane `apart` lanes on or back: where that is one bit of the lane's number, without LDS
+template <int N> __device__ __forceinline__ void from_partner(float (&z)[N], const float (&y)[N], int apart, int partner)
+{
+    if (apart == 8) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = xor_lane<8>(y[e]);
+    } else if (apart == 4) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = xor_lane<4>(y[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = __shfl(y[e], partner);
+    }
+}
+
 // grid (touched pages, sequences x layers, parts of the head rows).  The angle of a (token, pair) is the same for all heads: formed
 // once per workgroup, position * inv_freq in fp64 (at position 131 072 an angle in fp32 is off by up to 2^-8), see turn() of either
 // type.  A thread has one chunk of every groups-th row of a head, a row's chunks lie in the lanes of one wavefront, where
@@ -55,7 +70,7 @@ template <int B> __device__ __forceinline__ void over_row(float (&x)[B], int lan
 // Loads of a step are issued whatever the lane has to do there (at the nearest place that exists): behind a branch the compiler could
 // not count the loads in flight and would wait for all of them.  A step whose rows all exist stores without a branch for the same reason.
 template <bool BF16, bool ONE, bool SPLIT, typename Args>
-__global__ void __launch_bounds__(NT, ONE || (SPLIT && std::is_same_v<Args, AppendArgs>) ? 4 : 3)
+__global__ void __launch_bounds__(NT, ONE || (std::is_same_v<Args, AppendArgs> ? SPLIT : !BF16) ? 4 : 3)
 append_paged_kernel(Args a)
 {
     using E = Elem<BF16>;
@@ -94,24 +109,18 @@ append_paged_kernel(Args a)
         const int64_t *st = is_k ? a.t.ks : is_v ? a.t.vs : a.t.qs;
         return Source{(is_k ? a.k : is_v ? a.v : a.q) + (s * st[0] + layer * st[1] + head * st[2]) * E::BYTES + min(c, a.chunks - 1) * 16, st[3] * E::BYTES};
     };
-    // weights of this chunk's elements and, SPLIT, of those that its pairs have in the other chunk, with the sign that they come with; V's lanes load q's or K's, and do not use them
-    struct Weights { float own[NORM ? E::N : 1], other[NORM && SPLIT ? E::N : 1]; };
+    // weights of this chunk's elements; V's lanes load q's or K's, and do not use them
+    struct Weights { float own[NORM ? E::N : 1]; };
     auto load_weights = [&](int base, Weights &w) {
         if constexpr (NORM) {
             const int slot = min(base + lane_slot, slot_end - 1);
             const bool is_q = slot >= 2 * d.Hkv;
             const float *at = is_q ? a.q_weight + layer * a.q_layer + (slot - 2 * d.Hkv) * a.head : a.k_weight + layer * a.k_layer + min(slot, d.Hkv - 1) * a.head;
-            const int mine = min(c, a.chunks - 1), partner_chunk = mine + partner - tid;
 #pragma unroll
             for (int e = 0; e < E::N; e += 4) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(at + mine * E::N + e);
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(at + min(c, a.chunks - 1) * E::N + e);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w.own[e + j] = x[j];
-                if constexpr (SPLIT) {
-                    const f32x4 z = *reinterpret_cast<const f32x4 *>(at + partner_chunk * E::N + e);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w.other[e + j] = upper ? z[j] : -z[j];
-                }
             }
         }
     };
@@ -188,7 +197,7 @@ append_paged_kernel(Args a)
             }
             auto turn_row = [&](int i) {
                 u32x4 w = x[i], o{0, 0, 0, 0};
-                if constexpr (SPLIT) {
+                if constexpr (SPLIT && !NORM) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[e] = (uint32_t)__shfl((int)w[e], partner);
                 }
@@ -197,22 +206,25 @@ append_paged_kernel(Args a)
                     if (is_v) return w;
 #pragma unroll
                     for (int e = 0; e < E::N; ++e) y[e] = E::get(w, e) * weights.own[e];
+                    float z[SPLIT ? E::N : 1];                 // the pairs' other elements
+                    if constexpr (SPLIT) from_partner(z, y, pair_chunks, partner);
                     if (turned) {
                         const float4 *angles = reinterpret_cast<const float4 *>(turn + min(group + (bt * B + i) * a.groups, n - 1) * half + angle);
                         if constexpr (SPLIT) {
+                            const float sign = upper ? 1.f : -1.f;
 #pragma unroll
                             for (int e = 0; e < E::N; e += 2) {
                                 const float4 t = angles[e / 2];
-                                y[e] = y[e] * t.x + E::get(o, e) * weights.other[e] * t.y;
-                                y[e + 1] = y[e + 1] * t.z + E::get(o, e + 1) * weights.other[e + 1] * t.w;
+                                y[e] = fmaf(z[e], sign * t.y, y[e] * t.x);
+                                y[e + 1] = fmaf(z[e + 1], sign * t.w, y[e + 1] * t.z);
                             }
                         } else {
 #pragma unroll
                             for (int e = 0; e < E::N; e += 2) {
                                 const float4 t = angles[e / 4];
-                                const float u = y[e], z = y[e + 1], cs = e % 4 ? t.z : t.x, sn = e % 4 ? t.w : t.y;
-                                y[e] = u * cs - z * sn;
-                                y[e + 1] = z * cs + u * sn;
+                                const float u = y[e], v = y[e + 1], cs = e % 4 ? t.z : t.x, sn = e % 4 ? t.w : t.y;
+                                y[e] = u * cs - v * sn;
+                                y[e + 1] = v * cs + u * sn;
                             }
                         }
                     }
