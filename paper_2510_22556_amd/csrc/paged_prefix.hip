@@ -54,14 +54,9 @@ struct PrefixArgs : DecodePagedArgs {
 constexpr int XCDS = 8;
 constexpr int TILE = 16;                       // columns of a matrix product
 
-__device__ __forceinline__ int64_t over_wave(int64_t x)
-{
-    for (int m = 1; m < 64; m *= 2) x += (int64_t)__shfl_xor((long long)x, m);
-    return x;
-}
-
 // How the prefixes' rows are cut: pieces of `run` steps at most, as many as there are workgroups if those are enough.  A wavefront's view, a
-// prefix per lane, 64 of them at a time.
+// prefix per lane, 64 of them at a time.  32 bits count all steps (the call's limits see to it), as those of prefixes that do not follow each other: these are
+// cut somehow, and `slots` bounds the pieces.
 template <int STEP, int COLUMNS>
 struct Cut {
     const PrefixArgs &a;
@@ -70,17 +65,17 @@ struct Cut {
     __device__ Cut(const PrefixArgs &args, int l) : a(args), lane(l), heads(args.d.n_layers * args.d.Hkv)
     {
         own = load(lane);
-        int64_t steps = 0, blocks = 0;
+        uint32_t steps = 0, blocks = 0;
         for (int base = 0; base < a.prefixes.n; base += 64) {
             const Prefix x = at(base);
-            const int64_t b = x.pages ? (int64_t)heads * blocks_of(x) : 0;
+            const uint32_t b = x.pages ? (uint32_t)heads * blocks_of(x) : 0;
             steps += b * steps_of_pages(x.pages);
             blocks += b;
         }
-        steps = over_wave(steps);
-        blocks = over_wave(blocks);
-        const int64_t free = a.prefix_workgroups - blocks, shares = free > 0 ? free : a.prefix_workgroups;
-        run = (int)min(max((int64_t)LEAST_STEPS, (steps + shares - 1) / shares), (int64_t)1 << 27);      // no table has room for more
+        steps = of_lane(sum_upto_lane(steps), 63);
+        blocks = of_lane(sum_upto_lane(blocks), 63);
+        const uint32_t all = a.prefix_workgroups, shares = blocks < all ? all - blocks : all;
+        run = (int)min(max((uint32_t)LEAST_STEPS, (steps + shares - 1) / shares), 1u << 27);            // no table has room for more
         total = before(a.prefixes.n);
     }
     __device__ Prefix load(int i) const { return i < a.prefixes.n ? prefix_at(a.d, a.prefixes, i) : Prefix{0, 0, 0}; }
