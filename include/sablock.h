@@ -16,7 +16,9 @@
  * sablock_score_all_heads / sablock_compact_shared are the variant with one retained set per layer.
  * sablock_compact_paged puts the retained rows into the pages of a cache instead, sablock_append_paged adds new tokens to
  * those (rotating queries and keys on the way), sablock_decode_paged is the decode step over them, and
- * sablock_select_pages picks the pages that such a step should read.
+ * sablock_select_pages picks the pages that such a step should read.  sablock_append_normed_paged is the append of models that norm
+ * queries and keys per head; sablock_decode_weighed_paged a decode step that gathers every row's share of the attention, by which
+ * sablock_evict_paged cuts the cache back; sablock_decode_prefix_paged one that reads the pages that sequences have in common once.
  *
  * Conventions shared by all calls
  * -------------------------------
@@ -526,7 +528,8 @@ SABLOCK_API sablock_status sablock_decode_weighed_paged(const sablock_pages *pag
  *                 sequences of a prefix that only one has.
  *   ws            at least sablock_decode_prefix_paged_workspace_bytes(pages, n_prefixes) bytes, 16-byte aligned
  * Appends go behind the prefix as ever, into pages that only their sequence has: a prefix is whole pages.
- * 1 <= n_prefixes <= 4096; n_seq * n_layers * n_kv_heads * (max_pages * page_size / 16 + 1) < 2^30 (UNSUPPORTED beyond).  Values out of range in prefix_begin and prefix_pages are taken as the nearest in range. */
+ * 1 <= n_prefixes <= 4096; n_seq * n_layers * n_kv_heads * (max_pages * page_size / 16 + 1) < 2^30 (UNSUPPORTED beyond).  Values out of range in
+ * prefix_begin and prefix_pages are taken as the nearest in range. */
 SABLOCK_API sablock_status sablock_decode_prefix_paged_workspace_bytes(const sablock_pages *pages, int32_t n_prefixes, size_t *bytes_out);
 SABLOCK_API sablock_status sablock_decode_prefix_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool,
                                     const int32_t *page_table, const int32_t *lengths, const int32_t *prefix_begin,

@@ -1,4 +1,4 @@
-// The paged cache's writers: the retained rows of a compression into pages (end of Sec. 3.3), and new tokens behind them with
+// The paged cache's writers (what they share is in paged_rows.h, the appending kernel in paged_append.h): the retained rows of a compression into pages (end of Sec. 3.3), and new tokens behind them with
 // the position rotation of queries and keys on the way.  Both are copies, 16 bytes per lane, and both keep the page bounds: the
 // least and the largest value of every element of K over a page's rows, taken on order-preserving whole numbers (a
 // packed 16-bit minimum serves two bf16 elements) and joined over the rows of a workgroup through LDS.

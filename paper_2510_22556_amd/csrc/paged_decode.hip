@@ -1,3 +1,5 @@
+// The decode step over all of a sequence's pages or over listed ones: the kernel and its launch are paged_decode.h's, where the mathematics and what
+// bounds it are.
 #include "paged_decode.h"
 
 namespace sablock {

@@ -8,6 +8,15 @@
 //
 // A sequence takes part in its prefix if all the prefix's rows are its own; one that ends before reads its rows by itself, so that no row of
 // the prefix has to be masked for one column and not for another.
+//
+// What bounds it: with many columns the matrix products.  64 sequences x 32 query heads over 32 768 common rows and up to 2 048 of their own (8 heads of 128 bf16
+// elements, 405 MB, 35 GFLOP, twice that with probabilities in three parts): 113-117 us where a large product's rate would take 59 and the reads 62;
+// the start takes 13 us and the pieces' sums are 17 MB to write and read again, 13 us of it their joining.  The common rows alone 107 us; products run at
+// 690 TFLOP/s over the kernel, at 957 over 131 072 common rows (287 us), and a large product's at 1 204.  Few columns: the chain of begins, lengths, table
+// and rows, and that of the second launch: 8 sequences x 2 048 common rows 15.0 us in a graph (12.8 and 4.6), the counting in 64 bits 1 more.
+// On the way, 64 x 32 768 and 8 x 2 048: in three launches, a wavefront's tiles fed from memory 238 and 28.9; an XCD's blocks of columns over the same
+// rows 184; K and V in LDS 160; the probabilities' parts by dot products 157; one launch for prefixes and own rows, the joins as one 122 and 18.1;
+// pieces over all XCDs however few 115.  Products of a step between the next one's vector instructions: 123 in place of 115, not taken.
 #include "paged_decode.h"
 
 namespace sablock {
@@ -707,13 +716,16 @@ join_kernel(PrefixArgs a)
     *reinterpret_cast<out4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
 }
 
-// Prefixes have more than 64 columns on average, and the rows of a step lie within reach of 31 bits
+// Prefixes have more than 64 columns on average, and the rows of a step lie within reach of 31 bits.  Wide against narrow, 68 columns and 128: 2 048 rows 20.1 and
+// 21.5 us, 23.8 and 25.8; 8 192 rows 26.2 and 29.4, 30.3 and 34.0; 32 768 rows 57.5 and 56.7, 59.3 and 66.0.  64 columns, 32 768 rows: narrow 45.5.
 bool prefix_wide(const PageDims &d, int n_prefixes)
 {
     const int64_t reach = 31 * 2 * std::max(d.ks[3], d.vs[3]);
     return d.dtype == SABLOCK_BF16 && d.D <= 128 && (int64_t)d.n_seq * d.G > 64 * (int64_t)n_prefixes && reach + 256 < (int64_t)1 << 31;
 }
 int prefix_columns(const PageDims &d, int n_prefixes) { return prefix_wide(d, n_prefixes) ? WIDE : prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
+// A wide workgroup for every compute unit, beside one of the own rows' (two: 139 us in place of 122 for 64 x 32 768 and own rows, the common rows alone 101
+// in place of 107), and two narrow ones
 int prefix_workgroups(const PageDims &d, int n_prefixes) { return (d.cus * (prefix_wide(d, n_prefixes) ? 1 : 2) + XCDS - 1) / XCDS * XCDS; }
 // pieces at most: one more than its share for every workgroup, and one for every block of columns, of which the last ones of prefixes of two sequences
 // or more may be short

@@ -6,8 +6,8 @@
 //
 // What bounds it: the attention's reads, and the writes among them, which cost far more than their bytes: 64 sequences of up to 8 192 rows, 8 heads of 128 bf16
 // elements, four query heads each (1.07 GB read): the kernel takes 172 us without the logits' 34 MB, 228 with a store in every step, whatever its layout or
-// cache policy, 224 with stores of eight steps at a time, 217 with as many logits in LDS as fit: 230 us in all.  8 heads x 1 056 rows: 11.3 us, with
-// a launch of its own for the weighing 14.3.
+// cache policy, 224 with stores of eight steps at a time, 212-217 with as many logits in LDS as fit: 229 us in all, 18 of them the joining and weighing.  8 heads
+// x 1 056 rows: 10.6 us in a graph, with a launch of its own for the weighing 14.3.
 #include "paged_decode.h"
 
 namespace sablock {

@@ -17,7 +17,7 @@ def _call(lib, pages=None, **changed):  # noqa: F811
     return lib.sablock_decode_prefix_paged(ctypes.byref(pages or _pages()), *a.values(), None)
 
 
-@pytest.mark.parametrize("change,status", BAD_PAGES + [(dict(n_q_heads=34), 2), (dict(head_dim=48), 2), (dict(head_dim=24, dtype=0), 2), (dict(n_seq=3, max_pages=1 << 26), 2)], ids=lambda c: str(c))
+@pytest.mark.parametrize("change,status", BAD_PAGES + [(dict(n_q_heads=34), 2), (dict(head_dim=48), 2), (dict(head_dim=24, dtype=0), 2), (dict(n_seq=4, max_pages=1 << 26), 2)], ids=lambda c: str(c))
 def test_caches(lib, change, status):  # noqa: F811
     assert _call(lib, _pages(**change)) == status
     n = ctypes.c_size_t(7)
@@ -43,6 +43,8 @@ def test_workspace(lib):  # noqa: F811
     for n in (1, 5, 4096):
         assert lib.sablock_decode_prefix_paged_workspace_bytes(ctypes.byref(_pages()), n, ctypes.byref(size)) == 0 and size.value > plain.value
     assert lib.sablock_decode_prefix_paged_workspace_bytes(None, 1, ctypes.byref(size)) == 1
+    # 12 problems of 2^26 steps and one are 805 306 380, below 2^30; 16 of them, above, are refused
+    assert lib.sablock_decode_prefix_paged_workspace_bytes(ctypes.byref(_pages(n_seq=3, max_pages=1 << 26)), 1, ctypes.byref(size)) == 0
     assert lib.sablock_decode_prefix_paged_workspace_bytes(ctypes.byref(_pages()), 1, None) == 1
 
 
