@@ -544,7 +544,8 @@ SABLOCK_API sablock_status sablock_decode_prefix_paged(const sablock_pages *page
  *   weights        [n_layers][n_pages][n_kv_heads][page_size] fp32, dense, 16-byte aligned: of every row, what sablock_decode_weighed_paged
  *                  gathers in them or any other number
  *   page_table_out [n_seq][max_pages]: of its pages, those in front of ceil(rows that stay / page_size) are named once, and none of them
- *                  lies within a sequence's old rows
+ *                  lies within a sequence's old rows; but the rows of a sequence that keeps all may stay where they are, its entries those of the
+ *                  old table
  *   lengths_out    [n_seq]: min(rows, n_keep).  An array of its own, as the new table is: the calls of all layers take the old ones
  *   rows_out       [P][n_keep] int32: the old rows that stay, ascending, -1 behind the last
  *   bounds         nullable; written for every page that gets a row

@@ -40,7 +40,8 @@ row_keys_kernel(PageDims d, PageView pv, const float *weights, uint32_t *keys, i
     }
 }
 
-// grid (pages of the rows that stay, problems)
+// grid (pages of the rows that stay, problems).  Where a sequence keeps all its rows in the pages that they lie in, every thread writes what it has read from there
+// (not to do so costs the others' workgroups 2 %, 377 -> 383 us: they wait for the old page's number)
 template <bool BF16>
 __global__ void __launch_bounds__(NT)
 evict_kernel(PageDims d, PageView pv, EvictDims ed, int chunks)

@@ -107,6 +107,33 @@ def _check(c, first, last):
     return lists
 
 
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("f32", 64)])
+def test_sequences_that_stay_where_they_are(torch_cuda, dtype, page):  # noqa: F811
+    # the old entries of those that keep all their rows: pages that two of them share as well; the others' rows move
+    torch = torch_cuda
+    c = Evictable(torch, 21, [100, 300, 90, 0, 128, 77], 128, layers=2, heads=2, group=2, D=64, dtype=dtype, page=page).randomise()
+    for s in (0, 2, 4):
+        c.after[s] = c.table[s]
+    c.table[2, 0] = c.after[2, 0] = c.table[0, 0]
+    before = c.table.clone()
+    was = [t.clone() for t in (c.k_pool, c.v_pool, c.weights)]
+    c.evict(4, 16)
+    assert c.len_out.tolist() == [100, 128, 90, 0, 128, 77] and torch.equal(c.table, before)
+    lists = _ref_rows(c, was[2].cpu(), 4, 16)
+    assert c.rows_out.tolist() == [x + [-1] * (c.keep - len(x)) for x in lists]
+    held = {int(c.table[s, i]): min(page, n - i * page) for s, n in ((0, 100), (2, 90), (4, 128)) for i in range(-(-n // page))}
+    stay = sorted(held)
+    for at, m in held.items():
+        rows = c.k_pool[:, at, :, :m].float()
+        assert torch.equal(c.bounds[:, at, :, 0].float(), rows.amin(dim=2)) and torch.equal(c.bounds[:, at, :, 1].float(), rows.amax(dim=2))
+    for got, old in zip((c.k_pool, c.v_pool, c.weights), was):
+        assert torch.equal(got[:, stay], old[:, stay])
+        for p, rows in enumerate(lists):
+            s, l, h = p // 4, p // 2 % 2, p % 2
+            for j, r in enumerate(rows):
+                assert torch.equal(got[l, int(c.after[s, j // page]), h, j % page], old[l, int(c.table[s, r // page]), h, r % page])
+
+
 @pytest.mark.parametrize("D,dtype,page", [(8, "f32", 16), (64, "bf16", 16), (96, "bf16", 32), (128, "bf16", 64), (256, "bf16", 256), (256, "f32", 16), (40, "bf16", 128)])
 @pytest.mark.parametrize("keep,first,last", [(1, 0, 0), (1, 0, 1), (17, 1, 1), (64, 4, 16), (100, 0, 50), (300, 150, 150), (400, 3, 0)])
 def test_evict(torch_cuda, D, dtype, page, keep, first, last):  # noqa: F811
