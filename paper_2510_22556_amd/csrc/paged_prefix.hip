@@ -461,21 +461,23 @@ template <int N> __device__ __forceinline__ void row_of_lds(uint32_t (&w)[N], co
 // all LDS traffic of this wavefront done, then the workgroup barrier (loads to LDS stay in flight)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The same for prefixes with many columns, bf16 heads of up to 128 elements: a wavefront has columns of its own, 32 of the workgroup's 128, and all
-// wavefronts do every step, from K and V in LDS.  Steps come there four at a time, each wavefront seeing to a quarter of the pieces of 1 KiB; a
-// piece's rows lie in one page.  One barrier per step: everybody's pieces of this step have landed, and the last step's place is free.
+// The same for prefixes with many columns, bf16 heads of up to 128 elements, or 256: a wavefront has columns of its own, 32 of the workgroup's 128 (or
+// 16 of 64), and all wavefronts do every step, from K and V in LDS.  Steps come there four (two) at a time, each wavefront seeing to a quarter of the pieces of
+// 1 KiB; a piece's rows lie in one page.  One barrier per step: everybody's pieces of this step have landed, and the last step's place is free.
 // A row of K in LDS has its 16-byte chunks in the order of place(): the 16 rows of an operand, (m >> 2) * 8 + (m & 3) apart from 4, come from different banks.
-constexpr int WIDE_TILES = 2, WIDE = NW * WIDE_TILES * TILE, STAGES = 4;
+constexpr int wide_tiles(int D) { return D <= 128 ? 2 : 1; }
+constexpr int wide_columns(int D) { return NW * wide_tiles(D) * TILE; }
+constexpr int wide_stages(int D) { return D <= 128 ? 4 : 2; }
 template <int EP> __device__ __forceinline__ int place(int chunk, int row)
 {
-    return chunk ^ (EP == 8 ? (row >> 3) * 4 + (row & 3) : EP == 4 ? (row >> 3) * 2 + (row >> 1 & 1) : row >> 3);
+    return chunk ^ (EP >= 8 ? (row >> 3) * 4 + (row & 3) : EP == 4 ? (row >> 3) * 2 + (row >> 1 & 1) : row >> 3);
 }
 
-constexpr int wide_bytes(int D) { return STAGES * 2 * 32 * D * 2; }
+constexpr int wide_bytes(int D) { return wide_stages(D) * 2 * 32 * D * 2; }
 template <int EP>
 __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
 {
-    constexpr int D = EP * 16, STEP = 32, R = 8, KT = 2, CT = WIDE_TILES, KC = D / 32, VW = EP / 2;
+    constexpr int D = EP * 16, STEP = 32, R = 8, KT = 2, CT = wide_tiles(D), KC = D / 32, VW = EP / 2, WIDE = wide_columns(D), STAGES = wide_stages(D);
     constexpr int ROW = D * 2, CHUNKS = D / 8, PIECES = D / 16, OWN = (PIECES + NW - 1) / NW, KV = STEP * ROW;
     static_assert(wide_bytes(D) == STAGES * 2 * KV);
     const PageDims &d = a.d;
@@ -496,7 +498,7 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
     uint32_t k_at[KC];
 #pragma unroll
     for (int e = 0; e < KC; ++e) k_at[e] = krow * ROW + place<EP>(4 * e + c, krow) * 16;
-    const uint32_t v_at = R * c * ROW + m * (EP * 2);
+    const uint32_t v_at = R * c * ROW + m * (EP <= 8 ? EP * 2 : 16);
 
     const Cut<STEP, WIDE> cut(a, lane);
     cut.each_piece([&](int x) __attribute__((always_inline)) {
@@ -586,7 +588,18 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
             for (int u = 0; u < CT; ++u) asm volatile("" : "+v"(most[u]));
             uint32_t v[R][VW];
 #pragma unroll
-            for (int r = 0; r < R; ++r) row_of_lds<VW>(v[r], vt + v_at + r * ROW);
+            for (int r = 0; r < R; ++r) {
+                if constexpr (EP <= 8) {
+                    row_of_lds(v[r], vt + v_at + r * ROW);
+                } else {                                       // eight elements of either half: side by side the lanes' 32 bytes would lie in half of the banks
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const u32x4 x = *reinterpret_cast<const u32x4 *>(vt + v_at + r * ROW + y * ROW / 2);
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) v[r][4 * y + w] = x[w];
+                    }
+                }
+            }
             const uint32_t now = there >> 2 * (STAGES - 1) & 3;
             if (now != 3 && !(now >> (c >> 1) & 1)) {
 #pragma unroll
@@ -614,13 +627,14 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
             own.den[u] = over_quarters(own.den[u], false);
             const int col = column0 + u * TILE + m;
             if (col >= columns) continue;
-            const int64_t slot = (int64_t)x * WIDE + wave * CT * TILE + u * TILE + m;          // elements EP (4 c + w) + e of the column
+            const int64_t slot = (int64_t)x * WIDE + wave * CT * TILE + u * TILE + m;          // elements EP (4 c + w) + e of the column, or of either half 8 (4 c + w) + e
             if (c == 0) *reinterpret_cast<f32x2 *>(a.piece_weights + slot * 2) = f32x2{own.ref[u], own.den[u]};
-            float *o = a.piece_sums + slot * D + EP * 4 * c;
+            constexpr int RUN = EP <= 8 ? EP : 8;
+            float *o = a.piece_sums + slot * D + RUN * 4 * c;
 #pragma unroll
             for (int w = 0; w < 4; ++w)
 #pragma unroll
-                for (int e = 0; e < EP; ++e) o[EP * w + e] = own.acc[u][e][w];
+                for (int e = 0; e < EP; ++e) o[e / RUN * (D / 2) + RUN * w + e % RUN] = own.acc[u][e][w];
         }
     });
 }
@@ -638,8 +652,8 @@ template <bool BF16, int EP, bool MANY> struct PrefixPart : PrefixArgs {
 };
 
 constexpr int JOIN_EARLY = 4;
-// grid (G, problems)
-template <int STEP, int COLUMNS>
+// grid (G, problems).  STEP: of the own rows, CUT: of the prefixes
+template <int STEP, int CUT, int COLUMNS>
 __global__ void __launch_bounds__(MERGE_T)
 join_kernel(PrefixArgs a)
 {
@@ -653,7 +667,7 @@ join_kernel(PrefixArgs a)
     int64_t first = 0, by = 0, own_first = -1;                 // rows of weights and sums; own_first < 0: finished
     if (skip) {
         const int i = uniform(prefix_of(a.prefixes, s));
-        const Cut<STEP, COLUMNS> cut(a, lane);
+        const Cut<CUT, COLUMNS> cut(a, lane);
         const Prefix prefix = cut.get(i);
         const int blocks = cut.blocks_of(prefix), column = (s - prefix.first) * d.G + g, block = column / COLUMNS;
         pieces = cut.pieces_of(prefix);
@@ -721,9 +735,9 @@ join_kernel(PrefixArgs a)
 bool prefix_wide(const PageDims &d, int n_prefixes)
 {
     const int64_t reach = 31 * 2 * std::max(d.ks[3], d.vs[3]);
-    return d.dtype == SABLOCK_BF16 && d.D <= 128 && (int64_t)d.n_seq * d.G > 64 * (int64_t)n_prefixes && reach + 256 < (int64_t)1 << 31;
+    return d.dtype == SABLOCK_BF16 && (d.D <= 128 || d.D == 256) && (int64_t)d.n_seq * d.G > 64 * (int64_t)n_prefixes && reach + 256 < (int64_t)1 << 31;
 }
-int prefix_columns(const PageDims &d, int n_prefixes) { return prefix_wide(d, n_prefixes) ? WIDE : prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
+int prefix_columns(const PageDims &d, int n_prefixes) { return prefix_wide(d, n_prefixes) ? wide_columns(d.D) : prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
 // A wide workgroup for every compute unit, beside one of the own rows' (two: 139 us in place of 122 for 64 x 32 768 and own rows, the common rows alone 101
 // in place of 107), and two narrow ones
 int prefix_workgroups(const PageDims &d, int n_prefixes) { return (d.cus * (prefix_wide(d, n_prefixes) ? 1 : 2) + XCDS - 1) / XCDS * XCDS; }
@@ -768,7 +782,8 @@ hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView
     a.limit = (rows_alone(d) + step - 1) / step;
     const dim3 grid(a.prefix_workgroups + d.P + a.workgroups);
     using Join = void (*)(PrefixArgs);
-    const Join join = wide ? join_kernel<32, WIDE> : prefix_tiles(bf, d.D) == 1 ? join_kernel<16, TILE> : step == 32 ? join_kernel<32, 2 * TILE> : join_kernel<16, 2 * TILE>;
+    const Join join = wide ? (d.D <= 128 ? join_kernel<32, 32, wide_columns(128)> : join_kernel<16, 32, wide_columns(256)>)
+                    : prefix_tiles(bf, d.D) == 1 ? join_kernel<16, 16, TILE> : step == 32 ? join_kernel<32, 32, 2 * TILE> : join_kernel<16, 16, 2 * TILE>;
 #define SABLOCK_PREFIX(BV, EV, WV)                                                                                                            \
     if (bf == BV && d.D == EV * 16 && wide == WV)                                                                                             \
         hipLaunchKernelGGL((decode_paged_kernel<BV, EV, step_rows(BV, EV * 16, false), true, PrefixPart<BV, EV, WV>>), grid, dim3(NT), 0, st, \
@@ -777,7 +792,7 @@ hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView
 #define SABLOCK_PREFIX_B(EV) SABLOCK_PREFIX(true, EV, false) SABLOCK_PREFIX(false, EV, false)
 #define SABLOCK_PREFIX_W(EV) SABLOCK_PREFIX(true, EV, true) SABLOCK_PREFIX_B(EV)
     SABLOCK_PREFIX_F(1) SABLOCK_PREFIX_W(2) SABLOCK_PREFIX_F(3) SABLOCK_PREFIX_W(4) SABLOCK_PREFIX_F(5) SABLOCK_PREFIX_W(6) SABLOCK_PREFIX_F(7) SABLOCK_PREFIX_W(8)
-    SABLOCK_PREFIX_F(9) SABLOCK_PREFIX_B(10) SABLOCK_PREFIX_F(11) SABLOCK_PREFIX_B(12) SABLOCK_PREFIX_F(13) SABLOCK_PREFIX_B(14) SABLOCK_PREFIX_F(15) SABLOCK_PREFIX_B(16)
+    SABLOCK_PREFIX_F(9) SABLOCK_PREFIX_B(10) SABLOCK_PREFIX_F(11) SABLOCK_PREFIX_B(12) SABLOCK_PREFIX_F(13) SABLOCK_PREFIX_B(14) SABLOCK_PREFIX_F(15) SABLOCK_PREFIX_W(16)
 #undef SABLOCK_PREFIX_W
 #undef SABLOCK_PREFIX_B
 #undef SABLOCK_PREFIX_F
