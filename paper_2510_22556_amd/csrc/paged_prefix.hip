@@ -461,8 +461,8 @@ template <int N> __device__ __forceinline__ void row_of_lds(uint32_t (&w)[N], co
 // all LDS traffic of this wavefront done, then the workgroup barrier (loads to LDS stay in flight)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The same for prefixes with many columns, bf16 heads of up to 128 elements, or 256: a wavefront has columns of its own, 32 of the workgroup's 128 (or
-// 16 of 64), and all wavefronts do every step, from K and V in LDS.  Steps come there four (two) at a time, each wavefront seeing to a quarter of the pieces of
+// The same for prefixes with many columns, bf16: a wavefront has columns of its own, 32 of the workgroup's 128 (or,
+// heads of more than 128 elements, 16 of 64), and all wavefronts do every step, from K and V in LDS.  Steps come there four (two) at a time, each wavefront seeing to a quarter of the pieces of
 // 1 KiB; a piece's rows lie in one page.  One barrier per step: everybody's pieces of this step have landed, and the last step's place is free.
 // A row of K in LDS has its 16-byte chunks in the order of place(): the 16 rows of an operand, (m >> 2) * 8 + (m & 3) apart from 4, come from different banks.
 constexpr int wide_tiles(int D) { return D <= 128 ? 2 : 1; }
@@ -470,7 +470,7 @@ constexpr int wide_columns(int D) { return NW * wide_tiles(D) * TILE; }
 constexpr int wide_stages(int D) { return D <= 128 ? 4 : 2; }
 template <int EP> __device__ __forceinline__ int place(int chunk, int row)
 {
-    return chunk ^ (EP >= 8 ? (row >> 3) * 4 + (row & 3) : EP == 4 ? (row >> 3) * 2 + (row >> 1 & 1) : row >> 3);
+    return chunk ^ (EP % 8 == 0 ? (row >> 3) * 4 + (row & 3) : EP % 8 == 4 ? (row >> 3) * 2 + (row >> 1 & 1) : row >> 3);
 }
 
 constexpr int wide_bytes(int D) { return wide_stages(D) * 2 * 32 * D * 2; }
@@ -498,7 +498,7 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
     uint32_t k_at[KC];
 #pragma unroll
     for (int e = 0; e < KC; ++e) k_at[e] = krow * ROW + place<EP>(4 * e + c, krow) * 16;
-    const uint32_t v_at = R * c * ROW + m * (EP <= 8 ? EP * 2 : 16);
+    const uint32_t v_at = R * c * ROW + m * (EP < 16 ? EP * 2 : 16);
 
     const Cut<STEP, WIDE> cut(a, lane);
     cut.each_piece([&](int x) __attribute__((always_inline)) {
@@ -589,7 +589,7 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
             uint32_t v[R][VW];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                if constexpr (EP <= 8) {
+                if constexpr (EP < 16) {
                     row_of_lds(v[r], vt + v_at + r * ROW);
                 } else {                                       // eight elements of either half: side by side the lanes' 32 bytes would lie in half of the banks
 #pragma unroll
@@ -627,9 +627,9 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
             own.den[u] = over_quarters(own.den[u], false);
             const int col = column0 + u * TILE + m;
             if (col >= columns) continue;
-            const int64_t slot = (int64_t)x * WIDE + wave * CT * TILE + u * TILE + m;          // elements EP (4 c + w) + e of the column, or of either half 8 (4 c + w) + e
+            const int64_t slot = (int64_t)x * WIDE + wave * CT * TILE + u * TILE + m;          // elements EP (4 c + w) + e of the column; EP = 16: 8 (4 c + w) + e of either half
             if (c == 0) *reinterpret_cast<f32x2 *>(a.piece_weights + slot * 2) = f32x2{own.ref[u], own.den[u]};
-            constexpr int RUN = EP <= 8 ? EP : 8;
+            constexpr int RUN = EP < 16 ? EP : 8;
             float *o = a.piece_sums + slot * D + RUN * 4 * c;
 #pragma unroll
             for (int w = 0; w < 4; ++w)
@@ -730,12 +730,14 @@ join_kernel(PrefixArgs a)
     *reinterpret_cast<out4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
 }
 
-// Prefixes have more than 64 columns on average, and the rows of a step lie within reach of 31 bits.  Wide against narrow, 68 columns and 128: 2 048 rows 20.1 and
+// Prefixes have more than 64 columns on average, 16 where heads have more than 128 elements, and the rows of a step lie within reach of 31 bits.  Wide against narrow, 68 columns and 128: 2 048 rows 20.1 and
 // 21.5 us, 23.8 and 25.8; 8 192 rows 26.2 and 29.4, 30.3 and 34.0; 32 768 rows 57.5 and 56.7, 59.3 and 66.0.  64 columns, 32 768 rows: narrow 45.5.
+// Heads of 256, 16 columns and 64: 2 048 rows 16.8 and 18.6 us, 24.4 and 26.2; 8 192 rows 26.1 and 27.9, 33.9 and 44.7; 32 768 rows 56.8 and 57.3, 68.4 and 132; 256
+// columns 215 and 561.
 bool prefix_wide(const PageDims &d, int n_prefixes)
 {
     const int64_t reach = 31 * 2 * std::max(d.ks[3], d.vs[3]);
-    return d.dtype == SABLOCK_BF16 && (d.D <= 128 || d.D == 256) && (int64_t)d.n_seq * d.G > 64 * (int64_t)n_prefixes && reach + 256 < (int64_t)1 << 31;
+    return d.dtype == SABLOCK_BF16 && (int64_t)d.n_seq * d.G > (d.D <= 128 ? 64 : 16) * (int64_t)n_prefixes && reach + 512 < (int64_t)1 << 31;
 }
 int prefix_columns(const PageDims &d, int n_prefixes) { return prefix_wide(d, n_prefixes) ? wide_columns(d.D) : prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
 // A wide workgroup for every compute unit, beside one of the own rows' (two: 139 us in place of 122 for 64 x 32 768 and own rows, the common rows alone 101
@@ -789,11 +791,9 @@ hipError_t launch_decode_prefix(const PageDims &d, const void *q, const PageView
         hipLaunchKernelGGL((decode_paged_kernel<BV, EV, step_rows(BV, EV * 16, false), true, PrefixPart<BV, EV, WV>>), grid, dim3(NT), 0, st, \
                            PrefixPart<BV, EV, WV>{a});
 #define SABLOCK_PREFIX_F(EV) SABLOCK_PREFIX(false, EV, false)
-#define SABLOCK_PREFIX_B(EV) SABLOCK_PREFIX(true, EV, false) SABLOCK_PREFIX(false, EV, false)
-#define SABLOCK_PREFIX_W(EV) SABLOCK_PREFIX(true, EV, true) SABLOCK_PREFIX_B(EV)
-    SABLOCK_PREFIX_F(1) SABLOCK_PREFIX_W(2) SABLOCK_PREFIX_F(3) SABLOCK_PREFIX_W(4) SABLOCK_PREFIX_F(5) SABLOCK_PREFIX_W(6) SABLOCK_PREFIX_F(7) SABLOCK_PREFIX_W(8)
-    SABLOCK_PREFIX_F(9) SABLOCK_PREFIX_B(10) SABLOCK_PREFIX_F(11) SABLOCK_PREFIX_B(12) SABLOCK_PREFIX_F(13) SABLOCK_PREFIX_B(14) SABLOCK_PREFIX_F(15) SABLOCK_PREFIX_W(16)
-#undef SABLOCK_PREFIX_W
+#define SABLOCK_PREFIX_B(EV) SABLOCK_PREFIX(true, EV, true) SABLOCK_PREFIX(true, EV, false) SABLOCK_PREFIX_F(EV)
+    SABLOCK_PREFIX_F(1) SABLOCK_PREFIX_B(2) SABLOCK_PREFIX_F(3) SABLOCK_PREFIX_B(4) SABLOCK_PREFIX_F(5) SABLOCK_PREFIX_B(6) SABLOCK_PREFIX_F(7) SABLOCK_PREFIX_B(8)
+    SABLOCK_PREFIX_F(9) SABLOCK_PREFIX_B(10) SABLOCK_PREFIX_F(11) SABLOCK_PREFIX_B(12) SABLOCK_PREFIX_F(13) SABLOCK_PREFIX_B(14) SABLOCK_PREFIX_F(15) SABLOCK_PREFIX_B(16)
 #undef SABLOCK_PREFIX_B
 #undef SABLOCK_PREFIX_F
 #undef SABLOCK_PREFIX

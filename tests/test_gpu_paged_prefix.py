@@ -63,7 +63,8 @@ def test_groups_heads_pages_and_lengths(torch_cuda, G, D, dtype, page, prefixes,
 
 @pytest.mark.parametrize("G,D,dtype,page,count,pages,heads", [(4, 128, "bf16", 16, 40, 150, 2), (7, 64, "bf16", 32, 30, 40, 3), (16, 256, "bf16", 16, 9, 120, 1), (1, 96, "bf16", 16, 200, 60, 1),
                                                               (5, 64, "f32", 16, 33, 80, 2), (2, 128, "f32", 64, 50, 12, 1), (4, 128, "bf16", 128, 129, 9, 2), (8, 32, "bf16", 16, 300, 30, 1),
-                                                              (3, 256, "bf16", 64, 30, 50, 2), (8, 256, "bf16", 256, 21, 5, 1), (2, 256, "bf16", 16, 70, 33, 2)])
+                                                              (3, 256, "bf16", 64, 30, 50, 2), (8, 256, "bf16", 256, 21, 5, 1), (2, 256, "bf16", 16, 70, 33, 2),
+                                                              (4, 160, "bf16", 16, 40, 33, 2), (3, 192, "bf16", 64, 27, 12, 2), (8, 224, "bf16", 32, 17, 40, 1)])
 def test_many_sequences(torch_cuda, G, D, dtype, page, count, pages, heads):  # noqa: F811
     # several blocks of columns, the last one short; sequences that end at their prefix, in front of it, or have nothing
     torch = torch_cuda
