@@ -529,7 +529,8 @@ SABLOCK_API sablock_status sablock_decode_weighed_paged(const sablock_pages *pag
  *   ws            at least sablock_decode_prefix_paged_workspace_bytes(pages, n_prefixes) bytes, 16-byte aligned
  * Appends go behind the prefix as ever, into pages that only their sequence has: a prefix is whole pages.
  * 1 <= n_prefixes <= 4096; n_seq * n_layers * n_kv_heads * (max_pages * page_size / 16 + 1) < 2^30 (UNSUPPORTED beyond).  Values out of range in
- * prefix_begin and prefix_pages are taken as the nearest in range. */
+ * prefix_begin and prefix_pages are taken as the nearest in range.  Where the begins descend, prefixes may be more than the workspace has room for: the
+ * sequences of those without get the attention over the rows behind their prefix alone. */
 SABLOCK_API sablock_status sablock_decode_prefix_paged_workspace_bytes(const sablock_pages *pages, int32_t n_prefixes, size_t *bytes_out);
 SABLOCK_API sablock_status sablock_decode_prefix_paged(const sablock_pages *pages, const void *q, const void *k_pool, const void *v_pool,
                                     const int32_t *page_table, const int32_t *lengths, const int32_t *prefix_begin,

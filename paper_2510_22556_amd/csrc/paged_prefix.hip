@@ -63,9 +63,15 @@ struct PrefixArgs : DecodePagedArgs {
 constexpr int XCDS = 8;
 constexpr int TILE = 16;                       // columns of a matrix product
 
+// Prefixes that do not follow each other may have any number of pieces.  Of each so many are counted, no more than the workspace has room for: 32 bits then
+// hold the sums of 4 096 prefixes (229 374 places at most, with 65 536 compute units), which never descend
+__host__ __device__ inline int counted_pieces(int all, int slots) { return all < slots ? all : slots; }
+// whether pieces at, at + blocks, .. of a block of columns have places in the workspace
+__host__ __device__ inline bool have_places(int64_t at, int pieces, int blocks, int slots) { return at >= 0 && at + (int64_t)(pieces - 1) * blocks < slots; }
+
 // How the prefixes' rows are cut: pieces of `run` steps at most, as many as there are workgroups if those are enough.  A wavefront's view, a
-// prefix per lane, 64 of them at a time.  32 bits count all steps (the call's limits see to it), as those of prefixes that do not follow each other: these are
-// cut somehow, and `slots` bounds the pieces.
+// prefix per lane, 64 of them at a time.  32 bits count all steps of prefixes that follow each other (the call's limits see to it).  Of others the sum may pass
+// them, and is good enough for a `run`, the same one everywhere.
 template <int STEP, int COLUMNS>
 struct Cut {
     const PrefixArgs &a;
@@ -93,7 +99,7 @@ struct Cut {
     {
         return i < 64 ? Prefix{of_lane(own.first, i), of_lane(own.count, i), of_lane(own.pages, i)} : prefix_at(a.d, a.prefixes, i);
     }
-    __device__ int all_of(const Prefix &x) const { return x.pages ? heads * blocks_of(x) * pieces_of(x) : 0; }
+    __device__ int all_of(const Prefix &x) const { return x.pages ? counted_pieces(heads * blocks_of(x) * pieces_of(x), a.slots) : 0; }
     __device__ int blocks_of(const Prefix &x) const { return (x.count * a.d.G + COLUMNS - 1) / COLUMNS; }
     __device__ int steps_of_pages(int pages) const { return ((pages << a.d.shift) + STEP - 1) / STEP; }
     __device__ int pieces_of(const Prefix &x) const { return x.pages ? (steps_of_pages(x.pages) + run - 1) / run : 0; }
@@ -672,7 +678,7 @@ join_kernel(PrefixArgs a)
         const int blocks = cut.blocks_of(prefix), column = (s - prefix.first) * d.G + g, block = column / COLUMNS;
         pieces = cut.pieces_of(prefix);
         const int64_t at = cut.before(i) + (int64_t)(p - s * cut.heads) * pieces * blocks + block;
-        if (at + (int64_t)(pieces - 1) * blocks >= a.slots) return;            // prefixes that do not follow each other
+        if (!have_places(at, pieces, blocks, a.slots)) pieces = 0;             // prefixes that do not follow each other: the own rows alone
         first = at * COLUMNS + column - block * COLUMNS;
         by = (int64_t)blocks * COLUMNS;
     }
@@ -684,8 +690,9 @@ join_kernel(PrefixArgs a)
         if (count > 1) {
             own_first = from;
             own_pieces = count;
-        } else if (skip == 0) return;
+        }
     }
+    if (pieces == 0 && own_first < 0) return;                  // finished
     struct Entry { f32x2 weight; const float *sums; };         // reference, denominator; numerators
     float *out = a.out + (((int64_t)s * d.n_layers + layer_of_problem(d, p)) * d.Hq + head_of_problem(d, p) * d.G + g) * d.D;
     auto entry = [&](int j) {
