@@ -929,7 +929,7 @@ sablock_status sablock_decode_prefix_paged(const sablock_pages *pages, const voi
     PageView pv;
     st = make_page_view(who, page_table, lengths, k_pool, v_pool, nullptr, &pv);
     if (st != SABLOCK_OK) return st;
-    const size_t need = decode_prefix_ws_bytes(pd, n_prefixes);
+    const size_t need = decode_prefix_ws_need(pd, n_prefixes);
     if (!ws || ws_bytes < need) return fail(SABLOCK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
     return dev(launch_decode_prefix(pd, q, pv, prefix_begin, prefix_pages, n_prefixes, out, ws, static_cast<hipStream_t>(stream)), who);
 }

@@ -741,11 +741,12 @@ join_kernel(PrefixArgs a)
 // 21.5 us, 23.8 and 25.8; 8 192 rows 26.2 and 29.4, 30.3 and 34.0; 32 768 rows 57.5 and 56.7, 59.3 and 66.0.  64 columns, 32 768 rows: narrow 45.5.
 // Heads of 256, 16 columns and 64: 2 048 rows 16.8 and 18.6 us, 24.4 and 26.2; 8 192 rows 26.1 and 27.9, 33.9 and 44.7; 32 768 rows 56.8 and 57.3, 68.4 and 132; 256
 // columns 215 and 561.
-bool prefix_wide(const PageDims &d, int n_prefixes)
+int prefixes_wide(const PageDims &d)           // up to so many
 {
     const int64_t reach = 31 * 2 * std::max(d.ks[3], d.vs[3]);
-    return d.dtype == SABLOCK_BF16 && (int64_t)d.n_seq * d.G > (d.D <= 128 ? 64 : 16) * (int64_t)n_prefixes && reach + 512 < (int64_t)1 << 31;
+    return d.dtype == SABLOCK_BF16 && reach + 512 < (int64_t)1 << 31 ? (d.n_seq * d.G - 1) / (d.D <= 128 ? 64 : 16) : 0;
 }
+bool prefix_wide(const PageDims &d, int n_prefixes) { return n_prefixes <= prefixes_wide(d); }
 int prefix_columns(const PageDims &d, int n_prefixes) { return prefix_wide(d, n_prefixes) ? wide_columns(d.D) : prefix_tiles(d.dtype == SABLOCK_BF16, d.D) * TILE; }
 // A wide workgroup for every compute unit, beside one of the own rows' (two: 139 us in place of 122 for 64 x 32 768 and own rows, the common rows alone 101
 // in place of 107), and two narrow ones
@@ -763,9 +764,15 @@ size_t sums_bytes(const PageDims &d, int n_prefixes) { return align256((size_t)p
 
 }  // namespace
 
-size_t decode_prefix_ws_bytes(const PageDims &d, int32_t n_prefixes)
+size_t decode_prefix_ws_need(const PageDims &d, int32_t n_prefixes)
 {
     return decode_ws_bytes_of(d) + stats_bytes(d) + weights_bytes(d, n_prefixes) + sums_bytes(d, n_prefixes);
+}
+// It grows with the prefixes but for one step down, from blocks of many columns to blocks of few: 64 sequences of 8 x 4 heads of 128, 3 prefixes 21.8 MB, 4 12.3
+size_t decode_prefix_ws_bytes(const PageDims &d, int32_t n_prefixes)
+{
+    const int wide = std::min(n_prefixes, prefixes_wide(d));
+    return std::max(decode_prefix_ws_need(d, n_prefixes), wide ? decode_prefix_ws_need(d, wide) : 0);
 }
 
 // 32 bits count all steps, as they do not where a table has room for more

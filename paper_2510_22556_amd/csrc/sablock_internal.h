@@ -345,7 +345,8 @@ size_t decode_paged_ws_bytes(const PageDims &pd);
 hipError_t launch_decode_paged(const PageDims &pd, const void *q, const PageView &pv, const int32_t *list, int32_t n_listed, float *out,
                                void *ws, hipStream_t st);
 bool decode_prefix_supported(const PageDims &pd);
-size_t decode_prefix_ws_bytes(const PageDims &pd, int32_t n_prefixes);
+size_t decode_prefix_ws_need(const PageDims &pd, int32_t n_prefixes);          // of a call
+size_t decode_prefix_ws_bytes(const PageDims &pd, int32_t n_prefixes);         // of all calls with so many prefixes or fewer
 hipError_t launch_decode_prefix(const PageDims &pd, const void *q, const PageView &pv, const int32_t *begin, const int32_t *pages, int32_t n_prefixes,
                                 float *out, void *ws, hipStream_t st);
 size_t decode_weighed_ws_bytes(const PageDims &pd);

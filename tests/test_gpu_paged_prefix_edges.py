@@ -1,4 +1,4 @@
-"""Decode attention of sequences with common pages where the arguments are odd: begins that descend."""
+"""Decode attention of sequences with common pages where the arguments are odd: begins that descend, a workspace for more prefixes."""
 
 import pytest
 
@@ -85,3 +85,30 @@ def test_as_many_descending_begins_as_a_call_takes_over_long_prefixes(torch_cuda
     got = _guarded(c, q, begin, [m] * 4096)
     # equal logits: a share of 1 / rows in each of at most 16 rows, 2^-20 for the quotient and the sum
     assert bool(((got - (own > 0).float()[:, None, None, None]).abs() <= 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("D,most", [(128, 64), (128, 5), (256, 40)])
+def test_a_cache_serves_calls_with_fewer_prefixes_than_it_has_room_for(torch_cuda, D, most):  # noqa: F811
+    torch = torch_cuda
+    from paper_2510_22556_amd import binding as B
+
+    n, H, G, page, m = 64, 2, 4, 16, 20
+    cache = B.PagedCache(n, 1, H * G, H, D, page, m + 2 * n, m + 2, torch.bfloat16, "cuda", bounds=False, n_prefixes=most)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(D + most)
+    for pool in (cache.k_pool, cache.v_pool):
+        pool.copy_(torch.randn(pool.shape, generator=gen, device="cuda"))
+    cache.page_table[:, :m] = torch.randperm(m, generator=gen, device="cuda").to(torch.int32)
+    cache.page_table[:, m:] = m + torch.arange(2 * n, device="cuda", dtype=torch.int32).view(n, 2)
+    cache.lengths.copy_(m * page + torch.arange(n, device="cuda") % 33)
+    q = torch.randn((n, 1, H * G, D), generator=gen, device="cuda").to(torch.bfloat16)
+    want, got = (torch.full(q.shape, NAN, device="cuda") for _ in range(2))
+    B.sablock_decode_paged(cache.pages, q, cache.k_pool, cache.v_pool, cache.page_table, cache.lengths, want, cache.ws)
+    for prefixes in sorted({1, 2, 3, 4, 7, 8, 31, 40, 64, most}):
+        if prefixes > most:
+            break
+        begin = torch.tensor([n * i // prefixes for i in range(prefixes + 1)], dtype=torch.int32, device="cuda")
+        B.sablock_decode_prefix_paged(cache.pages, q, cache.k_pool, cache.v_pool, cache.page_table, cache.lengths, begin,
+                                      torch.full((prefixes,), m, dtype=torch.int32, device="cuda"), got.fill_(NAN), cache.prefix_ws)
+        # either is off by 2^-16 of the largest value, see the test of the attention without prefixes
+        assert bool(((got - want).abs() <= 2 * 2.0 ** -16 * cache.v_pool.abs().max().float()).all()), prefixes

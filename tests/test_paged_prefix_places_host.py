@@ -1,6 +1,11 @@
-"""Where the pieces of common prefixes lie in the workspace, as the kernels count them (host code, no GPU needed)."""
+"""Where the pieces of common prefixes lie in the workspace, as the kernels count them, and its size (host code, no GPU needed)."""
 
-from test_host_logic import _run_host_code
+import ctypes
+
+import pytest
+
+from test_host_logic import _run_host_code, lib  # noqa: F401
+from test_paged_host import FAKE, _pages
 
 MANY = 4096
 
@@ -47,3 +52,30 @@ int main()
                 at = i * all_ + problem * pieces * blocks + blocks - 1
                 want += at + (pieces - 1) * blocks >= room
         assert refused == want, (room, all_, blocks)
+
+
+# sequences, query and KV heads, elements, fp32, and the most prefixes that go by many columns: above 64 columns on average, 16 where heads have more than 128 elements
+SHAPES = [(64, 32, 8, 128, False, 3), (64, 32, 8, 64, False, 3), (65, 8, 8, 128, False, 1), (64, 8, 8, 128, False, 0), (32, 32, 8, 256, False, 7), (200, 16, 1, 256, False, 199),
+          (4096, 16, 1, 32, False, 1023), (64, 32, 8, 128, True, 0), (3, 2, 1, 160, False, 0)]
+
+
+def _size(lib, pages, n):  # noqa: F811
+    size = ctypes.c_size_t(0)
+    assert lib.sablock_decode_prefix_paged_workspace_bytes(ctypes.byref(pages), n, ctypes.byref(size)) == 0
+    return size.value
+
+
+@pytest.mark.parametrize("n_seq,hq,hkv,D,f32,wide", SHAPES, ids=str)
+def test_a_workspace_serves_calls_with_fewer_prefixes(lib, n_seq, hq, hkv, D, f32, wide):  # noqa: F811
+    pages = _pages(n_seq=n_seq, n_layers=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=D, dtype=0 if f32 else 1,
+                   k_stride=dict(enumerate([0, hkv * 16 * D, 16 * D, D])), v_stride=dict(enumerate([0, hkv * 16 * D, 16 * D, D])))
+    sizes = [_size(lib, pages, n) for n in range(1, 4097)]
+    assert sizes == sorted(sizes)
+    # the call itself takes what its own number needs: less where its columns are few, and nothing less than that
+    call = lambda n, size: lib.sablock_decode_prefix_paged(ctypes.byref(pages), *[FAKE] * 7, n, FAKE, FAKE, size, None)  # noqa: E731
+    for n in {1, max(wide, 1), wide + 1, 64, 4096}:
+        assert call(n, 0) == 3
+        need = int(lib.sablock_last_error().decode().split("<")[1].split()[0])
+        assert need <= sizes[n - 1] and call(n, need - 1) == 3
+        assert need == sizes[n - 1] or n > wide > 0
+        assert all(need <= x for x in sizes[n - 1:])
