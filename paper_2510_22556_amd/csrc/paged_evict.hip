@@ -20,6 +20,8 @@ namespace {
 constexpr int KEY_ROWS = 4;                    // of a thread, in one page
 constexpr int KEY_WGS = 8;                     // workgroups of the keys per compute unit, at most
 
+constexpr uint32_t NO_ROW = 0;                 // the key of a row whose page does not exist: below every number's, -infinity among them
+
 __device__ __forceinline__ uint32_t row_key(float w) { return w == w ? ordered_key(w) : NOT_A_NUMBER; }
 
 // grid (parts, problems)
@@ -31,11 +33,12 @@ row_keys_kernel(PageDims d, PageView pv, const float *weights, uint32_t *keys, i
     const int64_t step = (int64_t)gridDim.x * NT * KEY_ROWS;
     for (int64_t r = ((int64_t)blockIdx.x * NT + threadIdx.x) * KEY_ROWS; r < n; r += step) {
         const int id = page_at(d, pv.table, s, (int)(r >> d.shift));
-        f32x4 w{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        if (id >= 0) w = *reinterpret_cast<const f32x4 *>(weights + weight_at(d, layer, id, head) + (r & (d.page - 1)));
-        u32x4 key;
+        u32x4 key{NO_ROW, NO_ROW, NO_ROW, NO_ROW};
+        if (id >= 0) {
+            const f32x4 w = *reinterpret_cast<const f32x4 *>(weights + weight_at(d, layer, id, head) + (r & (d.page - 1)));
 #pragma unroll
-        for (int i = 0; i < KEY_ROWS; ++i) key[i] = row_key(w[i]);
+            for (int i = 0; i < KEY_ROWS; ++i) key[i] = row_key(w[i]);
+        }
         *reinterpret_cast<u32x4 *>(keys + (int64_t)p * stride + r) = key;
     }
 }
@@ -101,7 +104,7 @@ pick_rows_kernel(PageDims d, PageView pv, EvictDims ed)
         const int r = min(tid * RUN + j, capacity - KEY_ROWS), id = page_at(d, pv.table, s, r >> d.shift);
         const f32x4 w = *reinterpret_cast<const f32x4 *>(ed.weights + weight_at(d, layer, max(id, 0), head) + (r & (d.page - 1)));
 #pragma unroll
-        for (int i = 0; i < KEY_ROWS; ++i) own[j + i] = id < 0 ? ordered_key(-INFINITY) : row_key(w[i]);
+        for (int i = 0; i < KEY_ROWS; ++i) own[j + i] = id < 0 ? NO_ROW : row_key(w[i]);
     }
     const int n = rows_of(d, pv.lengths, s);
     int32_t *list = ed.rows_out + (int64_t)p * ed.n_keep;
