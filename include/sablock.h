@@ -553,7 +553,8 @@ SABLOCK_API sablock_status sablock_decode_prefix_paged(const sablock_pages *page
  *   bounds         nullable; written for every page that gets a row
  *   ws             at least sablock_evict_paged_workspace_bytes(pages) bytes, 16-byte aligned
  * A row whose page does not exist has less weight than any number; where it stays all the same, it becomes a row of zeros of weight 0.
- * n_keep >= 1, n_first, n_last >= 0, n_first + n_last <= n_keep (INVALID_ARG otherwise). */
+ * n_keep >= 1, n_first, n_last >= 0, n_first + n_last <= n_keep (INVALID_ARG otherwise); min(n_keep, max_pages * page_size) rows fill fewer than 2^24
+ * pages (UNSUPPORTED otherwise). */
 SABLOCK_API sablock_status sablock_evict_paged_workspace_bytes(const sablock_pages *pages, size_t *bytes_out);
 SABLOCK_API sablock_status sablock_evict_paged(const sablock_pages *pages, const int32_t *page_table, const int32_t *lengths,
                                     int32_t n_keep, int32_t n_first, int32_t n_last, const int32_t *page_table_out,

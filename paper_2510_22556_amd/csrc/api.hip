@@ -957,6 +957,7 @@ sablock_status sablock_evict_paged(const sablock_pages *pages, const int32_t *pa
         return fail(SABLOCK_ERR_INVALID_ARG, "%s: the table and the lengths of the rows that stay are arrays of their own", who);
     if (n_keep < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > n_keep)
         return fail(SABLOCK_ERR_INVALID_ARG, "%s: need n_keep >= 1 and n_first + n_last <= n_keep, none negative", who);
+    if (evict_pages(pd, n_keep) >= 1 << 24) return fail(SABLOCK_ERR_UNSUPPORTED, "%s: the rows that stay may fill 2^24 - 1 pages at most", who);
     if (!aligned16(weights) || !aligned16(ws)) return fail(SABLOCK_ERR_INVALID_ARG, "%s: the weights and the workspace must be 16-byte aligned", who);
     PageView pv;
     st = make_page_view(who, page_table, lengths, k_pool, v_pool, bounds, &pv);

@@ -123,7 +123,7 @@ size_t evict_ws_bytes(const PageDims &d) { return align256((size_t)d.P * row_str
 
 hipError_t launch_evict(const PageDims &d, const PageView &pv, const EvictDims &ed, void *ws, hipStream_t st)
 {
-    const int64_t rows = row_stride(d), pages = (std::min<int64_t>(rows, ed.n_keep) + d.page - 1) >> d.shift, run = (rows + PICK_NT - 1) / PICK_NT;
+    const int64_t rows = row_stride(d), pages = evict_pages(d, ed.n_keep), run = (rows + PICK_NT - 1) / PICK_NT;
     const int chunks = d.D * elt_bytes(d) / 16;
     if (run <= 16) {                                           // keys per thread
         hipLaunchKernelGGL(run <= 4 ? pick_rows_kernel<4> : run <= 8 ? pick_rows_kernel<8> : pick_rows_kernel<16>, dim3(d.P), dim3(PICK_NT), 0, st, d, pv, ed);

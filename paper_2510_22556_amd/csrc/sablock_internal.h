@@ -366,6 +366,8 @@ struct EvictDims {
     int32_t *lengths_out, *rows_out;                          // rows_out [P][n_keep]
     int32_t n_keep, n_first, n_last;
 };
+// pages of the rows that stay of a sequence, at most: a workgroup each, and a grid's axis has places for 2^32 - 1 threads
+inline int64_t evict_pages(const PageDims &pd, int32_t n_keep) { return (std::min<int64_t>((int64_t)pd.max_pages << pd.shift, n_keep) + pd.page - 1) >> pd.shift; }
 size_t evict_ws_bytes(const PageDims &pd);
 hipError_t launch_evict(const PageDims &pd, const PageView &pv, const EvictDims &ed, void *ws, hipStream_t st);
 
