@@ -1,9 +1,9 @@
-// The paged cache's writers (what they share is in paged_rows.h, the appending kernel in paged_append.h): the retained rows of a compression into pages (end of Sec. 3.3), and new tokens behind them with
-// the position rotation of queries and keys on the way.  Both are copies, 16 bytes per lane, and both keep the page bounds: the
+// The paged cache's writers (what they share is in paged_rows.h, the appending kernel in paged_append.h): the retained rows of a compression into
+// pages (end of Sec. 3.3), and new tokens behind them with the position rotation of queries and keys on the way.  Both are copies, 16 bytes per lane, and both keep the page bounds: the
 // least and the largest value of every element of K over a page's rows, taken on order-preserving whole numbers (a
 // packed 16-bit minimum serves two bf16 elements) and joined over the rows of a workgroup through LDS.
 //
-// What bounds them: the copy.  A large device copy reaches 5.0-5.3 TB/s here, read and written.  Compaction of 32 layers x 8 heads,
+// What bounds them: the copy.  A large device copy reaches 4.9-5.4 TB/s here, read and written (2 GB and 0.5 GB).  Compaction of 32 layers x 8 heads,
 // 1 024 rows of 256 bytes each out of 32 768 (272 MB in and out): 61 us, 4.6 TB/s; several rows per thread in flight gain
 // nothing over one and eight workgroups per compute unit (61.1, 60.2 us).  Appended prompts, 11 300 tokens x 48 heads (278 MB): 69 us,
 // 4.0 TB/s, the rotation's vector instructions a third of that time beside it; without a rotation 68; fp32 130 us.  One token: 4.4 us in a graph, as

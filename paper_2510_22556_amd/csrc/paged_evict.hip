@@ -7,9 +7,10 @@
 //   evict_kernel       a workgroup fills one page of one problem: K, V and weights of its rows, and the page's bounds.  The rows' places are found
 //       once, by a thread each, and wait in LDS: list, table and row are loads that depend on each other.
 //
-// What bounds it: the copy.  32 layers x 8 heads of 4 sequences of up to 4 352 rows cut to 2 048 (1.75 GB moved and weighed): 376 us, 4.7 TB/s, as a large copy;
-// 358 of them the rows', 16.6 the choice.  A layer, 8 heads x 1 184 rows to 1 056: 11.0 us in a graph, two chains of dependent loads (6.8 and 5.1).
-// The choice in three launches took 3 us more there; choice and rows in one kernel 14.7 and 395 us.  Larger tables: 8 heads of 41 523 rows 41 us, of 131 072 97;
+// What bounds it: the copy.  32 layers x 8 heads of 4 sequences of up to 4 352 rows cut to 2 048 (1.75 GB moved and weighed): 377 us, 4.65 TB/s, where a copy
+// of as much reaches 5.2; 358 of them the rows', 16.6 the choice.  A layer, 8 heads x 1 184 rows to 1 056: 11.0 us in a graph, two chains of dependent loads (6.8 and 5.1).
+// The choice in three launches took 3 us more there; choice and rows in one kernel 14.7 and 395 us.  Larger tables, the choice still one workgroup per problem,
+// which reads its keys again in every pass: 8 heads of 41 523 rows 41 us, of 131 072 97;
 // one launch with up to 64 keys per thread 44 us for the first, 83 in place of 97 for 256 heads of 65 536 (37 registers spilled): not taken.
 #include "paged_pick.h"
 #include "paged_rows.h"

@@ -13,7 +13,9 @@
 // elements, 405 MB, 35 GFLOP, twice that with probabilities in three parts): 113-117 us where a large product's rate would take 59 and the reads 62;
 // the start takes 13 us and the pieces' sums are 17 MB to write and read again, 13 us of it their joining.  The common rows alone 107 us; products run at
 // 690 TFLOP/s over the kernel, at 957 over 131 072 common rows (287 us), and a large product's at 1 204.  Few columns: the chain of begins, lengths, table
-// and rows, and that of the second launch: 8 sequences x 2 048 common rows 15.0 us in a graph (12.8 and 4.6), the counting in 64 bits 1 more.
+// and rows, and that of the second launch: 8 sequences x 2 048 common rows 15.0 us in a graph (12.8 and 4.6), the counting in 64 bits 1 more.  The same
+// chains make the call slower than sablock_decode_paged, which finds common rows in the caches, where these are few: 8 sequences with 256 rows of their
+// own behind 512 common rows 13.8 us against 11.9, behind 2 048 14.6 against 17.7, 64 sequences behind 2 048 40 against 57, behind 32 768 105 against 859.
 // On the way, 64 x 32 768 and 8 x 2 048: in three launches, a wavefront's tiles fed from memory 238 and 28.9; an XCD's blocks of columns over the same
 // rows 184; K and V in LDS 160; the probabilities' parts by dot products 157; one launch for prefixes and own rows, the joins as one 122 and 18.1;
 // pieces over all XCDs however few 115.  Products of a step between the next one's vector instructions: 123 in place of 115, not taken.
@@ -468,8 +470,8 @@ template <int N> __device__ __forceinline__ void row_of_lds(uint32_t (&w)[N], co
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // The same for prefixes with many columns, bf16: a wavefront has columns of its own, 32 of the workgroup's 128 (or,
-// heads of more than 128 elements, 16 of 64), and all wavefronts do every step, from K and V in LDS.  Steps come there four (two) at a time, each wavefront seeing to a quarter of the pieces of
-// 1 KiB; a piece's rows lie in one page.  One barrier per step: everybody's pieces of this step have landed, and the last step's place is free.
+// heads of more than 128 elements, 16 of 64), and all wavefronts do every step, from K and V in LDS.  Steps come there four (two) at a time, each
+// wavefront seeing to a quarter of the pieces of 1 KiB; a piece's rows lie in one page.  One barrier per step: everybody's pieces of this step have landed, and the last step's place is free.
 // A row of K in LDS has its 16-byte chunks in the order of place(): the 16 rows of an operand, (m >> 2) * 8 + (m & 3) apart from 4, come from different banks.
 constexpr int wide_tiles(int D) { return D <= 128 ? 2 : 1; }
 constexpr int wide_columns(int D) { return NW * wide_tiles(D) * TILE; }
@@ -633,7 +635,8 @@ __device__ __forceinline__ void wide_prefixes(const PrefixArgs &a, char *lds)
             own.den[u] = over_quarters(own.den[u], false);
             const int col = column0 + u * TILE + m;
             if (col >= columns) continue;
-            const int64_t slot = (int64_t)x * WIDE + wave * CT * TILE + u * TILE + m;          // elements EP (4 c + w) + e of the column; EP = 16: 8 (4 c + w) + e of either half
+            // elements EP (4 c + w) + e of the column; EP = 16: 8 (4 c + w) + e of either half
+            const int64_t slot = (int64_t)x * WIDE + wave * CT * TILE + u * TILE + m;
             if (c == 0) *reinterpret_cast<f32x2 *>(a.piece_weights + slot * 2) = f32x2{own.ref[u], own.den[u]};
             constexpr int RUN = EP < 16 ? EP : 8;
             float *o = a.piece_sums + slot * D + RUN * 4 * c;
@@ -737,11 +740,11 @@ join_kernel(PrefixArgs a)
     *reinterpret_cast<out4 *>(out + 4 * c) = den == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : t / den;
 }
 
-// Prefixes have more than 64 columns on average, 16 where heads have more than 128 elements, and the rows of a step lie within reach of 31 bits.  Wide against narrow, 68 columns and 128: 2 048 rows 20.1 and
-// 21.5 us, 23.8 and 25.8; 8 192 rows 26.2 and 29.4, 30.3 and 34.0; 32 768 rows 57.5 and 56.7, 59.3 and 66.0.  64 columns, 32 768 rows: narrow 45.5.
+// Prefixes have more than 64 columns on average, 16 where heads have more than 128 elements, and the rows of a step lie within reach of 31 bits.  Wide
+// against narrow, 68 columns and 128: 2 048 rows 20.1 and 21.5 us, 23.8 and 25.8; 8 192 rows 26.2 and 29.4, 30.3 and 34.0; 32 768 rows 57.5 and 56.7, 59.3 and 66.0.  64 columns, 32 768 rows: narrow 45.5.
 // Heads of 256, 16 columns and 64: 2 048 rows 16.8 and 18.6 us, 24.4 and 26.2; 8 192 rows 26.1 and 27.9, 33.9 and 44.7; 32 768 rows 56.8 and 57.3, 68.4 and 132; 256
 // columns 215 and 561.
-int prefixes_wide(const PageDims &d)           // up to so many
+int prefixes_wide(const PageDims &d)           // so many prefixes at most
 {
     const int64_t reach = 31 * 2 * std::max(d.ks[3], d.vs[3]);
     return d.dtype == SABLOCK_BF16 && reach + 512 < (int64_t)1 << 31 ? (d.n_seq * d.G - 1) / (d.D <= 128 ? 64 : 16) : 0;
